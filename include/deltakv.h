@@ -10,7 +10,8 @@
  *     throws, aborts or prints;
  *   - a call that fails leaves the pool's state unchanged;
  *   - calls that launch GPU work (dk_kv_append, dk_delta_attend, dk_append_attend, their _sized
- *     forms, dk_delta_attend_noalloc, dk_seq_gather, dk_verify_greedy) are
+ *     forms, dk_delta_attend_noalloc, dk_scored_attend, dk_rotate_append, dk_rotate_rows,
+ *     dk_seq_gather, dk_verify_greedy, dk_token_logprobs) are
  *     asynchronous on the HIP stream passed as `stream` (a hipStream_t cast to void*,
  *     NULL = the default stream).  They never wait for the device and never allocate
  *     device or pinned memory: descriptors travel through the caller's staging memory
@@ -244,6 +245,93 @@ int32_t dk_delta_attend_noalloc(dk_pool* pool, int32_t n_seqs, const int32_t* sl
                                 float* lse, void* stream);
 
 /*
+ * scored_attend: dk_delta_attend for layers whose scores are not the plain scaled products.  Row p (the absolute position of
+ * a new token) of query head h against position k:
+ *   s  = scale * q.k
+ *   s' = cap * tanh(s / cap)            if cap > 0
+ *   s''= s' - slopes[h] * |p - k|       if slopes
+ * and the row sees the positions max(first, p - window + 1) .. max(p, prefix - 1) that exist (window, prefix and first where
+ * given; otherwise 0 .. p, as in dk_delta_attend).  A row that sees nothing gets zeros, and -infinity as its log-sum-exp.
+ * K and V at positions a row does not see have no influence on it, whatever they hold.
+ *   cap      >= 0, finite; 0: scores are not capped
+ *   slopes   DEVICE float [n_q_heads] or NULL, finite
+ *   window   >= 0; 0: no window
+ *   prefix   HOST int64 [n_seqs] or NULL, each >= 0: all rows of entry b see the positions below prefix[b], those after their
+ *            own among them (a bidirectional prefix; positions from n_b + Delta_b on do not exist)
+ *   first    HOST int64 [cu_delta[n_seqs]] or NULL, each >= 0: the row of that token sees no position below it (the start of
+ *            its document; past the end of the sequence: a padding row that sees nothing)
+ * The arrays are read at call time.  Everything else is as in dk_delta_attend, with these differences: scale may be any
+ * finite number; lse is that of s''; q, out, k_new and v_new are 16-byte aligned (else DK_ERR_UNSUPPORTED); a call whose
+ * descriptors do not fit the kernel arguments (about 3 KiB: 48 bytes a sequence, 32 for each of its runs of cells and for
+ * each work item, 4 a token where `first` is given) cannot be captured into a graph (DK_ERR_UNSUPPORTED); the workspace is at
+ * least dk_scored_workspace_bytes() for the same batch, lengths, mode (staged = 0 or 1) and masks.
+ */
+typedef struct {
+  float cap;
+  int32_t window;
+  const float* slopes;   /* DEVICE */
+  const int64_t* prefix; /* HOST */
+  const int64_t* first;  /* HOST */
+} dk_scores;
+int32_t dk_scored_workspace_bytes(dk_pool* pool, int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta,
+                                  int32_t staged, const dk_scores* scores, int64_t* bytes_out);
+int32_t dk_scored_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta, const void* q,
+                         const void* k_new, const void* v_new, float scale, const dk_scores* scores, void* out, float* lse,
+                         void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Rotary positions, with norms of queries and keys in the same pass.  Of every head x of Q and K:
+ *   y = x / sqrt(mean(x^2) + eps) * weight           if norm (weight NULL: ones)
+ *   the first rotary_dim elements of y in pairs (a, b), pair i turned by the angle t = position * inv_freq[i]:
+ *   (a, b) <- amplitude * (a cos t - b sin t, b cos t + a sin t)
+ * pairs 0: pair i is elements (i, i + rotary_dim / 2); pairs 1: elements (2 i, 2 i + 1).  The other elements are y as it is.
+ * Computed in fp32 (angles in fp64, so that far positions keep their digits) and rounded once.
+ *   rotary_dim  even, 0 .. head_dim (0: norms only);  inv_freq  DEVICE float [rotary_dim / 2], finite
+ *   weights     DEVICE [head_dim] of the rows' type, 16-byte aligned, or NULL
+ *   q, k, v     DEVICE, token t's heads at p + t * stride, [heads][head_dim] contiguous, so slices of a fused projection's
+ *               rows will do; strides (elements) at least a token's heads, pointers and strides multiples of 16 bytes
+ *               (DK_ERR_UNSUPPORTED otherwise)
+ *   q_out, k_out  DEVICE [tokens][heads][head_dim] contiguous.  They may be q / k themselves if those are contiguous; any other
+ *               overlap of an output with an input or another output is DK_ERR_INVALID
+ * dk_rotate_append is dk_kv_append with that: token i of entry b is at position len(slot_b) + i, its Q goes to q_out, its
+ *   K -- turned -- and V -- as it is -- into the slot's next cells.  Batch, errors and bookkeeping as for dk_kv_append without
+ *   n_accept.  Appends that go to more than 300 runs of consecutive cells upload a table of them through the staging memory
+ *   (DK_ERR_BUSY, DK_ERR_WORKSPACE as for dk_kv_append) and cannot be captured into a graph (DK_ERR_UNSUPPORTED).
+ * dk_rotate_rows turns rows at positions given by DEVICE int64 [n_tokens] (negative ones turn back) without a pool: Q and K
+ *   for a staged call.  Either head count may be 0 (its pointers are not looked at).  n_tokens < 2^31.  No state.
+ * dk_rotary_freqs (HOST) writes the inverse frequencies of a scaled rotation, float [rotary_dim / 2], to be copied to the
+ *   device; f_i = base^(-2 i / rotary_dim), params HOST double [4] (PLAIN: may be NULL):
+ *   PLAIN   f_i
+ *   LINEAR  f_i / params[0]
+ *   BASE    that of base * params[0]^(rotary_dim / (rotary_dim - 2))   (rotary_dim > 2)
+ *   BANDS   by the wavelength w = 2 pi / f_i against the original length L = params[3]: f_i below L / params[2], f_i / params[0]
+ *           above L / params[1], in between (1 - s) f_i / params[0] + s f_i with s = (L / w - params[1]) / (params[2] - params[1])
+ *   RAMP    (1 - s_i) f_i / params[0] + s_i f_i, s_i = 1 - clamp((i - lo) / (hi - lo), 0, 1) with lo and hi the pairs that turn
+ *           params[2] and params[1] times within L = params[3], rounded down and up and held to [0, rotary_dim - 1]
+ *           (params[1] <= params[2])
+ *   *amplitude_out (nullable): 0.1 ln(params[0]) + 1 for RAMP with params[0] > 1, else 1.
+ */
+typedef struct {
+  int32_t rotary_dim;
+  int32_t pairs;
+  const float* inv_freq; /* DEVICE */
+  float amplitude;
+  int32_t norm;
+  float eps;
+  const void* q_weight; /* DEVICE */
+  const void* k_weight; /* DEVICE */
+} dk_rotary;
+enum { DK_ROTARY_PLAIN = 0, DK_ROTARY_LINEAR = 1, DK_ROTARY_BASE = 2, DK_ROTARY_BANDS = 3, DK_ROTARY_RAMP = 4 };
+int32_t dk_rotate_append(dk_pool* pool, int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta, const dk_rotary* rotary,
+                         const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                         void* q_out, void* stream);
+int32_t dk_rotate_rows(int32_t dtype, int32_t head_dim, int64_t n_tokens, const int64_t* positions, const dk_rotary* rotary,
+                       int32_t n_q_heads, const void* q, int64_t q_stride, void* q_out, int32_t n_k_heads, const void* k,
+                       int64_t k_stride, void* k_out, void* stream);
+int32_t dk_rotary_freqs(int32_t rotary_dim, double base, int32_t scaling, const double* params, float* inv_freq_out,
+                        float* amplitude_out);
+
+/*
  * verify_greedy: the step after the Delta = k+1 verification pass of paper Alg. 2, on the device
  * (Sec. 3.8: greedy sampling is an argmax over the vocabulary logits, batched over the k+1
  * speculated positions, and the host never scans the logits).  Slot b's batch rows
@@ -269,6 +357,27 @@ int32_t dk_verify_greedy(int32_t n_seqs, int32_t total_rows, const int32_t* cu_d
                          int32_t dtype, int64_t vocab, int64_t row_stride, const int32_t* batch_tokens,
                          int32_t* argmax_out, int32_t* n_keep_out, int32_t* next_token_out, void* workspace,
                          int64_t workspace_bytes, void* stream);
+
+/*
+ * token_logprobs: what the distribution softmax(scale * logits) of every row says of a given token, and at large (next to
+ * dk_verify_greedy: what the emitted tokens were worth; scale is the inverse of the temperature, > 0 and finite).
+ *   logits        as for dk_verify_greedy: DEVICE [total_rows, row_stride], 16-byte aligned rows
+ *   tokens        DEVICE int32 [total_rows], or NULL (then logprob_out and rank_out are NULL)
+ *   logprob_out   DEVICE float [total_rows] or NULL: natural log of the token's probability
+ *   rank_out      DEVICE int32 [total_rows] or NULL: how many logits of the row are larger than the token's
+ *   entropy_out   DEVICE float [total_rows] or NULL: -sum p ln p, natural log; logits of -infinity contribute nothing
+ *   top_ids_out   DEVICE int32 [total_rows, n_top], required with n_top > 0: the row's n_top largest logits, largest first,
+ *                 ties in the order of their ids;  top_logprobs_out  DEVICE float, likewise, or NULL
+ *   n_top         0 .. 32 (DK_ERR_UNSUPPORTED above), at most vocab
+ * A token outside [0, vocab) has log probability -infinity and rank vocab.  In a row that holds a NaN or +infinity, or nothing
+ * but -infinity, log probabilities and entropy are NaN; rank and ids count a NaN as +infinity, as dk_verify_greedy does.
+ *   workspace     DEVICE, 256-byte aligned, >= dk_logprobs_workspace_bytes() for the same arguments
+ * total_rows and vocab < 2^31.  Asynchronous on `stream`; stateless, needs no pool; allocates nothing.
+ */
+int32_t dk_logprobs_workspace_bytes(int32_t total_rows, int64_t vocab, int32_t dtype, int32_t n_top, int64_t* bytes_out);
+int32_t dk_token_logprobs(int32_t total_rows, const void* logits, int32_t dtype, int64_t vocab, int64_t row_stride, float scale,
+                          const int32_t* tokens, float* logprob_out, int32_t* rank_out, float* entropy_out, int32_t n_top,
+                          int32_t* top_ids_out, float* top_logprobs_out, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
  * Radix prefix cache and the per-turn procedure of paper Alg. 1 (Sec. 3.3), HOST only.  The trie is keyed

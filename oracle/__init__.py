@@ -36,3 +36,4 @@ from .costmodel import (  # noqa: F401
     kv_entry_bytes,
     kv_cell_bytes,
 )
+from .operators import scored_attend, rotate, token_logprobs  # noqa: F401

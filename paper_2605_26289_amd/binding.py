@@ -37,6 +37,16 @@ class PoolDesc(C.Structure):
                 ("host_staging_bytes", C.c_int64), ("staging_depth", C.c_int32)]
 
 
+class ScoresDesc(C.Structure):
+    _fields_ = [("cap", C.c_float), ("window", C.c_int32), ("slopes", C.c_void_p), ("prefix", C.c_void_p),
+                ("first", C.c_void_p)]
+
+
+class RotaryDesc(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("pairs", C.c_int32), ("inv_freq", C.c_void_p), ("amplitude", C.c_float),
+                ("norm", C.c_int32), ("eps", C.c_float), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p)]
+
+
 _lib = None
 
 _I32P = C.POINTER(C.c_int32)
@@ -81,6 +91,19 @@ SIGNATURES = {
     "dk_verify_greedy": (C.c_int32, [C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64,
                                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
                                      C.c_void_p]),
+    "dk_scored_workspace_bytes": (C.c_int32, [C.c_void_p, C.c_int32, _ARRAY, _ARRAY, C.c_int32, C.c_void_p, _I64P]),
+    "dk_scored_attend": (C.c_int32, [C.c_void_p, C.c_int32, _ARRAY, _ARRAY, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
+    "dk_rotate_append": (C.c_int32, [C.c_void_p, C.c_int32, _ARRAY, _ARRAY, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p,
+                                     C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+    "dk_rotate_rows": (C.c_int32, [C.c_int32, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
+                                   C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+    "dk_rotary_freqs": (C.c_int32, [C.c_int32, C.c_double, C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_float),
+                                    C.POINTER(C.c_float)]),
+    "dk_logprobs_workspace_bytes": (C.c_int32, [C.c_int32, C.c_int64, C.c_int32, C.c_int32, _I64P]),
+    "dk_token_logprobs": (C.c_int32, [C.c_int32, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_float, C.c_void_p,
+                                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                      C.c_int64, C.c_void_p]),
     "dk_radix_create": (C.c_int32, [C.c_void_p, C.c_int64, C.c_int32, C.POINTER(C.c_void_p)]),
     "dk_radix_destroy": (C.c_int32, [C.c_void_p]),
     "dk_radix_begin_turn": (C.c_int32, [C.c_void_p, C.c_int32, _I32P, C.c_int64, _I64P]),
@@ -334,6 +357,120 @@ def verify_greedy(n_seqs: int, total_rows: int, cu_delta_dev, logits, dtype: int
                                   int(vocab), int(row_stride), _ptr(batch_tokens), _ptr(argmax_out),
                                   _ptr(n_keep_out), _ptr(next_token_out), _ptr(workspace), ws_bytes,
                                   _stream(stream)), "verify_greedy")
+
+
+class Scores:
+    """How scored_attend changes the scores of a batch (dk_scores): kept by the caller, with the arrays it points to.
+
+    slopes: float32 device tensor, one per query head; prefix: one position per sequence; first: one per new token."""
+
+    def __init__(self, cap: float = 0.0, slopes=None, window: int = 0, prefix=None, first=None):
+        self.slopes = slopes
+        self.prefix = None if prefix is None else np.ascontiguousarray(prefix, dtype=np.int64)
+        self.first = None if first is None else np.ascontiguousarray(first, dtype=np.int64)
+        self.desc = ScoresDesc(cap, window, _ptr(slopes), None if prefix is None else self.prefix.ctypes.data,
+                               None if first is None else self.first.ctypes.data)
+        self.address = C.addressof(self.desc)
+
+    def check(self, n_seqs: int, tokens: int, n_q_heads: Optional[int] = None) -> None:
+        """The arrays' lengths, which the library cannot see."""
+        if ((self.prefix is not None and self.prefix.shape != (n_seqs,)) or (self.first is not None and self.first.shape != (tokens,))
+                or (self.slopes is not None and n_q_heads is not None and self.slopes.numel() != n_q_heads)):
+            raise DeltaKVError(-1, "scores", "prefix is one per sequence, first one per new token, slopes one per query head")
+
+
+def scored_workspace_bytes(pool, slots, cu_delta, staged, scores: Scores) -> int:
+    s_arr, s_p = _array(slots)
+    c_arr, c_p = _array(cu_delta)
+    scores.check(len(s_arr), int(c_arr[-1]) if len(s_arr) else 0)
+    out = C.c_int64()
+    _check(lib().dk_scored_workspace_bytes(pool, len(s_arr), s_p, c_p, int(staged), scores.address, C.byref(out)),
+           "scored_workspace_bytes", pool)
+    return out.value
+
+
+def scored_attend(pool, slots, cu_delta, q, out, scale: float, scores: Scores, k_new=None, v_new=None, lse=None,
+                  workspace=None, stream=None) -> None:
+    s_arr, s_p = _array(slots)
+    c_arr, c_p = _array(cu_delta)
+    scores.check(len(s_arr), int(c_arr[-1]) if len(s_arr) else 0, q.shape[1])
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _launch(lib().dk_scored_attend, (pool, len(s_arr), s_p, c_p, _ptr(q), _ptr(k_new), _ptr(v_new), float(scale),
+                                     scores.address, _ptr(out), _ptr(lse), _ptr(workspace), ws_bytes, _stream(stream)),
+            "scored_attend", pool)
+
+
+class Rotary:
+    """Norms and rotation of Q and K (dk_rotary): kept by the caller, with the tensors it points to.
+
+    inv_freq: float32 device tensor of rotary_dim / 2; norm_eps None: no norm; weights: head_dim of the rows' type."""
+
+    def __init__(self, rotary_dim: int, inv_freq=None, pairs: bool = False, amplitude: float = 1.0,
+                 norm_eps: Optional[float] = None, q_weight=None, k_weight=None):
+        if inv_freq is not None and (inv_freq.numel() < rotary_dim // 2 or inv_freq.element_size() != 4):
+            raise DeltaKVError(-1, "rotary", "inv_freq is float32 [rotary_dim / 2]")
+        self.tensors = (inv_freq, q_weight, k_weight)
+        self.desc = RotaryDesc(rotary_dim, int(pairs), _ptr(inv_freq), amplitude, int(norm_eps is not None), norm_eps or 0.0,
+                               _ptr(q_weight), _ptr(k_weight))
+        self.address = C.addressof(self.desc)
+
+
+def _heads(t, where: str):
+    """(address, elements from token to token) of [tokens, heads, head_dim] rows whose tokens are contiguous"""
+    if t.dim() != 3 or (t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]))):
+        raise DeltaKVError(-1, where, "rows are [tokens, heads, head_dim], each token's contiguous")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2])
+
+
+def rotate_append(pool, slots, cu_delta, q, k, v, rotary: Rotary, q_out, stream=None) -> None:
+    """q, k, v: [tokens, heads, head_dim], strided over tokens; q_out contiguous."""
+    s_arr, s_p = _array(slots)
+    c_arr, c_p = _array(cu_delta)
+    _launch(lib().dk_rotate_append, (pool, len(s_arr), s_p, c_p, rotary.address, *_heads(q, "rotate_append"),
+                                     *_heads(k, "rotate_append"), *_heads(v, "rotate_append"), _ptr(q_out), _stream(stream)),
+            "rotate_append", pool)
+
+
+def rotate_rows(positions, q, k, rotary: Rotary, q_out, k_out, stream=None) -> None:
+    """positions: int64 device tensor; q or k may be None."""
+    some = q if q is not None else k
+    dtype = BF16 if some.element_size() == 2 else F32
+    args = []
+    for x, out in ((q, q_out), (k, k_out)):
+        args += [0, None, 0, None] if x is None else [x.shape[1], *_heads(x, "rotate_rows"), _ptr(out)]
+    _check(lib().dk_rotate_rows(dtype, some.shape[2], some.shape[0], _ptr(positions), rotary.address, *args, _stream(stream)),
+           "rotate_rows")
+
+
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_BANDS, ROTARY_RAMP = range(5)
+
+
+def rotary_freqs(rotary_dim: int, base: float, scaling: int = ROTARY_PLAIN, params=None):
+    """(float32 inverse frequencies, amplitude) of a scaled rotation (dk_rotary_freqs)"""
+    out = np.zeros(max(rotary_dim // 2, 1), dtype=np.float32)
+    amplitude = C.c_float()
+    p = None if params is None else (C.c_double * 4)(*params)
+    _check(lib().dk_rotary_freqs(rotary_dim, float(base), scaling, p, out.ctypes.data_as(C.POINTER(C.c_float)),
+                                 C.byref(amplitude)), "rotary_freqs")
+    return out[: rotary_dim // 2], amplitude.value
+
+
+def logprobs_workspace_bytes(total_rows: int, vocab: int, dtype: int, n_top: int = 0) -> int:
+    out = C.c_int64()
+    _check(lib().dk_logprobs_workspace_bytes(int(total_rows), int(vocab), int(dtype), int(n_top), C.byref(out)),
+           "logprobs_workspace_bytes")
+    return out.value
+
+
+def token_logprobs(total_rows: int, logits, dtype: int, vocab: int, row_stride: int, tokens, logprob_out, workspace,
+                   scale: float = 1.0, rank_out=None, entropy_out=None, n_top: int = 0, top_ids_out=None,
+                   top_logprobs_out=None, stream=None) -> None:
+    """All tensors are device tensors; nothing is synchronised."""
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().dk_token_logprobs(int(total_rows), _ptr(logits), int(dtype), int(vocab), int(row_stride), float(scale),
+                                   _ptr(tokens), _ptr(logprob_out), _ptr(rank_out), _ptr(entropy_out), int(n_top),
+                                   _ptr(top_ids_out), _ptr(top_logprobs_out), _ptr(workspace), ws_bytes, _stream(stream)),
+           "token_logprobs")
 
 
 # -- host-only: radix prefix cache, prompt lookup, scheduler helpers ---------------------------------------

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <chrono>
 #include <cstdio>
 #include <cstdlib>
@@ -15,6 +16,7 @@
 #include "../../include/deltakv.h"
 #include "kernels.hpp"
 #include "plan.hpp"
+#include "plan_scored.hpp"
 #include "pool.hpp"
 #include "radix.hpp"
 
@@ -79,6 +81,7 @@ struct dk_pool {
   std::mutex launch_mu;  // serialises GPU-launching calls (shared staging ring, dev_meta and plan)
   dk::AttendPlan plan;   // reused from call to call so that steady-state planning allocates nothing
   int64_t last_plan[DK_PLAN_FIELDS] = {-1};  // see dk_last_plan
+  dk::ScoredPlan scored_plan;  // likewise, for dk_scored_attend
   std::vector<int64_t> append_cells, append_old_len;  // likewise, for the bookkeeping of appends
 
   dk_pool(const dk_pool_desc& d, int32_t granule)
@@ -809,6 +812,270 @@ int32_t dk_last_plan(dk_pool* pool, int64_t* fields_out) {
 
 }  // extern "C"
 
+namespace {
+
+// Masks of a call, if its description is one.
+int32_t score_masks(const dk_scores* scores, dk::ScoreMasks* out) {
+  if (!scores || !(scores->cap >= 0.f) || !(scores->cap <= FLT_MAX) || scores->window < 0) return DK_ERR_INVALID;
+  *out = {scores->window, scores->prefix, scores->first};
+  return DK_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t dk_scored_workspace_bytes(dk_pool* pool, int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta,
+                                  int32_t staged, const dk_scores* scores, int64_t* bytes_out) {
+  if (!pool || !bytes_out || staged < 0 || staged > 1) return DK_ERR_INVALID;
+  return guarded([&]() -> int32_t {
+    std::lock_guard<std::mutex> launch(pool->launch_mu);
+    dk::ScoreMasks masks;
+    int32_t rc = score_masks(scores, &masks);
+    if (rc != DK_OK) return rc;
+    std::lock_guard<std::mutex> lk(pool->meta.mutex());
+    rc = dk::build_scored_plan(pool->meta, n_seqs, slots, cu_delta, staged != 0, masks, &pool->scored_plan);
+    if (rc == DK_OK) *bytes_out = (int64_t)pool->scored_plan.total_bytes;
+    return rc;
+  });
+}
+
+int32_t dk_scored_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta, const void* q,
+                         const void* k_new, const void* v_new, float scale, const dk_scores* scores, void* out, float* lse,
+                         void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!pool || (k_new == nullptr) != (v_new == nullptr) || !(scale >= -FLT_MAX && scale <= FLT_MAX)) return DK_ERR_INVALID;
+  return guarded([&]() -> int32_t {
+    std::lock_guard<std::mutex> launch(pool->launch_mu);
+    hipStream_t st = (hipStream_t)stream;
+    dk::ScoredPlan& plan = pool->scored_plan;
+    dk::ScoreMasks masks;
+    int32_t rc = score_masks(scores, &masks);
+    if (rc != DK_OK) return rc;
+    {
+      std::lock_guard<std::mutex> lk(pool->meta.mutex());
+      rc = dk::build_scored_plan(pool->meta, n_seqs, slots, cu_delta, k_new != nullptr, masks, &plan);
+      if (rc != DK_OK) return rc;
+    }
+    if (plan.total_tokens == 0) return DK_OK;
+    if (!q || !out) return DK_ERR_INVALID;
+    // rows move in pieces of 16 bytes
+    if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)k_new | (uintptr_t)v_new) & 15) return DK_ERR_UNSUPPORTED;
+    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < (int64_t)plan.total_bytes) return DK_ERR_WORKSPACE;
+    const bool inline_blob = plan.blob_bytes <= (size_t)dk::INLINE_BLOB_BYTES;
+    // a captured upload would be replayed from a staging buffer that has other descriptors by then
+    if (!inline_blob && pool->ring_size > 0 && capturing(st)) return DK_ERR_UNSUPPORTED;
+    dk::InlineBlob blob_args{};
+    char* h = (char*)&blob_args;
+    Staging* s = nullptr;
+    if (!inline_blob) {
+      rc = pool->stage(plan.blob_bytes, &s);
+      if (rc != DK_OK) return rc;
+      h = s->host;
+    }
+    const auto put = [&](size_t off, const void* src, size_t bytes) { if (bytes) std::memcpy(h + off, src, bytes); };
+    put(plan.off_entries, plan.entries.data(), plan.entries.size() * sizeof(DkEntry));
+    put(plan.off_segs, plan.segs.data(), plan.segs.size() * sizeof(DkSeg));
+    put(plan.off_first, plan.first.data(), plan.first.size() * sizeof(int32_t));
+    if (!inline_blob) {
+      rc = pool->upload(s, workspace, plan.blob_bytes, st);
+      if (rc != DK_OK) return rc;
+    }
+    const uintptr_t desc = inline_blob ? 0 : (uintptr_t)workspace;
+    dk::AttendArgs a;
+    a.inline_blob = inline_blob ? &blob_args : nullptr;
+    a.arena = pool->view();
+    a.entries = (const DkEntry*)(desc + plan.off_entries);
+    a.n_entries = (int32_t)plan.entries.size();
+    a.segs = (const DkSeg*)(desc + plan.off_segs);
+    a.q = q;
+    a.k_new = k_new;
+    a.v_new = v_new;
+    a.out = out;
+    a.lse = lse;
+    a.scale = scale;
+    a.total_tokens = (int32_t)plan.total_tokens;
+    dk::ScoreArgs sc;
+    sc.cap = scores->cap;
+    sc.slopes = scores->slopes;
+    sc.window = scores->window;
+    sc.masked_first = masks.first != nullptr;
+    sc.first = (const int32_t*)(desc + plan.off_first);
+    const hipError_t e = dk::launch_attend_scored(a, sc, st);
+    return e == hipSuccess ? DK_OK : pool->hip_fail(e);
+  });
+}
+
+}  // extern "C"
+
+namespace {
+
+// A rotation of heads of this width, and whether rows of `elem` bytes can be read the way the kernels read them.
+int32_t rotary_ok(const dk_rotary* r, int32_t head_dim) {
+  if (!r || r->rotary_dim < 0 || r->rotary_dim > head_dim || r->rotary_dim % 2 || (r->rotary_dim > 0 && !r->inv_freq))
+    return DK_ERR_INVALID;
+  if (!(r->amplitude >= -FLT_MAX && r->amplitude <= FLT_MAX) || (r->norm && !(r->eps >= 0.f && r->eps <= FLT_MAX)))
+    return DK_ERR_INVALID;
+  if (((uintptr_t)r->q_weight | (uintptr_t)r->k_weight) & 15) return DK_ERR_UNSUPPORTED;
+  return DK_OK;
+}
+
+struct Span {
+  uintptr_t lo = 0, hi = 0;
+};
+Span span_of(const void* p, int64_t n_tok, int64_t stride, int64_t row, int64_t elem) {
+  if (!p || n_tok <= 0) return {};
+  return {(uintptr_t)p, (uintptr_t)p + (uintptr_t)(((n_tok - 1) * stride + row) * elem)};
+}
+bool overlap(const Span& a, const Span& b) { return a.lo < b.hi && b.lo < a.hi; }
+
+// Checks rows of `heads` heads a token: `in`, strided, and `out`, contiguous.
+int32_t rotary_rows_ok(const void* in, int64_t stride, const void* out, int64_t row, int64_t elem) {
+  if (!in || !out || stride < row) return DK_ERR_INVALID;
+  if ((((uintptr_t)in | (uintptr_t)out) & 15) || (stride * elem) % 16) return DK_ERR_UNSUPPORTED;
+  return DK_OK;
+}
+
+dk::RotaryArgs rotary_args(const dk_rotary* r, int32_t dtype, int32_t head_dim, int32_t n_q_heads, int32_t n_k_heads) {
+  dk::RotaryArgs a{};
+  a.dtype = dtype;
+  a.head_dim = head_dim;
+  a.n_q_heads = n_q_heads;
+  a.n_k_heads = n_k_heads;
+  a.rotary_dim = r->rotary_dim;
+  a.pairs = r->pairs != 0;
+  a.norm = r->norm != 0;
+  a.eps = r->eps;
+  a.amplitude = r->amplitude;
+  a.inv_freq = r->inv_freq;
+  a.q_weight = r->q_weight;
+  a.k_weight = r->k_weight;
+  return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t dk_rotate_append(dk_pool* pool, int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta, const dk_rotary* rotary,
+                         const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                         void* q_out, void* stream) {
+  if (!pool) return DK_ERR_INVALID;
+  return guarded([&]() -> int32_t {
+    std::lock_guard<std::mutex> launch(pool->launch_mu);
+    const dk_pool_desc& d = pool->desc;
+    int32_t rc = rotary_ok(rotary, d.head_dim);
+    if (rc != DK_OK) return rc;
+    {  // the batch is checked before its lengths are looked at
+      std::lock_guard<std::mutex> lk(pool->meta.mutex());
+      rc = pool->meta.check_batch(n_seqs, slots, cu_delta);
+      if (rc != DK_OK) return rc;
+    }
+    const int64_t total = n_seqs > 0 ? cu_delta[n_seqs] : 0;
+    if (total == 0) return DK_OK;
+    const int64_t elem = d.dtype == DK_BF16 ? 2 : 4, q_row = (int64_t)d.n_q_heads * d.head_dim, k_row = (int64_t)d.n_kv_heads * d.head_dim;
+    if ((rc = rotary_rows_ok(q, q_stride, q_out, q_row, elem)) != DK_OK) return rc;
+    if ((rc = rotary_rows_ok(k, k_stride, d.k_arena, k_row, elem)) != DK_OK) return rc;
+    if ((rc = rotary_rows_ok(v, v_stride, d.v_arena, k_row, elem)) != DK_OK) return rc;
+    const Span qo = span_of(q_out, total, q_row, q_row, elem);
+    if (!(q_out == q && q_stride == q_row) && overlap(qo, span_of(q, total, q_stride, q_row, elem))) return DK_ERR_INVALID;
+    if (overlap(qo, span_of(k, total, k_stride, k_row, elem)) || overlap(qo, span_of(v, total, v_stride, k_row, elem)))
+      return DK_ERR_INVALID;
+    const int64_t per_launch = std::min<int64_t>(d.dev_meta_bytes, (int64_t)pool->stage_cap) / (2 * (int64_t)sizeof(int32_t));
+    std::vector<int64_t>& dst = pool->append_cells;
+    std::vector<int64_t>& old_len = pool->append_old_len;
+    rc = pool->meta.append(n_seqs, slots, cu_delta, nullptr, &dst, &old_len);
+    if (rc != DK_OK) return rc;
+    const auto undo = [&](int32_t status) {
+      undo_append(pool, n_seqs, slots, old_len);
+      return status;
+    };
+    for (int32_t b = 0; b < n_seqs; ++b)
+      if (old_len[b] + cu_delta[b + 1] - cu_delta[b] > INT32_MAX / 2) return undo(DK_ERR_UNSUPPORTED);
+    dk::RotaryArgs a = rotary_args(rotary, d.dtype, d.head_dim, d.n_q_heads, d.n_kv_heads);
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.q_out = q_out;
+    a.k_out = d.k_arena;
+    a.v_out = d.v_arena;
+    a.arena_cells = pool->meta_arena_cells;
+    hipStream_t st = (hipStream_t)stream;
+    // The runs of cells and positions travel in the kernel arguments where they fit; else a table of every token's is uploaded.
+    dk::RotaryRuns runs;
+    int32_t n_runs = 0, b = 0;
+    int64_t t = 0;
+    while (t < total && n_runs < dk::ROTARY_INLINE_MAX_RUNS) {
+      while (cu_delta[b + 1] <= t) ++b;
+      runs.tok[n_runs] = (int32_t)t;
+      runs.cell[n_runs] = (int32_t)dst[t];
+      runs.pos[n_runs++] = (int32_t)(old_len[b] + t - cu_delta[b]);
+      for (++t; t < cu_delta[b + 1] && dst[t] == dst[t - 1] + 1; ++t) {
+      }
+    }
+    if (t == total) {
+      runs.tok[n_runs] = (int32_t)total;
+      const hipError_t e = dk::launch_rotate_append(a, runs, n_runs, (int32_t)total, st);
+      return e == hipSuccess ? DK_OK : undo(pool->hip_fail(e));
+    }
+    if (per_launch <= 0) return undo(DK_ERR_WORKSPACE);
+    // a captured upload would be replayed from a staging buffer that has other descriptors by then
+    if (capturing(st)) return undo(DK_ERR_UNSUPPORTED);
+    b = 0;
+    for (int64_t base = 0; base < total; base += per_launch) {
+      const int32_t n = (int32_t)std::min<int64_t>(per_launch, total - base);
+      Staging* s;
+      rc = pool->stage((size_t)n * 2 * sizeof(int32_t), &s);
+      if (rc != DK_OK) return undo(rc);
+      int32_t* h = (int32_t*)s->host;
+      for (int32_t i = 0; i < n; ++i) {
+        while (cu_delta[b + 1] <= base + i) ++b;
+        h[2 * i] = (int32_t)(old_len[b] + base + i - cu_delta[b]);
+        h[2 * i + 1] = (int32_t)dst[base + i];
+      }
+      rc = pool->upload(s, d.dev_meta, (size_t)n * 2 * sizeof(int32_t), st);
+      if (rc != DK_OK) return undo(rc);
+      const hipError_t e = dk::launch_rotate_append_table(a, (const int32_t*)d.dev_meta, (int32_t)base, n, st);
+      if (e != hipSuccess) return undo(pool->hip_fail(e));
+    }
+    return DK_OK;
+  });
+}
+
+int32_t dk_rotate_rows(int32_t dtype, int32_t head_dim, int64_t n_tokens, const int64_t* positions, const dk_rotary* rotary,
+                       int32_t n_q_heads, const void* q, int64_t q_stride, void* q_out, int32_t n_k_heads, const void* k,
+                       int64_t k_stride, void* k_out, void* stream) {
+  if (n_tokens < 0 || n_q_heads < 0 || n_k_heads < 0 || head_dim <= 0) return DK_ERR_INVALID;
+  if ((head_dim != 64 && head_dim != 128) || (dtype != DK_F32 && dtype != DK_BF16)) return DK_ERR_UNSUPPORTED;
+  int32_t rc = rotary_ok(rotary, head_dim);
+  if (rc != DK_OK) return rc;
+  if (n_tokens == 0 || (n_q_heads == 0 && n_k_heads == 0)) return DK_OK;
+  if (!positions) return DK_ERR_INVALID;
+  if (n_tokens > INT32_MAX || (int64_t)n_q_heads * head_dim > INT32_MAX / 4 || (int64_t)n_k_heads * head_dim > INT32_MAX / 4)
+    return DK_ERR_UNSUPPORTED;
+  const int64_t elem = dtype == DK_BF16 ? 2 : 4, q_row = (int64_t)n_q_heads * head_dim, k_row = (int64_t)n_k_heads * head_dim;
+  if (n_q_heads > 0 && (rc = rotary_rows_ok(q, q_stride, q_out, q_row, elem)) != DK_OK) return rc;
+  if (n_k_heads > 0 && (rc = rotary_rows_ok(k, k_stride, k_out, k_row, elem)) != DK_OK) return rc;
+  const Span qi = n_q_heads ? span_of(q, n_tokens, q_stride, q_row, elem) : Span{}, qo = n_q_heads ? span_of(q_out, n_tokens, q_row, q_row, elem) : Span{};
+  const Span ki = n_k_heads ? span_of(k, n_tokens, k_stride, k_row, elem) : Span{}, ko = n_k_heads ? span_of(k_out, n_tokens, k_row, k_row, elem) : Span{};
+  if ((overlap(qo, qi) && !(q_out == q && q_stride == q_row)) || (overlap(ko, ki) && !(k_out == k && k_stride == k_row)) ||
+      overlap(qo, ki) || overlap(ko, qi) || overlap(qo, ko))
+    return DK_ERR_INVALID;
+  dk::RotaryArgs a = rotary_args(rotary, dtype, head_dim, n_q_heads, n_k_heads);
+  a.q = q;
+  a.k = k;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  const hipError_t e = dk::launch_rotate_rows(a, positions, n_tokens, (hipStream_t)stream);
+  return e == hipSuccess ? DK_OK : DK_ERR_HIP;
+}
+
+}  // extern "C"
+
 struct dk_radix {
   dk_pool* pool;
   dk::Radix trie;
@@ -887,6 +1154,33 @@ int32_t dk_verify_greedy(int32_t n_seqs, int32_t total_rows, const int32_t* cu_d
   hipError_t e = dk::launch_verify_greedy(n_seqs, total_rows, cu_delta_dev, logits, dtype, vocab, row_stride,
                                           batch_tokens, argmax_out, n_keep_out, next_token_out, workspace,
                                           (hipStream_t)stream);
+  return e == hipSuccess ? DK_OK : DK_ERR_HIP;
+}
+
+int32_t dk_logprobs_workspace_bytes(int32_t total_rows, int64_t vocab, int32_t dtype, int32_t n_top, int64_t* bytes_out) {
+  if (!bytes_out || total_rows < 0 || vocab <= 0 || vocab > INT32_MAX || n_top < 0 || n_top > vocab) return DK_ERR_INVALID;
+  if ((dtype != DK_F32 && dtype != DK_BF16) || n_top > dk::LOGPROBS_MAX_TOP) return DK_ERR_UNSUPPORTED;
+  *bytes_out = dk::logprobs_workspace_bytes(total_rows, vocab, dtype, n_top);
+  return DK_OK;
+}
+
+int32_t dk_token_logprobs(int32_t total_rows, const void* logits, int32_t dtype, int64_t vocab, int64_t row_stride, float scale,
+                          const int32_t* tokens, float* logprob_out, int32_t* rank_out, float* entropy_out, int32_t n_top,
+                          int32_t* top_ids_out, float* top_logprobs_out, void* workspace, int64_t workspace_bytes, void* stream) {
+  int64_t need = 0;
+  const int32_t rc = dk_logprobs_workspace_bytes(total_rows, vocab, dtype, n_top, &need);
+  if (rc != DK_OK) return rc;
+  if (row_stride < vocab || !(scale > 0.f) || !(scale <= FLT_MAX)) return DK_ERR_INVALID;
+  if (total_rows == 0) return DK_OK;
+  if (!logits || (!tokens && (logprob_out || rank_out)) || (n_top > 0 && !top_ids_out) || (n_top == 0 && (top_ids_out || top_logprobs_out)))
+    return DK_ERR_INVALID;
+  const int64_t elem = dtype == DK_BF16 ? 2 : 4;
+  // rows are read with 16-byte loads
+  if (((uintptr_t)logits & 15) || (row_stride * elem) % 16) return DK_ERR_UNSUPPORTED;
+  if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return DK_ERR_WORKSPACE;
+  const dk::LogprobArgs a{logits, dtype, total_rows, vocab, row_stride, scale, n_top, tokens, logprob_out, rank_out, entropy_out,
+                          top_ids_out, top_logprobs_out};
+  const hipError_t e = dk::launch_token_logprobs(a, workspace, (hipStream_t)stream);
   return e == hipSuccess ? DK_OK : DK_ERR_HIP;
 }
 

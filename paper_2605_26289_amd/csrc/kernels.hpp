@@ -111,11 +111,69 @@ hipError_t launch_attend_stream(const AttendArgs& a, const DkItem* items, const 
 hipError_t launch_attend_merge(const AttendArgs& a, const DkMerge* merges, int32_t n_merges, int32_t max_rows,
                                int32_t max_split, hipStream_t stream);
 
+// Attention with changed scores.
+struct ScoreArgs {
+  float cap = 0.f;                  // > 0: scores are capped
+  const float* slopes = nullptr;    // [n_q_heads]: bias by distance
+  int32_t window = 0;               // > 0: a row sees its own position and window - 1 before it
+  const int32_t* first = nullptr;   // with masked_first (a descriptor): [tokens], first position that the row sees
+  bool masked_first = false;
+};
+hipError_t launch_attend_scored(const AttendArgs& a, const ScoreArgs& sc, hipStream_t stream);
+
 // Greedy verification (argmax per logits row, accepted-draft count and next token per slot).
 int64_t verify_workspace_bytes(int32_t total_rows, int64_t vocab, int32_t dtype);
 hipError_t launch_verify_greedy(int32_t n_seqs, int32_t total_rows, const int32_t* cu_delta_dev, const void* logits,
                                 int32_t dtype, int64_t vocab, int64_t row_stride, const int32_t* batch_tokens,
                                 int32_t* argmax_out, int32_t* n_keep_out, int32_t* next_token_out, void* workspace,
                                 hipStream_t stream);
+
+// Log probabilities of given tokens, their rank, entropy and the best alternatives, a logits row each.
+constexpr int32_t LOGPROBS_MAX_TOP = 32;
+struct LogprobArgs {
+  const void* logits;
+  int32_t dtype, rows;
+  int64_t vocab, row_stride;
+  float scale;
+  int32_t n_top;
+  const int32_t* tokens;
+  float* logprob;
+  int32_t* rank;
+  float* entropy;
+  int32_t* top_ids;
+  float* top_logprobs;
+};
+int64_t logprobs_workspace_bytes(int32_t rows, int64_t vocab, int32_t dtype, int32_t n_top);
+hipError_t launch_token_logprobs(const LogprobArgs& a, void* workspace, hipStream_t stream);
+
+// Norms and rotation of Q and K.  Appends carry the runs of consecutive cells and positions that their tokens go to in the
+// kernel arguments, at most this many of them: run r is tokens tok[r] .. tok[r + 1] - 1, from cell[r] and pos[r] on.
+constexpr int32_t ROTARY_INLINE_MAX_RUNS = 300;
+struct RotaryRuns {
+  int32_t tok[ROTARY_INLINE_MAX_RUNS + 1];
+  int32_t cell[ROTARY_INLINE_MAX_RUNS];
+  int32_t pos[ROTARY_INLINE_MAX_RUNS];
+};
+struct RotaryArgs {
+  int32_t dtype, head_dim, n_q_heads, n_k_heads;
+  int32_t rotary_dim, pairs, norm;
+  float eps, amplitude;
+  const float* inv_freq;
+  const void* q_weight;
+  const void* k_weight;
+  const void* q;
+  const void* k;
+  const void* v;
+  int64_t q_stride, k_stride, v_stride;  // elements from token to token
+  void* q_out;  // token-major
+  void* k_out;  // token-major, or the K arena
+  void* v_out;  // the V arena
+  int64_t arena_cells;
+};
+static_assert(sizeof(RotaryRuns) + sizeof(RotaryArgs) + 64 <= 4096, "kernel arguments are limited to 4 KiB");
+hipError_t launch_rotate_append(const RotaryArgs& a, const RotaryRuns& runs, int32_t n_runs, int32_t n_tok, hipStream_t stream);
+// table_dev: position and cell of each of the n_tok tokens from tok_base on
+hipError_t launch_rotate_append_table(const RotaryArgs& a, const int32_t* table_dev, int32_t tok_base, int32_t n_tok, hipStream_t stream);
+hipError_t launch_rotate_rows(const RotaryArgs& a, const int64_t* positions, int64_t n_tok, hipStream_t stream);
 
 }  // namespace dk

@@ -94,7 +94,9 @@ class DevicePool:
         dk.kv_append(self.handle, slots, cu_delta, k_new, v_new, n_accept)
 
     def ensure_workspace(self, slots, cu_delta, staged) -> torch.Tensor:
-        need = dk.attend_workspace_bytes(self.handle, slots, cu_delta, staged)
+        return self._grow_workspace(dk.attend_workspace_bytes(self.handle, slots, cu_delta, staged))
+
+    def _grow_workspace(self, need: int) -> torch.Tensor:
         if self.workspace is None or self.workspace.numel() < need:
             size = int(need * 1.25) + 4096
             if self.workspace is not None:
@@ -130,6 +132,26 @@ class DevicePool:
                 raise
             ws = self.ensure_workspace(slots, cu_delta, 2)
             dk.append_attend(self.handle, slots, cu_delta, q, k_new, v_new, out, scale, lse, ws, sized=True)
+        return out
+
+    def scored_attend(self, slots, cu_delta, q, scale: float, scores: dk.Scores, k_new=None, v_new=None, out=None, lse=None):
+        """attend() with capped or biased scores and rows that see ranges of their own (dk_scored_attend)."""
+        if out is None:
+            out = torch.empty_like(q)
+        try:
+            dk.scored_attend(self.handle, slots, cu_delta, q, out, scale, scores, k_new, v_new, lse, self.workspace)
+        except dk.DeltaKVError as e:
+            if e.name != "WORKSPACE":
+                raise
+            ws = self._grow_workspace(dk.scored_workspace_bytes(self.handle, slots, cu_delta, k_new is not None, scores))
+            dk.scored_attend(self.handle, slots, cu_delta, q, out, scale, scores, k_new, v_new, lse, ws)
+        return out
+
+    def rotate_append(self, slots, cu_delta, q, k, v, rotary: dk.Rotary, out=None):
+        """Normalises and rotates Q and K by position, K and V into the slots' next cells; returns Q (dk_rotate_append)."""
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        dk.rotate_append(self.handle, slots, cu_delta, q, k, v, rotary, out)
         return out
 
     def gather(self, slot: int):
