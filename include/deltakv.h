@@ -253,7 +253,7 @@ int32_t dk_delta_attend_noalloc(dk_pool* pool, int32_t n_seqs, const int32_t* sl
  * and the row sees the positions max(first, p - window + 1) .. max(p, prefix - 1) that exist (window, prefix and first where
  * given; otherwise 0 .. p, as in dk_delta_attend).  A row that sees nothing gets zeros, and -infinity as its log-sum-exp.
  * K and V at positions a row does not see have no influence on it, whatever they hold.
- *   cap      >= 0, finite; 0: scores are not capped
+ *   cap      0: scores are not capped; else 1/1024 .. 1024 (DK_ERR_UNSUPPORTED for other positive values)
  *   slopes   DEVICE float [n_q_heads] or NULL, finite
  *   window   >= 0; 0: no window
  *   prefix   HOST int64 [n_seqs] or NULL, each >= 0: all rows of entry b see the positions below prefix[b], those after their

@@ -81,6 +81,7 @@ struct dk_pool {
   std::mutex launch_mu;  // serialises GPU-launching calls (shared staging ring, dev_meta and plan)
   dk::AttendPlan plan;   // reused from call to call so that steady-state planning allocates nothing
   int64_t last_plan[DK_PLAN_FIELDS] = {-1};  // see dk_last_plan
+  dk::ScoredConfig scored_cfg;
   dk::ScoredPlan scored_plan;  // likewise, for dk_scored_attend
   std::vector<int64_t> append_cells, append_old_len;  // likewise, for the bookkeeping of appends
 
@@ -259,6 +260,10 @@ int32_t dk_pool_create(const dk_pool_desc* desc, dk_pool** pool_out) {
       }
     }
     p->cfg = dk::default_config(desc->n_q_heads, desc->n_kv_heads, desc->head_dim, desc->dtype == DK_BF16);
+    p->scored_cfg.n_q_heads = desc->n_q_heads;
+    p->scored_cfg.n_kv_heads = desc->n_kv_heads;
+    p->scored_cfg.head_dim = desc->head_dim;
+    p->scored_cfg.bf16 = desc->dtype == DK_BF16;
     p->arrival_slice = take_slice();
     *pool_out = p;
     return DK_OK;
@@ -817,6 +822,8 @@ namespace {
 // Masks of a call, if its description is one.
 int32_t score_masks(const dk_scores* scores, dk::ScoreMasks* out) {
   if (!scores || !(scores->cap >= 0.f) || !(scores->cap <= FLT_MAX) || scores->window < 0) return DK_ERR_INVALID;
+  // Beyond, what is left of a score that is small against its cap has too few digits (2^-22 of the cap).
+  if (scores->cap > 0.f && (scores->cap < 1.f / 1024 || scores->cap > 1024.f)) return DK_ERR_UNSUPPORTED;
   *out = {scores->window, scores->prefix, scores->first};
   return DK_OK;
 }
@@ -834,7 +841,7 @@ int32_t dk_scored_workspace_bytes(dk_pool* pool, int32_t n_seqs, const int32_t* 
     int32_t rc = score_masks(scores, &masks);
     if (rc != DK_OK) return rc;
     std::lock_guard<std::mutex> lk(pool->meta.mutex());
-    rc = dk::build_scored_plan(pool->meta, n_seqs, slots, cu_delta, staged != 0, masks, &pool->scored_plan);
+    rc = dk::build_scored_plan(pool->meta, pool->scored_cfg, n_seqs, slots, cu_delta, staged != 0, masks, &pool->scored_plan);
     if (rc == DK_OK) *bytes_out = (int64_t)pool->scored_plan.total_bytes;
     return rc;
   });
@@ -853,13 +860,15 @@ int32_t dk_scored_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     if (rc != DK_OK) return rc;
     {
       std::lock_guard<std::mutex> lk(pool->meta.mutex());
-      rc = dk::build_scored_plan(pool->meta, n_seqs, slots, cu_delta, k_new != nullptr, masks, &plan);
+      rc = dk::build_scored_plan(pool->meta, pool->scored_cfg, n_seqs, slots, cu_delta, k_new != nullptr, masks, &plan);
       if (rc != DK_OK) return rc;
     }
     if (plan.total_tokens == 0) return DK_OK;
     if (!q || !out) return DK_ERR_INVALID;
     // rows move in pieces of 16 bytes
     if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)k_new | (uintptr_t)v_new) & 15) return DK_ERR_UNSUPPORTED;
+    // and a staged one is found by a 24-bit multiplication
+    if ((int64_t)pool->desc.n_kv_heads * pool->desc.head_dim * 4 >= (1 << 24)) return DK_ERR_UNSUPPORTED;
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < (int64_t)plan.total_bytes) return DK_ERR_WORKSPACE;
     const bool inline_blob = plan.blob_bytes <= (size_t)dk::INLINE_BLOB_BYTES;
     // a captured upload would be replayed from a staging buffer that has other descriptors by then
@@ -875,6 +884,9 @@ int32_t dk_scored_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     const auto put = [&](size_t off, const void* src, size_t bytes) { if (bytes) std::memcpy(h + off, src, bytes); };
     put(plan.off_entries, plan.entries.data(), plan.entries.size() * sizeof(DkEntry));
     put(plan.off_segs, plan.segs.data(), plan.segs.size() * sizeof(DkSeg));
+    put(plan.off_few, plan.few.data(), plan.few.size() * sizeof(DkItem));
+    put(plan.off_rows, plan.rows.data(), plan.rows.size() * sizeof(DkItem));
+    put(plan.off_merges, plan.merges.data(), plan.merges.size() * sizeof(DkMerge));
     put(plan.off_first, plan.first.data(), plan.first.size() * sizeof(int32_t));
     if (!inline_blob) {
       rc = pool->upload(s, workspace, plan.blob_bytes, st);
@@ -894,13 +906,32 @@ int32_t dk_scored_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     a.lse = lse;
     a.scale = scale;
     a.total_tokens = (int32_t)plan.total_tokens;
-    dk::ScoreArgs sc;
-    sc.cap = scores->cap;
-    sc.slopes = scores->slopes;
-    sc.window = scores->window;
-    sc.masked_first = masks.first != nullptr;
-    sc.first = (const int32_t*)(desc + plan.off_first);
-    const hipError_t e = dk::launch_attend_scored(a, sc, st);
+    a.parts = (float*)((char*)workspace + plan.off_parts);
+    a.parts_ml = a.parts + (size_t)plan.part_rows * pool->desc.n_kv_heads * pool->desc.head_dim;
+    const double log2e = 1.4426950408889634;
+    dk::ScoreParams sp;
+    sp.f32 = pool->desc.dtype == DK_F32;
+    sp.capped = scores->cap > 0.f;
+    // (the bf16 kernels take the tangent from an exponential of base 2, the fp32 kernel by its name)
+    const double c = sp.capped ? (double)scale / scores->cap * (sp.f32 ? 1.0 : 2.0 * log2e) : scale * log2e;
+    sp.c = (float)std::min<double>(std::max<double>(c, -FLT_MAX), FLT_MAX);
+    sp.cap = (float)(scores->cap * log2e);
+    sp.slopes = scores->slopes;
+    sp.window = scores->window;
+    sp.has_first = masks.first != nullptr;
+    sp.first = (const int32_t*)(desc + plan.off_first);
+    sp.in_args = inline_blob;
+    dk::ScoredItems items;
+    items.rows = (const DkItem*)(desc + plan.off_rows);
+    items.n_rows = (int32_t)plan.rows.size();
+    items.tile_rows = plan.tile_rows;
+    items.few = (const DkItem*)(desc + plan.off_few);
+    items.n_few = (int32_t)plan.few.size();
+    items.few_rows = plan.few_rows;
+    items.merges = (const DkMerge*)(desc + plan.off_merges);
+    items.n_merges = (int32_t)plan.merges.size();
+    items.merge_rows = plan.merge_rows;
+    const hipError_t e = dk::launch_attend_scored(a, sp, items, st);
     return e == hipSuccess ? DK_OK : pool->hip_fail(e);
   });
 }

@@ -22,8 +22,8 @@
 
 #include <mutex>
 
-#include "attend_common.hpp"
 #include "kernels.hpp"
+#include "scored_common.hpp"
 
 namespace dk {
 namespace mfma {
@@ -104,12 +104,90 @@ __device__ __forceinline__ void redo_quad(const Ctx& c, const DkEntry& e, const 
   else *(f32x4*)((float*)c.out + orow * HD + depth) = x * (1.f / l);
 }
 
+// The changed scores of dk_scored_attend (see attend_scored.hip), in log2 units: an accumulator's key is `ahead` + r after the row.
+// The hyperbolic tangent is the library's, good to a few units of the last place: its 30-odd instructions for each of a block's
+// four scores a lane hide behind the block's 64 products (128-wide heads).
+__device__ __forceinline__ f32x4 changed_scores(const ScoreParams& sp, f32x4 s, float slope, int ahead) {
+  f32x4 t;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) t[r] = sp.capped ? sp.cap * tanhf(s[r] * sp.c) : s[r] * sp.c;
+  if (sp.slopes) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) t[r] -= slope * __builtin_fabsf((float)(ahead + r));
+  }
+  return t;
+}
+
+// redo_quad for rows that see ranges of their own: what the non-finite elements of V make of a row is counted by products.
+template <int HD>
+__device__ __forceinline__ void redo_quad_scored(const Ctx& c, const ScoreParams& sp, const int32_t* first, const DkEntry& e, const DkItem& it,
+                                                 int g, int rl0, uint32_t bad, float m, float l, int lane, int u, int r) {
+  constexpr int ROW = 4 * HD, NI = HD / 16;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // after the ordinary store of the same rows
+  const int col = lane & 15, h = lane >> 4;
+  const int row = min(it.row0 + rl0 + col, it.row0 + it.nrows - 1);
+  const int tok = row_token<true>(c, row);
+  const int head = g * c.group + row_head<true>(c, row, tok);
+  const RowRange rr = row_range(sp, first, e, tok);
+  const float slope = sp.slopes ? sp.slopes[head] * 1.4426950408889634f : 0.f;
+  const int64_t orow = (int64_t)(e.tok0 + tok) * c.n_q_heads + head;
+  const float ms = m == -INFINITY ? 0.f : m;
+  f32x4 qf[NI], o[4], odd[3][4];  // sums; counts of NaN, +infinity, -infinity
+#pragma unroll
+  for (int i = 0; i < NI; ++i) qf[i] = *(const f32x4*)((const float*)c.q + orow * HD + 16 * i + 4 * h);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) o[j] = odd[0][j] = odd[1][j] = odd[2][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  KvCursor<ROW> cur{c.segs, e.seg_begin, e.seg_end, it.kv_lo, it.kv_hi};
+  KvTile t;
+  while (cur.next(c, g, F32_KT, t)) {
+    const char* kp = t.k + (uint32_t)min(col, t.cnt - 1) * t.stride + 16 * h;
+    f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const f32x4 kf = *(const f32x4*)(kp + 64 * i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[j & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j], qf[i][j], s[j & 1], 0, 0, 0);
+    }
+    const f32x4 score = changed_scores(sp, s[0] + s[1], slope, t.pos + 4 * h - rr.pos);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const f32x4 vf = *(const f32x4*)(t.v + (uint32_t)min(4 * h + k, t.cnt - 1) * t.stride + 16 * col + 256 * u);
+      const int key = t.pos + 4 * h + k;
+      const bool seen = 4 * h + k < t.cnt && key >= rr.from && key <= rr.last;
+      const float p = seen ? __builtin_amdgcn_exp2f(score[k] - ms) : 0.f, one = seen ? 1.f : 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t bits = __float_as_uint(vf[j]);
+        const bool fine = (bits & 0x7f800000u) != 0x7f800000u;
+        o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fine ? vf[j] : 0.f, p, o[j], 0, 0, 0);
+        odd[0][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(!fine && (bits & 0x7fffffu) ? 1.f : 0.f, one, odd[0][j], 0, 0, 0);
+        odd[1][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(bits == 0x7f800000u ? 1.f : 0.f, one, odd[1][j], 0, 0, 0);
+        odd[2][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(bits == 0xff800000u ? 1.f : 0.f, one, odd[2][j], 0, 0, 0);
+      }
+    }
+  }
+  const auto of = [&](const f32x4& x) { return r == 0 ? x[0] : r == 1 ? x[1] : r == 2 ? x[2] : x[3]; };
+  f32x4 x;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = with_non_finite(of(o[j]), of(odd[0][j]), of(odd[1][j]), of(odd[2][j]));
+  if ((bad >> col & 1) == 0 || rl0 + col >= it.nrows || l != l) return;
+  const int depth = 64 * u + 4 * (4 * h + r);
+  if (it.part_row0 >= 0) *(f32x4*)(c.parts + ((int64_t)(it.part_row0 + rl0 + col) * c.n_kv_heads + g) * HD + depth) = x;
+  else *(f32x4*)((float*)c.out + orow * HD + depth) = x * (l == 0.f ? 0.f : 1.f / l);
+}
+
+// Parameters of changed scores, for the kernels that have them.
+template <bool SCORED> struct ScoreArg;
+template <> struct ScoreArg<true> { ScoreParams sp; };
+template <> struct ScoreArg<false> {};
+
 }  // namespace
 
 // grid = n_chains * n_kv_heads, as the tile kernel: workgroup w walks chain w / n_kv_heads of the planner's items.
-template <int HD, int RB, bool INLINE>
+// SCORED: attention with changed scores (dk_scored_attend); workgroup w does item w / n_kv_heads, there are no links.
+template <int HD, int RB, bool INLINE, bool SCORED>
 __global__ __launch_bounds__(64 * F32_WAVES, 2) void attend_f32_kernel(BlobArg<INLINE> blob, Ctx c, const int32_t* links,
-                                                                       int n_chains) {
+                                                                       int n_chains, ScoreArg<SCORED> score) {
   typedef F32Geo<HD, RB> G;
   constexpr int NI = G::NI, NU = G::NU;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -119,6 +197,8 @@ __global__ __launch_bounds__(64 * F32_WAVES, 2) void attend_f32_kernel(BlobArg<I
   c.segs = resolve_desc<INLINE>(c.segs);
   c.items = resolve_desc<INLINE>(c.items);
   links = resolve_desc<INLINE>(links);
+  const int32_t* first_seen = nullptr;
+  if constexpr (SCORED) first_seen = resolve_desc<INLINE>(score.sp.first);
   const int g = blockIdx.x % c.n_kv_heads;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -127,8 +207,8 @@ __global__ __launch_bounds__(64 * F32_WAVES, 2) void attend_f32_kernel(BlobArg<I
   float2* xml = (float2*)(smem + G::ML_OFFSET);  // [wave][row]: running maximum, weight sum
 
   bool first = true;
-  for (int item_idx = load_desc(links, blockIdx.x / c.n_kv_heads); item_idx >= 0;
-       item_idx = load_desc(links, n_chains + item_idx)) {
+  for (int item_idx = SCORED ? (int)(blockIdx.x / c.n_kv_heads) : load_desc(links, blockIdx.x / c.n_kv_heads); item_idx >= 0;
+       item_idx = SCORED ? -1 : load_desc(links, n_chains + item_idx)) {
     const DkItem it = load_desc(c.items, item_idx);
     const DkEntry e = load_desc(c.entries, it.entry);
     const int last_row = it.row0 + it.nrows - 1;
@@ -136,11 +216,17 @@ __global__ __launch_bounds__(64 * F32_WAVES, 2) void attend_f32_kernel(BlobArg<I
 
     f32x4 qf[RB][NI];
     int limit[RB];
+    RowRange range[RB];
+    float slope[RB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       const int row = min(it.row0 + rb * 16 + col, last_row);
       const int tok = row_token<true>(c, row);
       limit[rb] = e.n + tok;
+      if constexpr (SCORED) {
+        range[rb] = row_range(score.sp, first_seen, e, tok);
+        slope[rb] = score.sp.slopes ? score.sp.slopes[g * c.group + row_head<true>(c, row, tok)] * 1.4426950408889634f : 0.f;
+      }
       const float* qp = (const float*)c.q + ((int64_t)(e.tok0 + tok) * c.n_q_heads + g * c.group + row_head<true>(c, row, tok)) * HD + 4 * h;
 #pragma unroll
       for (int i = 0; i < NI; ++i) qf[rb][i] = *(const f32x4*)(qp + 16 * i);
@@ -205,13 +291,21 @@ __global__ __launch_bounds__(64 * F32_WAVES, 2) void attend_f32_kernel(BlobArg<I
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         s[rb][0] = s[rb][0] + s[rb][1];
-        if (cnt < F32_KT || pos + F32_KT - 1 > min_limit) {
+        if constexpr (SCORED) {
+          const int at = pos + 4 * h;
+          s[rb][0] = changed_scores(score.sp, s[rb][0], slope[rb], at - range[rb].pos);
+          const int from = range[rb].from - at, last = min(pos + cnt - 1, range[rb].last) - at;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (r < from || r > last) s[rb][0][r] = -INFINITY;
+        } else if (cnt < F32_KT || pos + F32_KT - 1 > min_limit) {
           const int lim = min(cnt - 1, limit[rb] - pos) - 4 * h;
 #pragma unroll
           for (int r = 0; r < 4; ++r)
             if (r > lim) s[rb][0][r] = -INFINITY;
         }
-        mx[rb] = fmaxf(fmaxf(s[rb][0][0], s[rb][0][1]), fmaxf(s[rb][0][2], s[rb][0][3])) * c.c;
+        mx[rb] = fmaxf(fmaxf(s[rb][0][0], s[rb][0][1]), fmaxf(s[rb][0][2], s[rb][0][3]));
+        if constexpr (!SCORED) mx[rb] *= c.c;
         grow |= mx[rb] > m[rb] + F32_RESCALE_SLACK;
       }
       // The reference maximum of a row is only raised when a score outgrows it by more than the slack, so the four
@@ -234,7 +328,7 @@ __global__ __launch_bounds__(64 * F32_WAVES, 2) void attend_f32_kernel(BlobArg<I
       for (int rb = 0; rb < RB; ++rb) {
         const float ms = (m[rb] == -INFINITY) ? 0.f : m[rb];  // no key seen yet: keep the arithmetic finite
 #pragma unroll
-        for (int r = 0; r < 4; ++r) p[rb][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][0][r], c.c, -ms));
+        for (int r = 0; r < 4; ++r) p[rb][r] = __builtin_amdgcn_exp2f(SCORED ? s[rb][0][r] - ms : __builtin_fmaf(s[rb][0][r], c.c, -ms));
         l[rb] += (p[rb][0] + p[rb][1]) + (p[rb][2] + p[rb][3]);
       }
 #pragma unroll
@@ -299,12 +393,14 @@ __global__ __launch_bounds__(64 * F32_WAVES, 2) void attend_f32_kernel(BlobArg<I
         const int row = it.row0 + rl;
         const int tok = row_token<true>(c, row);
         const int64_t orow = (int64_t)(e.tok0 + tok) * c.n_q_heads + g * c.group + row_head<true>(c, row, tok);
-        *(f32x4*)((float*)c.out + orow * HD + depth) = acc * (1.f / lsum);
+        *(f32x4*)((float*)c.out + orow * HD + depth) = acc * (SCORED && lsum == 0.f ? 0.f : 1.f / lsum);
         if (c.lse && u == 0 && r == 0 && eh == 0) c.lse[orow] = (mm + log2f(lsum)) * 0.6931471805599453f;
       }
       if (bad != 0) {
         bad |= bad >> 32;
-        redo_quad<HD>(c, e, it, g, rb * 16, (uint32_t)(bad | bad >> 16) & 0xffffu, mm, lsum, el, u, r);
+        const uint32_t rows = (uint32_t)(bad | bad >> 16) & 0xffffu;
+        if constexpr (SCORED) redo_quad_scored<HD>(c, score.sp, first_seen, e, it, g, rb * 16, rows, mm, lsum, el, u, r);
+        else redo_quad<HD>(c, e, it, g, rb * 16, rows, mm, lsum, el, u, r);
       }
     }
   }
@@ -312,30 +408,30 @@ __global__ __launch_bounds__(64 * F32_WAVES, 2) void attend_f32_kernel(BlobArg<I
 
 namespace {
 
-template <int HD, int RB, bool INLINE>
+template <int HD, int RB, bool INLINE, bool SCORED>
 hipError_t launch_f32(const BlobArg<INLINE>& blob, const Ctx& c, const int32_t* links, int32_t n_chains,
-                      hipStream_t stream) {
+                      const ScoreArg<SCORED>& score, hipStream_t stream) {
   // once per process and instantiation, whatever thread or pool gets here first
   static std::once_flag once;
   static hipError_t status = hipSuccess;
   std::call_once(once, [] {
-    status = hipFuncSetAttribute((const void*)attend_f32_kernel<HD, RB, INLINE>,
+    status = hipFuncSetAttribute((const void*)attend_f32_kernel<HD, RB, INLINE, SCORED>,
                                  hipFuncAttributeMaxDynamicSharedMemorySize, F32Geo<HD, RB>::LDS_BYTES);
   });
   if (status != hipSuccess) return status;
   const dim3 grid((unsigned)n_chains * (unsigned)c.n_kv_heads);
-  attend_f32_kernel<HD, RB, INLINE><<<grid, 64 * F32_WAVES, F32Geo<HD, RB>::LDS_BYTES, stream>>>(blob, c, links, n_chains);
+  attend_f32_kernel<HD, RB, INLINE, SCORED><<<grid, 64 * F32_WAVES, F32Geo<HD, RB>::LDS_BYTES, stream>>>(blob, c, links, n_chains, score);
   return hipGetLastError();
 }
 
-template <bool INLINE>
+template <bool INLINE, bool SCORED>
 hipError_t launch_f32_shape(int head_dim, bool wide, const BlobArg<INLINE>& blob, const Ctx& c, const int32_t* links,
-                            int32_t n_chains, hipStream_t stream) {
+                            int32_t n_chains, const ScoreArg<SCORED>& score, hipStream_t stream) {
   if (head_dim == 64)
-    return wide ? launch_f32<64, 2, INLINE>(blob, c, links, n_chains, stream)
-                : launch_f32<64, 1, INLINE>(blob, c, links, n_chains, stream);
-  return wide ? launch_f32<128, 2, INLINE>(blob, c, links, n_chains, stream)
-              : launch_f32<128, 1, INLINE>(blob, c, links, n_chains, stream);
+    return wide ? launch_f32<64, 2, INLINE, SCORED>(blob, c, links, n_chains, score, stream)
+                : launch_f32<64, 1, INLINE, SCORED>(blob, c, links, n_chains, score, stream);
+  return wide ? launch_f32<128, 2, INLINE, SCORED>(blob, c, links, n_chains, score, stream)
+              : launch_f32<128, 1, INLINE, SCORED>(blob, c, links, n_chains, score, stream);
 }
 
 }  // namespace
@@ -350,8 +446,20 @@ hipError_t launch_attend_f32(const AttendArgs& a, const DkItem* items, const int
   if (tile_rows != 16 && tile_rows != 32) return hipErrorInvalidValue;
   const Ctx c = make_ctx(a, items);
   if (a.inline_blob)
-    return launch_f32_shape<true>(a.arena.head_dim, tile_rows == 32, BlobArg<true>{*a.inline_blob}, c, links, n_chains, stream);
-  return launch_f32_shape<false>(a.arena.head_dim, tile_rows == 32, BlobArg<false>{0}, c, links, n_chains, stream);
+    return launch_f32_shape<true, false>(a.arena.head_dim, tile_rows == 32, BlobArg<true>{*a.inline_blob}, c, links, n_chains, {}, stream);
+  return launch_f32_shape<false, false>(a.arena.head_dim, tile_rows == 32, BlobArg<false>{0}, c, links, n_chains, {}, stream);
+}
+
+hipError_t launch_attend_f32_scored(const AttendArgs& a, const ScoreParams& sp, const DkItem* items, int32_t n_items, int32_t tile_rows,
+                                    hipStream_t stream) {
+  using namespace mfma;
+  if (n_items <= 0) return hipSuccess;
+  if (a.arena.dtype != 0 || (a.arena.head_dim != 64 && a.arena.head_dim != 128)) return hipErrorInvalidValue;
+  if (tile_rows != 16 && tile_rows != 32) return hipErrorInvalidValue;
+  const Ctx c = make_ctx(a, items);
+  if (a.inline_blob)
+    return launch_f32_shape<true, true>(a.arena.head_dim, tile_rows == 32, BlobArg<true>{*a.inline_blob}, c, nullptr, n_items, {sp}, stream);
+  return launch_f32_shape<false, true>(a.arena.head_dim, tile_rows == 32, BlobArg<false>{0}, c, nullptr, n_items, {sp}, stream);
 }
 
 }  // namespace dk

@@ -112,14 +112,28 @@ hipError_t launch_attend_merge(const AttendArgs& a, const DkMerge* merges, int32
                                int32_t max_split, hipStream_t stream);
 
 // Attention with changed scores.
-struct ScoreArgs {
-  float cap = 0.f;                  // > 0: scores are capped
-  const float* slopes = nullptr;    // [n_q_heads]: bias by distance
-  int32_t window = 0;               // > 0: a row sees its own position and window - 1 before it
-  const int32_t* first = nullptr;   // with masked_first (a descriptor): [tokens], first position that the row sees
-  bool masked_first = false;
+struct ScoreParams {
+  float c = 0.f;    // raw product to score in log2 units; capped: to the exponent of u, 2 log2(e) scale / cap
+  float cap = 0.f;  // log2 units
+  bool capped = false, has_first = false, f32 = false;
+  bool in_args = false;           // descriptors travel in the kernel arguments: pointers to them are offsets
+  int32_t window = 0;             // > 0: a row sees its own position and window - 1 before it
+  const float* slopes = nullptr;  // [n_q_heads]: bias by distance
+  const int32_t* first = nullptr;  // with has_first (a descriptor): [tokens], first position that the row sees
 };
-hipError_t launch_attend_scored(const AttendArgs& a, const ScoreArgs& sc, hipStream_t stream);
+// Work items by kernel (descriptors).
+struct ScoredItems {
+  const DkItem* rows = nullptr;  // of at most tile_rows packed rows (bf16: 128)
+  int32_t n_rows = 0, tile_rows = 0;
+  const DkItem* few = nullptr;   // of at most few_rows
+  int32_t n_few = 0, few_rows = 0;
+  const DkMerge* merges = nullptr;
+  int32_t n_merges = 0, merge_rows = 0;  // most rows of a merge
+};
+hipError_t launch_attend_scored(const AttendArgs& a, const ScoreParams& sp, const ScoredItems& items, hipStream_t stream);
+// fp32 pools: items of at most tile_rows (16 or 32) packed rows, without the merge.
+hipError_t launch_attend_f32_scored(const AttendArgs& a, const ScoreParams& sp, const DkItem* items, int32_t n_items, int32_t tile_rows,
+                                    hipStream_t stream);
 
 // Greedy verification (argmax per logits row, accepted-draft count and next token per slot).
 int64_t verify_workspace_bytes(int32_t total_rows, int64_t vocab, int32_t dtype);

@@ -4,14 +4,85 @@
 
 namespace dk {
 
-int32_t build_scored_plan(Pool& pool, int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta, bool staged,
+namespace {
+
+typedef ScoredPlan::Tile Tile;
+
+// The positions that some row of the tile sees.
+void see(const ScoreMasks& masks, const DkEntry& e, int32_t group, const std::vector<int32_t>& first, Tile* t) {
+  const int32_t t0 = t->row0 / group, t1 = (t->row0 + t->nrows - 1) / group;
+  const auto from_of = [&](int32_t tok) { return masks.window > 0 ? std::max(0, e.n + tok - masks.window + 1) : 0; };
+  t->lo = from_of(t0);
+  t->hi = std::max(e.n + t1, e.pad[0] - 1) + 1;
+  if (!masks.first) return;
+  int32_t lo = INT32_MAX, hi = 0;
+  for (int32_t tok = t0; tok <= t1; ++tok) {
+    const int32_t from = std::max(from_of(tok), first[(size_t)(e.tok0 + tok)]), last = std::max(e.n + tok, e.pad[0] - 1);
+    if (from > last) continue;
+    lo = std::min(lo, from);
+    hi = std::max(hi, last + 1);
+  }
+  t->lo = hi > 0 ? lo : 0;  // (rows that see nothing still get their zeros)
+  t->hi = hi;
+}
+
+// Work items of tiles whose workgroups run `at_once` at a time per KV head: key ranges are cut where the longest would outlast an
+// equal share, in pieces of no less than min_chunk; longest first.
+void cut(const std::vector<Tile>& tiles, int32_t at_once, int32_t min_chunk, ScoredPlan* p, std::vector<DkItem>* items) {
+  int64_t total = 0;
+  for (const Tile& t : tiles) total += t.hi - t.lo;
+  int64_t chunk = std::max<int64_t>(min_chunk, (total + at_once - 1) / at_once);
+  chunk = (chunk + 63) / 64 * 64;
+  for (const Tile& t : tiles) {
+    const int64_t keys = t.hi - t.lo;
+    int32_t ns = (int32_t)std::max<int64_t>(1, (keys + chunk - 1) / chunk);
+    if (ns > 1 && keys - (int64_t)(ns - 1) * chunk < chunk / 4) --ns;  // no sliver at the end
+    const int64_t each = ((keys + ns - 1) / ns + 63) / 64 * 64;
+    ns = (int32_t)std::max<int64_t>(1, (keys + each - 1) / std::max<int64_t>(each, 1));
+    int32_t part0 = -1;
+    if (ns > 1) {
+      part0 = (int32_t)p->part_rows;
+      p->part_rows += (int64_t)ns * t.nrows;
+      p->merges.push_back({t.entry, t.row0, t.nrows, part0, ns, p->entries[(size_t)t.entry].tok0, {0, 0}});
+      p->merge_rows = std::max(p->merge_rows, t.nrows);
+    }
+    for (int32_t sp = 0; sp < ns; ++sp) {
+      DkItem it{};
+      it.entry = t.entry;
+      it.row0 = t.row0;
+      it.nrows = t.nrows;
+      it.kv_lo = t.lo + (int32_t)(sp * each);
+      it.kv_hi = sp + 1 == ns ? t.hi : t.lo + (int32_t)((sp + 1) * each);
+      it.part_row0 = ns > 1 ? part0 + sp * t.nrows : -1;
+      items->push_back(it);
+    }
+  }
+  std::stable_sort(items->begin(), items->end(), [](const DkItem& a, const DkItem& b) { return a.kv_hi - a.kv_lo > b.kv_hi - b.kv_lo; });
+}
+
+}  // namespace
+
+int32_t build_scored_plan(Pool& pool, const ScoredConfig& cfg, int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta, bool staged,
                           const ScoreMasks& masks, ScoredPlan* p) {
   int32_t rc = pool.check_batch(n_seqs, slots, cu_delta);
   if (rc != OK) return rc;
   p->entries.clear();
   p->segs.clear();
   p->first.clear();
+  p->few_tiles.clear();
+  p->row_tiles.clear();
+  p->few.clear();
+  p->rows.clear();
+  p->merges.clear();
+  p->part_rows = 0;
+  p->few_rows = p->merge_rows = 0;
   p->total_tokens = n_seqs ? cu_delta[n_seqs] : 0;
+  const int64_t group = cfg.n_q_heads / cfg.n_kv_heads;
+  int64_t most = 0;
+  for (int32_t b = 0; b < n_seqs; ++b) most = std::max<int64_t>(most, (int64_t)cu_delta[b + 1] - cu_delta[b]);
+  // packed row numbers are divided by the group by a multiplication that is exact while row * (group - 1) < 2^32
+  if (most >= (int64_t(1) << 31) / (group * group)) return ERR_UNSUPPORTED;
+  p->tile_rows = cfg.bf16 ? 128 : (p->total_tokens * group + 31) / 32 * cfg.n_kv_heads >= 256 ? 32 : 16;
   for (int32_t b = 0; b < n_seqs; ++b) {
     const int32_t delta = cu_delta[b + 1] - cu_delta[b];
     int64_t len = 0;
@@ -32,13 +103,25 @@ int32_t build_scored_plan(Pool& pool, int32_t n_seqs, const int32_t* slots, cons
     }
     e.seg_end = (int32_t)p->segs.size();
     p->entries.push_back(e);
-    if (!masks.first) continue;
-    for (int32_t t = 0; t < delta; ++t) {
-      const int64_t f = masks.first[cu_delta[b] + t];
-      if (f < 0) return ERR_INVALID;
-      p->first.push_back((int32_t)std::min<int64_t>(f, INT32_MAX / 2));
+    if (masks.first) {
+      for (int32_t t = 0; t < delta; ++t) {
+        const int64_t f = masks.first[cu_delta[b] + t];
+        if (f < 0) return ERR_INVALID;
+        p->first.push_back((int32_t)std::min<int64_t>(f, INT32_MAX / 2));
+      }
+    }
+    const int32_t rows = (int32_t)group * delta;
+    const bool few = cfg.bf16 && rows <= cfg.few_rows;
+    const int32_t step = few ? cfg.few_rows : p->tile_rows;
+    if (few) p->few_rows = std::max(p->few_rows, rows);
+    for (int32_t r0 = 0; r0 < rows; r0 += step) {
+      Tile t{b, r0, std::min(step, rows - r0), 0, 0};
+      see(masks, e, (int32_t)group, p->first, &t);
+      (few ? p->few_tiles : p->row_tiles).push_back(t);
     }
   }
+  cut(p->few_tiles, std::max(1, 256 / cfg.n_kv_heads), cfg.few_chunk, p, &p->few);
+  cut(p->row_tiles, std::max(1, (cfg.bf16 ? 512 : 256) / cfg.n_kv_heads), cfg.rows_chunk, p, &p->rows);
   const auto section = [](size_t& at, size_t bytes) {
     const size_t off = at;
     at = (at + bytes + 15) / 16 * 16;
@@ -47,9 +130,13 @@ int32_t build_scored_plan(Pool& pool, int32_t n_seqs, const int32_t* slots, cons
   size_t at = 0;
   p->off_entries = section(at, p->entries.size() * sizeof(DkEntry));
   p->off_segs = section(at, p->segs.size() * sizeof(DkSeg));
+  p->off_few = section(at, p->few.size() * sizeof(DkItem));
+  p->off_rows = section(at, p->rows.size() * sizeof(DkItem));
+  p->off_merges = section(at, p->merges.size() * sizeof(DkMerge));
   p->off_first = section(at, p->first.size() * sizeof(int32_t));
   p->blob_bytes = at;
-  p->total_bytes = (at + 255) / 256 * 256 + 256;
+  p->off_parts = (at + 255) / 256 * 256;
+  p->total_bytes = p->off_parts + (size_t)p->part_rows * cfg.n_kv_heads * (cfg.head_dim + 2) * sizeof(float) + 256;
   return OK;
 }
 

@@ -16,19 +16,35 @@ struct ScoreMasks {
   const int64_t* first = nullptr;   // [tokens]: the row sees no position below it
 };
 
+// What the cuts go by.
+struct ScoredConfig {
+  int32_t n_q_heads = 0, n_kv_heads = 0, head_dim = 0;
+  bool bf16 = true;
+  int32_t few_rows = 64;     // bf16: entries of at most this many packed rows go to the kernel for few rows
+  int32_t few_chunk = 256;   // smallest key range worth a work item there
+  int32_t rows_chunk = 256;  // and in the rows kernels
+};
+
 // May be reused from call to call: planning a batch like the previous one allocates next to nothing.
 struct ScoredPlan {
+  struct Tile {  // packed rows row0 .. row0 + nrows - 1 of an entry, which see positions of [lo, hi)
+    int32_t entry, row0, nrows, lo, hi;
+  };
   std::vector<Extent> ext;
+  std::vector<Tile> few_tiles, row_tiles;
   std::vector<DkEntry> entries;  // pad[0]: the entry's prefix
   std::vector<DkSeg> segs;
   std::vector<int32_t> first;  // first position that the rows of a token see, where the call says so
-  int64_t total_tokens = 0;
-  size_t off_entries = 0, off_segs = 0, off_first = 0;
-  size_t blob_bytes = 0, total_bytes = 0;
+  std::vector<DkItem> few, rows;
+  std::vector<DkMerge> merges;
+  int64_t total_tokens = 0, part_rows = 0;
+  int32_t few_rows = 0, tile_rows = 0, merge_rows = 0;  // most rows of an item, of a merge
+  size_t off_entries = 0, off_segs = 0, off_first = 0, off_few = 0, off_rows = 0, off_merges = 0;
+  size_t blob_bytes = 0, off_parts = 0, total_bytes = 0;
 };
 
 // Caller holds pool.mutex().
-int32_t build_scored_plan(Pool& pool, int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta, bool staged,
+int32_t build_scored_plan(Pool& pool, const ScoredConfig& cfg, int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta, bool staged,
                           const ScoreMasks& masks, ScoredPlan* plan);
 
 }  // namespace dk

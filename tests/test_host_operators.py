@@ -43,6 +43,11 @@ def test_scored_attend_refuses_bad_scores(pool, scores):
     assert dk.lib().dk_scored_workspace_bytes(pool, 1, _i32(0), _i32(0, 2), 0, s.address, C.byref(out)) == -1
 
 
+@pytest.mark.parametrize("cap", [1e-4, 1025.0, FLT_MAX])
+def test_scored_attend_refuses_caps_it_would_be_inexact_for(pool, cap):
+    assert _attend(pool, dk.Scores(cap=cap)) == -6
+
+
 def test_scored_attend_refuses_bad_calls(pool):
     s = dk.Scores(cap=30.0)
     assert _attend(pool, None) == -1
