@@ -360,8 +360,9 @@ int32_t dk_verify_greedy(int32_t n_seqs, int32_t total_rows, const int32_t* cu_d
 
 /*
  * token_logprobs: what the distribution softmax(scale * logits) of every row says of a given token, and at large (next to
- * dk_verify_greedy: what the emitted tokens were worth; scale is the inverse of the temperature, > 0 and finite).
- *   logits        as for dk_verify_greedy: DEVICE [total_rows, row_stride], 16-byte aligned rows
+ * dk_verify_greedy: what the emitted tokens were worth; scale is the inverse of the temperature, 2^-20 .. 2^20).
+ *   logits        as for dk_verify_greedy: DEVICE [total_rows, row_stride], 16-byte aligned rows (what lies between vocab and
+ *                 row_stride may be read, up to the end of the 16 bytes that hold the last logit, and counts for nothing)
  *   tokens        DEVICE int32 [total_rows], or NULL (then logprob_out and rank_out are NULL)
  *   logprob_out   DEVICE float [total_rows] or NULL: natural log of the token's probability
  *   rank_out      DEVICE int32 [total_rows] or NULL: how many logits of the row are larger than the token's
@@ -372,7 +373,8 @@ int32_t dk_verify_greedy(int32_t n_seqs, int32_t total_rows, const int32_t* cu_d
  * A token outside [0, vocab) has log probability -infinity and rank vocab.  In a row that holds a NaN or +infinity, or nothing
  * but -infinity, log probabilities and entropy are NaN; rank and ids count a NaN as +infinity, as dk_verify_greedy does.
  *   workspace     DEVICE, 256-byte aligned, >= dk_logprobs_workspace_bytes() for the same arguments
- * total_rows and vocab < 2^31.  Asynchronous on `stream`; stateless, needs no pool; allocates nothing.
+ * total_rows < 2^24, vocab <= 2^24, less than 2^35 logits in all (DK_ERR_UNSUPPORTED).  Asynchronous on `stream`;
+ * stateless, needs no pool; allocates nothing.
  */
 int32_t dk_logprobs_workspace_bytes(int32_t total_rows, int64_t vocab, int32_t dtype, int32_t n_top, int64_t* bytes_out);
 int32_t dk_token_logprobs(int32_t total_rows, const void* logits, int32_t dtype, int64_t vocab, int64_t row_stride, float scale,

@@ -1191,6 +1191,8 @@ int32_t dk_verify_greedy(int32_t n_seqs, int32_t total_rows, const int32_t* cu_d
 int32_t dk_logprobs_workspace_bytes(int32_t total_rows, int64_t vocab, int32_t dtype, int32_t n_top, int64_t* bytes_out) {
   if (!bytes_out || total_rows < 0 || vocab <= 0 || vocab > INT32_MAX || n_top < 0 || n_top > vocab) return DK_ERR_INVALID;
   if ((dtype != DK_F32 && dtype != DK_BF16) || n_top > dk::LOGPROBS_MAX_TOP) return DK_ERR_UNSUPPORTED;
+  // (what one launch can hold)
+  if (vocab > dk::LOGPROBS_MAX_VOCAB || total_rows >= (1 << 24) || (int64_t)total_rows * vocab >= (int64_t(1) << 35)) return DK_ERR_UNSUPPORTED;
   *bytes_out = dk::logprobs_workspace_bytes(total_rows, vocab, dtype, n_top);
   return DK_OK;
 }
@@ -1202,6 +1204,7 @@ int32_t dk_token_logprobs(int32_t total_rows, const void* logits, int32_t dtype,
   const int32_t rc = dk_logprobs_workspace_bytes(total_rows, vocab, dtype, n_top, &need);
   if (rc != DK_OK) return rc;
   if (row_stride < vocab || !(scale > 0.f) || !(scale <= FLT_MAX)) return DK_ERR_INVALID;
+  if (scale < 0x1p-20f || scale > 0x1p20f) return DK_ERR_UNSUPPORTED;  // products with a logit stay within the type
   if (total_rows == 0) return DK_OK;
   if (!logits || (!tokens && (logprob_out || rank_out)) || (n_top > 0 && !top_ids_out) || (n_top == 0 && (top_ids_out || top_logprobs_out)))
     return DK_ERR_INVALID;

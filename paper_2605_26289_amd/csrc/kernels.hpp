@@ -144,6 +144,7 @@ hipError_t launch_verify_greedy(int32_t n_seqs, int32_t total_rows, const int32_
 
 // Log probabilities of given tokens, their rank, entropy and the best alternatives, a logits row each.
 constexpr int32_t LOGPROBS_MAX_TOP = 32;
+constexpr int64_t LOGPROBS_MAX_VOCAB = 1 << 24;
 struct LogprobArgs {
   const void* logits;
   int32_t dtype, rows;

@@ -65,7 +65,8 @@ def _tokens(rng, x):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,vocab,n_top", [(1, 1, 1), (3, 2, 2), (2, 7, 3), (5, 64, 32), (4, 255, 1), (3, 256, 5), (2, 1000, 20), (7, 4099, 32),
-                                             (3, 16384, 5), (2, 16385, 20), (2, 32003, 8), (1, 128256, 20), (2, 128256, 0), (300, 50, 4)])
+                                             (3, 16384, 5), (2, 16385, 20), (2, 32003, 8), (1, 128256, 20), (2, 128256, 0), (300, 50, 4), (1, 1 << 24, 32),
+                                             (1, 3 << 20, 7)])
 def test_rows_of_all_widths(rows, vocab, n_top, dtype):
     rng = np.random.default_rng(rows * vocab)
     x = wl.normal(rng, (rows, vocab), dtype) * np.float32(2)

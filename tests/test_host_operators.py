@@ -213,6 +213,9 @@ def test_token_logprobs_refuses_bad_calls():
     assert call(dtype=5) == -6 and call(logits=4104) == -6 and call(stride=1004) == -6 and call(logits=None) == -1
     for scale in (0.0, -1.0, float("nan"), float("inf")):
         assert call(scale=scale) == -1
+    assert call(scale=1e-7) == -6 and call(scale=2e6) == -6
+    assert call(rows=1 << 24, vocab=8, stride=8) == -6 and call(vocab=2 ** 24 + 1, stride=2 ** 31) == -6
+    assert call(rows=1 << 23, vocab=4096, stride=4096) == -6
     assert call(tokens=None) == -1 and call(tokens=None, lp=None, rank=2048) == -1
     assert call(n_top=-1) == -1 and call(n_top=33, ids=2048) == -6 and call(n_top=5) == -1 and call(ids=2048) == -1 and call(tlp=2048) == -1
     assert call(vocab=4, stride=8, n_top=5, ids=2048) == -1  # more alternatives than tokens
