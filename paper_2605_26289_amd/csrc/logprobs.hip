@@ -9,11 +9,16 @@
 //
 // The n largest of a chunk.  Of the 64 lanes of a wavefront each has its largest logit; T, the n-th largest of those, is found bit
 // by bit with ballots.  At least n of the wavefront's logits are T or more, and those above T are in less than n lanes: some n and a
-// few candidates, at most 64 n.  The largest T of the four wavefronts does for all.  Candidates go to LDS -- all above T, and of
-// those equal to T the first n in the order of their ids -- and are put in order by counting, for each, those before it.
+// few candidates, at most 64 n.  The largest T of the four wavefronts does for all; so does the least of their (n / 4)-th largest
+// lanes, since every wavefront has n / 4 logits from there on, and it lies higher where the large logits are spread: with n = 20 over
+// chunks of 8192 some 30 candidates instead of 110.  The candidates --
+// all from T on; where those are many, all above T and of those equal to T the first n in the order of their ids -- go to LDS and are
+// put in order by counting, for each, those before it.
 //
 // Ties go to the lowest id; a NaN counts as +infinity there and makes the sums NaN.
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "kernels.hpp"
 
@@ -28,13 +33,6 @@ constexpr int LP_CAP = 256;                      // candidates of a wavefront
 constexpr int LP_MAX_CHUNKS = 2048;              // of a row: 2^24 logits of 4 bytes, LP_UNROLL loads a lane
 static_assert(LP_MAX_CHUNKS * (LP_THREADS * LP_UNROLL * 4) >= LOGPROBS_MAX_VOCAB, "and so are 2^24 / 4 in shorter chunks, see cut_rows");
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-
-struct Pick {
-  float v;
-  int32_t i;
-};
-// `a` comes before `b`: larger, or equal with the lower id
-__device__ __forceinline__ bool before(Pick a, Pick b) { return a.v > b.v || (a.v == b.v && a.i < b.i); }
 
 // What a chunk says of its row.
 struct Part {
@@ -62,16 +60,25 @@ __device__ __forceinline__ uint32_t ordered(float x) {
   return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float from_ordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
-// The n-th largest of the lanes' values.
-__device__ __forceinline__ float nth_largest(float x, int n) {
+// A logit and its id as one whole number: the larger comes first, of equals the one with the lower id.  0: none.
+typedef uint64_t Pick;
+__device__ __forceinline__ Pick pick_of(float x, int32_t id) { return (uint64_t)ordered(x) << 32 | (uint32_t)~id; }
+__device__ __forceinline__ float pick_value(Pick p) { return from_ordered((uint32_t)(p >> 32)); }
+__device__ __forceinline__ int32_t pick_id(Pick p) { return (int32_t)~(uint32_t)p; }
+// The n-th and the k-th largest of the lanes' values, or a little less: the first BITS bits of each, and the smallest value that
+// begins with them.
+template <int BITS>
+__device__ __forceinline__ float2 nth_and_kth_largest(float x, int n, int k) {
   const uint32_t key = ordered(x);
-  uint32_t t = 0;
+  uint32_t tn = 0, tk = 0;
 #pragma unroll
-  for (int bit = 31; bit >= 0; --bit) {
-    const uint32_t trial = t | (1u << bit);
-    if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(key >= trial)) >= n) t = trial;
+  for (int bit = 31; bit >= 32 - BITS; --bit) {
+    const uint32_t un = tn | (1u << bit), uk = tk | (1u << bit);
+    if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(key >= un)) >= n) tn = un;
+    if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(key >= uk)) >= k) tk = uk;
   }
-  return from_ordered(t);
+  // (below are no values, -infinity is the first)
+  return make_float2(from_ordered(max(tn, 0x007fffffu)), from_ordered(max(tk, 0x007fffffu)));
 }
 
 // The wavefront's n first logits in order, one after the other and from memory: where more logits lie above T than there is room for.
@@ -79,31 +86,57 @@ template <typename T, int UNROLL>
 __device__ __forceinline__ int pick_rounds(const T* p, int32_t base, int32_t vocab, int n, Pick* out) {
   constexpr int VEC = 16 / (int)sizeof(T);
   const int lane = threadIdx.x & 63;
-  Pick last{INFINITY, -1};
+  Pick last = ~uint64_t(0);
   int count = 0;
   for (int k = 0; k < n; ++k) {
-    Pick best{-INFINITY, INT32_MAX};
+    Pick best = 0;
 #pragma unroll 1
     for (int u = 0; u < UNROLL; ++u) {
 #pragma unroll 1
       for (int j = 0; j < VEC; ++j) {
         const int32_t id = base + u * (LP_THREADS * VEC) + j;
         if (id >= vocab) continue;
-        const Pick x{logit_key(logit_at(p, id)), id};
-        if (before(last, x) && before(x, best)) best = x;
+        const Pick x = pick_of(logit_key(logit_at(p, id)), id);
+        if (x < last && x > best) best = x;
       }
     }
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) {
-      const Pick o{__shfl_xor(best.v, off), __shfl_xor(best.i, off)};
-      if (before(o, best)) best = o;
-    }
-    if (best.i == INT32_MAX) break;
+    for (int off = 32; off >= 1; off >>= 1) best = max(best, (Pick)__shfl_xor((unsigned long long)best, off));
+    if (best == 0) break;
     if (lane == 0) out[count] = best;
     ++count;
     last = best;
   }
   return count;
+}
+
+// How many of list[0 .. n) come before q; the list is padded with none to whole eights, so that eight are on their way at a time.
+__device__ __forceinline__ int count_before(const Pick* list, int n, Pick q) {
+  int rank = 0;
+  for (int k = 0; k < n; k += 8) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) rank += list[k + j] > q ? 1 : 0;
+  }
+  return rank;
+}
+__device__ __forceinline__ void pad_list(Pick* list, int n, int thread) {
+  if (thread < 8) list[n + thread] = 0;
+}
+
+// x[AT + e], e below 32 and a lane's own: a tree of selections, by masks (the compiler would turn a tree of conditions into one
+// that goes through the elements one by one, fifty times as long).
+template <int AT, int N>
+__device__ __forceinline__ float element(const float (&x)[N], int e) {
+  uint32_t v[32];
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = AT + i < N ? __float_as_uint(x[AT + i < N ? AT + i : 0]) : 0u;
+#pragma unroll
+  for (int half = 16, bit = 0; half >= 1; half >>= 1, ++bit) {
+    const uint32_t odd = 0u - ((uint32_t)e >> bit & 1u);
+#pragma unroll
+    for (int i = 0; i < half; ++i) v[i] = (v[2 * i + 1] & odd) | (v[2 * i] & ~odd);
+  }
+  return __uint_as_float(v[0]);
 }
 
 // A chunk is LP_THREADS * UNROLL * VEC logits; element VEC u + j of a thread is id base + (u LP_THREADS + thread) VEC + j.
@@ -112,7 +145,7 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_chunk_kernel(Logpro
                                                                           Pick* __restrict__ tops) {
   constexpr int VEC = 16 / (int)sizeof(T), N = UNROLL * VEC;
   __shared__ Part wave_parts[LP_WAVES];
-  __shared__ float wave_t[LP_WAVES];
+  __shared__ float2 wave_t[LP_WAVES];
   __shared__ int32_t counts[LP_WAVES];
   __shared__ Pick cands[TOP ? LP_WAVES * LP_CAP : 1];
   const int32_t row = blockIdx.x / n_chunks, chunk = blockIdx.x - row * n_chunks;
@@ -181,7 +214,9 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_chunk_kernel(Logpro
   int32_t above = 0;
   if constexpr (STATS) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(x[e] > given));
+    for (int e = 0; e < N; ++e) above += x[e] > given ? 1 : 0;
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) above += __shfl_xor(above, off);
   }
   s0 = wave_sum(s0);
   if constexpr (STATS) s1 = wave_sum(s1);
@@ -189,7 +224,7 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_chunk_kernel(Logpro
   const float r = __builtin_fabsf(mc) <= 1048576.f ? __builtin_fmaf(mr, c, -mc) : 0.f;
   if (lane == 0) wave_parts[wave] = Part{m, s0 * __builtin_amdgcn_exp2f(-r), (s1 - r * s0) * __builtin_amdgcn_exp2f(-r), above};
   if constexpr (TOP) {
-    const float t = nth_largest(mine, a.n_top);
+    const float2 t = nth_and_kth_largest<sizeof(T) == 2 ? 16 : 20>(mine, a.n_top, (a.n_top + LP_WAVES - 1) / LP_WAVES);
     if (lane == 0) wave_t[wave] = t;
   }
   __syncthreads();
@@ -210,68 +245,95 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_chunk_kernel(Logpro
     parts[(int64_t)row * n_chunks + chunk] = q;
   }
   if constexpr (TOP) {
-    float t = wave_t[0];
+    float t = wave_t[0].x, every = wave_t[0].y;
 #pragma unroll
-    for (int w = 1; w < LP_WAVES; ++w) t = fmaxf(t, wave_t[w]);
+    for (int w = 1; w < LP_WAVES; ++w) {
+      t = fmaxf(t, wave_t[w].x);
+      every = fminf(every, wave_t[w].y);
+    }
+    t = fmaxf(t, every);
     t = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(t)));
     Pick* out = cands + wave * LP_CAP;
-    int count = 0, ties = 0;
+    int count = 0;
     if (__builtin_amdgcn_ballot_w64(mine >= t) != 0) {
+      uint32_t which[(N + 31) / 32];  // of the lane's logits; the last one in the lowest bit
+      const auto mark = [&](auto take) {
 #pragma unroll
-      for (int u = 0; u < UNROLL; ++u) {
-        uint64_t equal[VEC], any = 0;
+        for (int k = 0; k < (N + 31) / 32; ++k) {
+          which[k] = 0;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          const float v = x[u * VEC + j];
-          const uint64_t b = __builtin_amdgcn_ballot_w64(v > t);
-          if (b != 0) {
-            const int n = __builtin_popcountll(b);
-            if (v > t && count + n <= LP_CAP - LOGPROBS_MAX_TOP)
-              out[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)b, 0))] = Pick{v, id_of(u * VEC + j)};
-            count += n;
-          }
-          equal[j] = __builtin_amdgcn_ballot_w64(v == t && id_of(u * VEC + j) < vocab);
-          any |= equal[j];
+          for (int e = 32 * k; e < min(N, 32 * k + 32); ++e) which[k] = which[k] + which[k] + (take(x[e]) ? 1u : 0u);
         }
-        if (any != 0 && ties < a.n_top && count <= LP_CAP - LOGPROBS_MAX_TOP) {  // in the order of the ids: lane by lane
-          int at = ties;
+      };
+      const auto collect_32 = [&](auto part) {  // false: more than there is room for
+        constexpr int AT = 32 * decltype(part)::value;
+        uint32_t w = which[AT / 32];
+        for (uint64_t b; (b = __builtin_amdgcn_ballot_w64(w != 0)) != 0;) {
+          const int n = __builtin_popcountll(b);
+          if (count + n > LP_CAP - 8) return false;
+          const int e = min(N - AT, 32) - 1 - __builtin_ctz(w | 0x80000000u);
+          const Pick q = pick_of(element<AT>(x, e), id_of(AT + e));
+          if (w != 0) out[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)b, 0))] = q;
+          w &= w - 1;
+          count += n;
+        }
+        return true;
+      };
+      const auto collect = [&]() {
+        if constexpr (N > 32) return collect_32(std::integral_constant<int, 0>()) && collect_32(std::integral_constant<int, 1>());
+        else return collect_32(std::integral_constant<int, 0>());
+      };
+      mark([&](float v) { return v >= t; });
+      if (t == -INFINITY || !collect()) {
+        // Many logits are equal to T (a row held to a few tokens has -infinity everywhere else): all above it, and of those
+        // equal the first n, in the order of the ids: lane by lane, 16 bytes by 16 bytes.
+        count = 0;
+        mark([&](float v) { return v > t; });
+        if (collect() && count <= LP_CAP - 8 - LOGPROBS_MAX_TOP) {
+          int ties = 0;
 #pragma unroll
-          for (int j = 0; j < VEC; ++j)
-            at += __builtin_amdgcn_mbcnt_hi((uint32_t)(equal[j] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)equal[j], 0));
+          for (int u = 0; u < UNROLL; ++u) {
+            if (ties >= a.n_top) continue;
+            uint64_t equal[VEC];
+            int at = ties;
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) {
-            if (equal[j] >> lane & 1) {
-              // (from the end of the wavefront's room, where those above T do not get to)
-              if (at < a.n_top) out[LP_CAP - 1 - at] = Pick{t, id_of(u * VEC + j)};
-              ++at;
+            for (int j = 0; j < VEC; ++j) {
+              equal[j] = __builtin_amdgcn_ballot_w64(x[u * VEC + j] == t && id_of(u * VEC + j) < vocab);
+              at += __builtin_amdgcn_mbcnt_hi((uint32_t)(equal[j] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)equal[j], 0));
             }
-            ties += __builtin_popcountll(equal[j]);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+              if (equal[j] >> lane & 1) {
+                if (at < a.n_top) out[count + at] = pick_of(t, id_of(u * VEC + j));
+                ++at;
+              }
+              ties += __builtin_popcountll(equal[j]);
+            }
           }
+          count += min(ties, a.n_top);
+        } else {
+          count = pick_rounds<T, UNROLL>(p, base, vocab, a.n_top, out);
         }
       }
-      if (count > LP_CAP - LOGPROBS_MAX_TOP) {
-        count = pick_rounds<T, UNROLL>(p, base, vocab, a.n_top, out);
-        ties = 0;
-      }
-      ties = min(ties, a.n_top);
-      if (lane < ties) out[count + lane] = out[LP_CAP - 1 - lane];
     }
-    if (lane == 0) counts[wave] = count + ties;
+    pad_list(out, count, lane);
+    if (lane == 0) counts[wave] = count;
     __syncthreads();
     Pick* list = tops + ((int64_t)row * n_chunks + chunk) * a.n_top;
     int total = 0;
 #pragma unroll
     for (int w = 0; w < LP_WAVES; ++w) total += counts[w];
+    // a candidate's place is the number of those before it
     for (int k = threadIdx.x; k < total; k += LP_THREADS) {
       int w = 0, at = k;
       while (at >= counts[w]) at -= counts[w++];
       const Pick mypick = cands[w * LP_CAP + at];
       int rank = 0;
-      for (int o = 0; o < LP_WAVES; ++o)
-        for (int q = 0; q < counts[o]; ++q) rank += before(cands[o * LP_CAP + q], mypick);
+#pragma unroll
+      for (int o = 0; o < LP_WAVES; ++o) rank += count_before(cands + o * LP_CAP, counts[o], mypick);
       if (rank < a.n_top) list[rank] = mypick;
     }
-    if ((int)threadIdx.x >= total && (int)threadIdx.x < a.n_top) list[threadIdx.x] = Pick{-INFINITY, INT32_MAX};  // a short last chunk
+    if ((int)threadIdx.x >= total && (int)threadIdx.x < a.n_top) list[threadIdx.x] = 0;  // a short last chunk
   }
 }
 
@@ -294,16 +356,16 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_finish_kernel(Logpr
                                                                            const Pick* __restrict__ tops) {
   __shared__ float fbuf[LP_WAVES];
   __shared__ int32_t ibuf[LP_WAVES];
-  __shared__ Pick heads[TOP ? LP_MAX_CHUNKS : 1];
+  __shared__ Pick heads[TOP ? LP_MAX_CHUNKS + 8 : 1];
   __shared__ int32_t lists[TOP ? LOGPROBS_MAX_TOP : 1];
-  __shared__ Pick cands[TOP ? LOGPROBS_MAX_TOP * (LOGPROBS_MAX_TOP + 1) / 2 : 1];
+  __shared__ Pick cands[TOP ? LOGPROBS_MAX_TOP * (LOGPROBS_MAX_TOP + 1) / 2 + 8 : 1];
   const int32_t row = blockIdx.x;
   const int tid = threadIdx.x, threads = blockDim.x;
   const float c = a.scale * LOG2E;
   const Part* mine = parts + (int64_t)row * n_chunks;
   const Pick* top = tops + (int64_t)row * n_chunks * a.n_top;
   if constexpr (TOP)
-    for (int k = tid; k < n_chunks; k += threads) heads[k] = top[(int64_t)k * a.n_top];
+    for (int k = tid; k < n_chunks + 8; k += threads) heads[k] = k < n_chunks ? top[(int64_t)k * a.n_top] : 0;
   const int32_t token = a.tokens ? a.tokens[row] : -1;
   const bool given = token >= 0 && token < a.vocab;
   const int64_t at = (int64_t)row * a.row_stride + (given ? token : 0);
@@ -334,9 +396,7 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_finish_kernel(Logpr
   if constexpr (TOP) {
     const int n = a.n_top, best = min(n, n_chunks);
     for (int k = tid; k < n_chunks; k += threads) {
-      const Pick h = heads[k];
-      int rank = 0;
-      for (int l = 0; l < n_chunks && rank < n; ++l) rank += before(heads[l], h);
+      const int rank = count_before(heads, n_chunks, heads[k]);
       if (rank < best) lists[rank] = k;
     }
     __syncthreads();
@@ -346,14 +406,14 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_finish_kernel(Logpr
       while (e >= n - r) e -= n - r++;
       cands[k] = top[(int64_t)lists[r] * n + e];
     }
+    pad_list(cands, total, tid);
     __syncthreads();
     for (int k = tid; k < total; k += threads) {
       const Pick q = cands[k];
-      int rank = 0;
-      for (int l = 0; l < total; ++l) rank += before(cands[l], q);
-      if (rank >= n || q.i == INT32_MAX) continue;
-      a.top_ids[(int64_t)row * n + rank] = q.i;
-      if (a.top_logprobs) a.top_logprobs[(int64_t)row * n + rank] = (q.v - m) * a.scale - ln_z;
+      const int rank = count_before(cands, total, q);
+      if (rank >= n || q == 0) continue;
+      a.top_ids[(int64_t)row * n + rank] = pick_id(q);
+      if (a.top_logprobs) a.top_logprobs[(int64_t)row * n + rank] = (pick_value(q) - m) * a.scale - ln_z;
     }
   }
 }
@@ -404,7 +464,7 @@ hipError_t launch_token_logprobs(const LogprobArgs& a, void* workspace, hipStrea
   else wide ? launch_chunks<float, LP_UNROLL>(a, cut, parts, tops, stream) : launch_chunks<float, LP_UNROLL_FEW>(a, cut, parts, tops, stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (a.n_top > 0) token_logprobs_finish_kernel<true><<<dim3((unsigned)a.rows), LP_THREADS, 0, stream>>>(a, cut.n_chunks, parts, tops);
+  if (a.n_top > 0) token_logprobs_finish_kernel<true><<<dim3((unsigned)a.rows), a.n_top > 22 ? LP_THREADS : 64, 0, stream>>>(a, cut.n_chunks, parts, tops);
   else token_logprobs_finish_kernel<false><<<dim3((unsigned)a.rows), 64, 0, stream>>>(a, cut.n_chunks, parts, tops);
   return hipGetLastError();
 }
