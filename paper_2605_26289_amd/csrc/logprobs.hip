@@ -182,30 +182,39 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_chunk_kernel(Logpro
   const auto lane_max = [&]() {
     float m = x[0];
 #pragma unroll
-    for (int e = 1; e < N; ++e) m = fmaxf(m, x[e]);
+    for (int e = 0; e < N; e += 2) asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(m), "v"(x[e]), "v"(x[e + 1]));
     return m;
   };
   float mine = lane_max();
   const float m = wave_max(mine);
   const float c = a.scale * LOG2E, mr = m == -INFINITY ? 0.f : m, mc = mr * c;
   float s0 = 0.f, s1 = 0.f;
-  if (__builtin_fabsf(mc) <= 1048576.f) {
+  // (eight at a time: an exponential's result may not be used by the very next instruction)
+  const auto sums = [&](auto y) {
+    float q0 = 0.f, q1 = 0.f;
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const float t = __builtin_fmaf(x[e], c, -mc);
-      const float w = __builtin_amdgcn_exp2f(t);
-      s0 += w;
-      if constexpr (STATS) s1 = __builtin_fmaf(w, fmaxf(t, -200.f), s1);  // (2^-200 is no float: the weight is zero there)
-    }
-  } else {  // the difference first: it may be small against what is multiplied
+    for (int e = 0; e < N; e += 8) {
+      float t[8], w[8];
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const float t = (x[e] - mr) * c;
-      const float w = __builtin_amdgcn_exp2f(t);
-      s0 += w;
-      if constexpr (STATS) s1 = __builtin_fmaf(w, fmaxf(t, -200.f), s1);
+      for (int i = 0; i < 8; ++i) t[i] = y(x[e + i]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = __builtin_amdgcn_exp2f(t[i]);
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        s0 += w[i];
+        q0 += w[i + 1];
+        if constexpr (STATS) {
+          s1 = __builtin_fmaf(w[i], fmaxf(t[i], -200.f), s1);  // (2^-200 is no float: the weight is zero there)
+          q1 = __builtin_fmaf(w[i + 1], fmaxf(t[i + 1], -200.f), q1);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
-  }
+    s0 += q0;
+    s1 += q1;
+  };
+  if (__builtin_fabsf(mc) <= 1048576.f) sums([&](float v) { return __builtin_fmaf(v, c, -mc); });
+  else sums([&](float v) { return (v - mr) * c; });  // the difference first: it may be small against what is multiplied
   if (__builtin_amdgcn_ballot_w64(s0 != s0) != 0) {  // a NaN or an infinity: from here on they count by their place
 #pragma unroll
     for (int e = 0; e < N; ++e) x[e] = logit_key(x[e]);
