@@ -84,6 +84,7 @@ struct dk_pool {
   dk::ScoredConfig scored_cfg;
   dk::ScoredPlan scored_plan;  // likewise, for dk_scored_attend
   std::vector<int64_t> append_cells, append_old_len;  // likewise, for the bookkeeping of appends
+  std::vector<dk::Extent> append_runs;
 
   dk_pool(const dk_pool_desc& d, int32_t granule)
       : desc(d), meta(d.n_slots, d.n_session_slots, d.arena_cells, granule), granule_cells(granule) {}
@@ -1012,16 +1013,16 @@ int32_t dk_rotate_append(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     if (overlap(qo, span_of(k, total, k_stride, k_row, elem)) || overlap(qo, span_of(v, total, v_stride, k_row, elem)))
       return DK_ERR_INVALID;
     const int64_t per_launch = std::min<int64_t>(d.dev_meta_bytes, (int64_t)pool->stage_cap) / (2 * (int64_t)sizeof(int32_t));
-    std::vector<int64_t>& dst = pool->append_cells;
+    std::vector<dk::Extent>& runs_of = pool->append_runs;
     std::vector<int64_t>& old_len = pool->append_old_len;
-    rc = pool->meta.append(n_seqs, slots, cu_delta, nullptr, &dst, &old_len);
+    rc = pool->meta.append(n_seqs, slots, cu_delta, nullptr, nullptr, &old_len, &runs_of);
     if (rc != DK_OK) return rc;
     const auto undo = [&](int32_t status) {
       undo_append(pool, n_seqs, slots, old_len);
       return status;
     };
-    for (int32_t b = 0; b < n_seqs; ++b)
-      if (old_len[b] + cu_delta[b + 1] - cu_delta[b] > INT32_MAX / 2) return undo(DK_ERR_UNSUPPORTED);
+    for (int32_t i = 0; i < n_seqs; ++i)
+      if (old_len[i] + cu_delta[i + 1] - cu_delta[i] > INT32_MAX / 2) return undo(DK_ERR_UNSUPPORTED);
     dk::RotaryArgs a = rotary_args(rotary, d.dtype, d.head_dim, d.n_q_heads, d.n_kv_heads);
     a.q = q;
     a.k = k;
@@ -1035,18 +1036,15 @@ int32_t dk_rotate_append(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     a.arena_cells = pool->meta_arena_cells;
     hipStream_t st = (hipStream_t)stream;
     // The runs of cells and positions travel in the kernel arguments where they fit; else a table of every token's is uploaded.
-    dk::RotaryRuns runs;
-    int32_t n_runs = 0, b = 0;
-    int64_t t = 0;
-    while (t < total && n_runs < dk::ROTARY_INLINE_MAX_RUNS) {
-      while (cu_delta[b + 1] <= t) ++b;
-      runs.tok[n_runs] = (int32_t)t;
-      runs.cell[n_runs] = (int32_t)dst[t];
-      runs.pos[n_runs++] = (int32_t)(old_len[b] + t - cu_delta[b]);
-      for (++t; t < cu_delta[b + 1] && dst[t] == dst[t - 1] + 1; ++t) {
+    if (runs_of.size() <= (size_t)dk::ROTARY_INLINE_MAX_RUNS) {
+      dk::RotaryRuns runs;
+      int32_t n_runs = 0, b = 0;
+      for (const dk::Extent& r : runs_of) {
+        while (cu_delta[b + 1] <= r.pos) ++b;
+        runs.tok[n_runs] = (int32_t)r.pos;
+        runs.cell[n_runs] = (int32_t)r.cell;
+        runs.pos[n_runs++] = (int32_t)(old_len[b] + r.pos - cu_delta[b]);
       }
-    }
-    if (t == total) {
       runs.tok[n_runs] = (int32_t)total;
       const hipError_t e = dk::launch_rotate_append(a, runs, n_runs, (int32_t)total, st);
       return e == hipSuccess ? DK_OK : undo(pool->hip_fail(e));
@@ -1054,7 +1052,8 @@ int32_t dk_rotate_append(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     if (per_launch <= 0) return undo(DK_ERR_WORKSPACE);
     // a captured upload would be replayed from a staging buffer that has other descriptors by then
     if (capturing(st)) return undo(DK_ERR_UNSUPPORTED);
-    b = 0;
+    size_t r = 0;
+    int32_t b = 0;
     for (int64_t base = 0; base < total; base += per_launch) {
       const int32_t n = (int32_t)std::min<int64_t>(per_launch, total - base);
       Staging* s;
@@ -1062,9 +1061,11 @@ int32_t dk_rotate_append(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
       if (rc != DK_OK) return undo(rc);
       int32_t* h = (int32_t*)s->host;
       for (int32_t i = 0; i < n; ++i) {
-        while (cu_delta[b + 1] <= base + i) ++b;
-        h[2 * i] = (int32_t)(old_len[b] + base + i - cu_delta[b]);
-        h[2 * i + 1] = (int32_t)dst[base + i];
+        const int64_t t = base + i;
+        while (cu_delta[b + 1] <= t) ++b;
+        while (t >= runs_of[r].pos + runs_of[r].len) ++r;
+        h[2 * i] = (int32_t)(old_len[b] + t - cu_delta[b]);
+        h[2 * i + 1] = (int32_t)(runs_of[r].cell + t - runs_of[r].pos);
       }
       rc = pool->upload(s, d.dev_meta, (size_t)n * 2 * sizeof(int32_t), st);
       if (rc != DK_OK) return undo(rc);

@@ -327,7 +327,7 @@ int32_t Pool::check_batch(int32_t n_seqs, const int32_t* slots, const int32_t* c
 }
 
 int32_t Pool::append(int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta, const int32_t* n_accept,
-                     std::vector<int64_t>* dst_cell, std::vector<int64_t>* old_len) {
+                     std::vector<int64_t>* dst_cell, std::vector<int64_t>* old_len, std::vector<Extent>* runs) {
   std::lock_guard<std::mutex> lk(mu_);
   int32_t rc = check_batch(n_seqs, slots, cu_delta);
   if (rc != OK) return rc;
@@ -341,7 +341,11 @@ int32_t Pool::append(int32_t n_seqs, const int32_t* slots, const int32_t* cu_del
     need += s.head ? s.head->granules_needed(cnt) : (cnt + gr_ - 1) / gr_;
   }
   if (need > alloc_.free_count()) return ERR_NO_CELLS;
-  dst_cell->assign(total, -1);
+  if (dst_cell) dst_cell->assign(total, -1);
+  if (runs) {
+    runs->clear();
+    runs->reserve((size_t)(3 * (int64_t)n_seqs + total / gr_ + 1));
+  }
   if (old_len) {
     old_len->resize((size_t)n_seqs);
     for (int32_t b = 0; b < n_seqs; ++b) (*old_len)[b] = slots_[slots[b]].len;
@@ -355,7 +359,18 @@ int32_t Pool::append(int32_t n_seqs, const int32_t* slots, const int32_t* cu_del
     Node& h = *s.head;
     const int64_t old = h.len;
     h.grow(cnt);
-    for (int64_t j = 0; j < cnt; ++j) (*dst_cell)[cu_delta[b] + j] = h.cell_of(old + j);
+    if (dst_cell)
+      for (int64_t j = 0; j < cnt; ++j) (*dst_cell)[cu_delta[b] + j] = h.cell_of(old + j);
+    if (runs) {
+      for (int64_t j = 0; j < cnt;) {
+        const int64_t at = old + j, cell = h.cell_of(at);
+        const int64_t room = at < h.borrow_cap ? h.borrow_cap - at : h.gr - (at - h.borrow_cap) % h.gr;
+        const int64_t some = std::min(cnt - j, room);
+        if (j > 0 && runs->back().cell + runs->back().len == cell) runs->back().len += some;
+        else runs->push_back({cell, cu_delta[b] + j, some});
+        j += some;
+      }
+    }
     s.len += cnt;
   }
   return OK;

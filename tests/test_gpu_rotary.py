@@ -87,6 +87,17 @@ def test_in_place_and_one_kind_of_rows(dtype):
     assert torch.equal(out, x)
 
 
+@pytest.mark.parametrize("rotary,pairs", [(16, False), (16, True), (18, False), (6, True)])
+def test_what_is_not_turned_stays_whatever_its_neighbours_hold(rotary, pairs):
+    x = torch.randn((3, 2, 64), device="cuda", dtype=torch.bfloat16)
+    x[:, :, rotary::3] = float("nan")
+    x[:, 1, rotary + 1::5] = float("inf")
+    out = torch.empty_like(x)
+    dk.rotate_rows(torch.tensor([3, 9, 1000], device="cuda"), x, None, dk.Rotary(rotary, torch.ones(rotary // 2, device="cuda"), pairs), out, None)
+    assert torch.equal(out[:, :, rotary:].view(torch.int16), x[:, :, rotary:].view(torch.int16))
+    assert torch.isfinite(out[:, :, :rotary]).all()
+
+
 def test_no_rows_and_many_rows():
     r = dk.Rotary(64, torch.ones(32, device="cuda"))
     none = torch.empty((0, 4, 64), device="cuda")
