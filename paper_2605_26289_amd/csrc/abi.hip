@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cfloat>
+#include <cmath>
 #include <chrono>
 #include <cstdio>
 #include <cstdlib>
@@ -916,6 +917,10 @@ int32_t dk_scored_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     // (the bf16 kernels take the tangent from an exponential of base 2, the fp32 kernel by its name)
     const double c = sp.capped ? (double)scale / scores->cap * (sp.f32 ? 1.0 : 2.0 * log2e) : scale * log2e;
     sp.c = (float)std::min<double>(std::max<double>(c, -FLT_MAX), FLT_MAX);
+    if (!sp.f32) {  // (a scale of nothing makes all scores alike, and so does the smallest)
+      sp.flip = sp.c < 0.f ? 0x80008000u : 0u;
+      sp.c = std::max(std::fabs(sp.c), FLT_MIN);
+    }
     sp.cap = (float)(scores->cap * log2e);
     sp.slopes = scores->slopes;
     sp.window = scores->window;

@@ -9,6 +9,7 @@
 #include <hip/hip_runtime.h>
 
 #include <mutex>
+#include <type_traits>
 
 #include "kernels.hpp"
 #include "scored_common.hpp"
@@ -20,10 +21,21 @@ namespace {
 
 constexpr float SCORED_RESCALE_SLACK = 8.f;  // log2 units, as in the block kernel
 
-__device__ __forceinline__ float max3(float a, float b, float c) {
+// The largest of 16 values, raw products among them: the builtin would first make each of those canonical, an instruction a value.
+__device__ __forceinline__ float max16(const f32x16& s) {
   float d;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+  asm("v_max3_f32 %0, %1, %2, %3\n\tv_max3_f32 %0, %0, %4, %5\n\tv_max3_f32 %0, %0, %6, %7\n\tv_max3_f32 %0, %0, %8, %9\n\t"
+      "v_max3_f32 %0, %0, %10, %11\n\tv_max3_f32 %0, %0, %12, %13\n\tv_max3_f32 %0, %0, %14, %15\n\tv_max_f32 %0, %0, %16"
+      : "=&v"(d)
+      : "v"(s[0]), "v"(s[1]), "v"(s[2]), "v"(s[3]), "v"(s[4]), "v"(s[5]), "v"(s[6]), "v"(s[7]), "v"(s[8]), "v"(s[9]), "v"(s[10]),
+        "v"(s[11]), "v"(s[12]), "v"(s[13]), "v"(s[14]), "v"(s[15]));
   return d;
+}
+
+// A Q fragment, its signs turned where the scale is negative (the kernels work with the scale's size).
+__device__ __forceinline__ bf16x8 signed_q(bf16x8 q, uint32_t flip) {
+  typedef __attribute__((ext_vector_type(4))) uint32_t words;
+  return __builtin_bit_cast(bf16x8, __builtin_bit_cast(words, q) ^ words{flip, flip, flip, flip});
 }
 
 // The kernels' first argument holds the descriptors if they fit; otherwise they are in the workspace.
@@ -72,15 +84,107 @@ __device__ __forceinline__ void change_scores(const ScoreParams& sp, float slope
     s[r] = t;
   }
 }
-// Hides the keys of a 32-key block outside lo .. hi (relative to the block's key 4 h).
-__device__ __forceinline__ void hide_scores(int lo, int hi, f32x16& s) {
+// The keys of a 32-key block that a row does not see: those outside lo .. lo + span - 1 (relative to the block's key 4 h).
+struct Seen {
+  int32_t lo;
+  uint32_t span;
+  __device__ __forceinline__ bool hidden(int r) const { return (uint32_t)(8 * (r >> 2) + (r & 3) - lo) >= span; }
+};
+__device__ __forceinline__ Seen seen_of(const RowRange& rr, int at, int end) {  // at: the block's key 4 h; end: behind the tile's last
+  const int lo = max(rr.from - at, 0);
+  return {lo, (uint32_t)max(0, min(end, rr.last + 1) - at - lo)};
+}
+__device__ __forceinline__ void hide_scores(const Seen& seen, f32x16& s) {
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int key = 8 * (r >> 2) + (r & 3);
-    if (key < lo || key > hi) s[r] = -INFINITY;
-  }
+  for (int r = 0; r < 16; ++r) s[r] = seen.hidden(r) ? -INFINITY : s[r];
 }
 
+// One tile's raw products of 32 rows, KB blocks of 32 keys, to weights: packed pairs in the order of the second product's operand.
+// Scores rise with the products (the scale is positive), so without a bias by distance the tile's largest score is that of its largest
+// product, and a score and its distance from the reference maximum are one fused operation.  `rescale(alpha)` is called where the
+// reference maximum is raised, which it only is when the tile outgrows it by more than the slack; `tick(i)` four times for every eight
+// weights, i from 0 to 8 KB - 1, for matrix instructions of the caller's to stand between those of the vector unit.
+template <bool CAP, bool BIAS, int KB, typename Rescale, typename Tick>
+__device__ __forceinline__ void weigh(const ScoreParams& sp, const RowRange& rr, float slope, int tpos, int tcnt, int h, bool whole,
+                                      f32x16 (&s)[KB], float& m, float& l, uint32_t (&pw)[KB][8], Rescale&& rescale, Tick&& tick) {
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) {
+    const int at = tpos + 32 * kb + 4 * h;
+    if constexpr (BIAS) change_scores<CAP, BIAS>(sp, slope, (float)(at - rr.pos), s[kb]);
+    if (!whole) hide_scores(seen_of(rr, at, tpos + tcnt), s[kb]);
+  }
+  float mx = max16(s[0]);
+  if constexpr (KB == 2) mx = fmaxf(mx, max16(s[KB - 1]));
+  mx = fmaxf(mx, __shfl_xor(mx, 32));
+  if constexpr (!BIAS) {
+    const float t = CAP ? __builtin_fmaf(-2.f * sp.cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(mx * sp.c)), sp.cap) : mx * sp.c;
+    mx = mx == -INFINITY ? mx : t;
+  }
+  if (__builtin_amdgcn_ballot_w64(mx > m + SCORED_RESCALE_SLACK) != 0) {
+    const float mn = fmaxf(m, mx);
+    const float alpha = __builtin_amdgcn_exp2f(m - ((mn == -INFINITY) ? 0.f : mn));
+    m = mn;
+    l *= alpha;
+    rescale(alpha);
+  }
+  const float ms = (m == -INFINITY) ? 0.f : m;
+  const float top = sp.cap - ms;
+  float sums[2] = {0.f, 0.f};
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int at = 8 * kb + 4 * q;
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float raw = s[kb][8 * q + i];
+        if constexpr (BIAS) x[i] = raw - ms;
+        else if constexpr (CAP) x[i] = raw * sp.c;
+        else x[i] = __builtin_fmaf(raw, sp.c, -ms);
+      }
+      tick(at);
+      if constexpr (CAP && !BIAS) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(x[i]);
+        tick(at + 1);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_rcpf(1.f + x[i]);
+        tick(at + 2);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(-2.f * sp.cap, x[i], top);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(x[i]);
+      if constexpr (!CAP || BIAS) {
+        tick(at + 1);
+        tick(at + 2);
+      }
+      if constexpr (CAP && !BIAS) {
+        if (!whole) {  // (a hidden score has come out as -cap)
+          Seen seen = seen_of(rr, tpos + 32 * kb + 4 * h, tpos + tcnt);
+          asm volatile("" : "+v"(seen.lo), "+v"(seen.span));  // (compared anew: 32 masks do not fit the scalar registers)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = seen.hidden(8 * q + i) ? 0.f : x[i];
+        }
+      }
+      tick(at + 3);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        sums[0] += x[2 * w];
+        sums[1] += x[2 * w + 1];
+        pw[kb][4 * q + w] = pack_pair(x[2 * w], x[2 * w + 1]);
+      }
+    }
+  l += sums[0] + sums[1];
+}
+// Fragment j (16 keys) of a tile's weights.
+template <int KB>
+__device__ __forceinline__ bf16x8 weight_frag(const uint32_t (&pw)[KB][8], int j) {
+  typedef __attribute__((ext_vector_type(4))) uint32_t words;
+  const uint32_t* w = &pw[j >> 1][4 * (j & 1)];
+  return __builtin_bit_cast(bf16x8, words{w[0], w[1], w[2], w[3]});
+}
 // Rows rl0 .. rl0 + 31 of the item, depth block db, done again without the non-finite elements of V (see redo_rows): what
 // those make of a row is counted by products of their own, of one for every element and one for every key that a row sees.
 // Of the block's four quads of depths, `quads` from quad0 on are this wavefront's to store.
@@ -100,7 +204,7 @@ __device__ __forceinline__ void redo_scored(const Ctx& c, const ScoreParams& sp,
   const int64_t orow = (int64_t)(e.tok0 + tok) * c.n_q_heads + head;
   bf16x8 qf[G::KS];
 #pragma unroll
-  for (int ks = 0; ks < G::KS; ++ks) qf[ks] = *(const bf16x8*)(c.q + orow * HD + ks * 16 + 8 * h);
+  for (int ks = 0; ks < G::KS; ++ks) qf[ks] = signed_q(*(const bf16x8*)(c.q + orow * HD + ks * 16 + 8 * h), sp.flip);
   if (m == -INFINITY) m = 0.f;
   f32x16 o, odd[3];  // sums; counts of NaN, +infinity, -infinity
 #pragma unroll
@@ -116,7 +220,7 @@ __device__ __forceinline__ void redo_scored(const Ctx& c, const ScoreParams& sp,
     for (int ks = 0; ks < G::KS; ++ks)
       s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(kp + 32 * ks), qf[ks], s, 0, 0, 0);
     change_scores<CAP, BIAS>(sp, slope, (float)(t.pos + 4 * h - rr.pos), s);
-    hide_scores(rr.from - t.pos - 4 * h, min(t.cnt - 1, rr.last - t.pos) - 4 * h, s);
+    const Seen sees = seen_of(rr, t.pos + 4 * h, t.pos + t.cnt);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       bf16x8 p, seen, v, is[3];
@@ -129,9 +233,9 @@ __device__ __forceinline__ void redo_scored(const Ctx& c, const ScoreParams& sp,
         is[0][x] = (__bf16)(!fine && (bits & 0x7fu) ? 1.f : 0.f);
         is[1][x] = (__bf16)(bits == 0x7f80u ? 1.f : 0.f);
         is[2][x] = (__bf16)(bits == 0xff80u ? 1.f : 0.f);
-        const float score = s[8 * j + x];
-        seen[x] = (__bf16)(score != -INFINITY ? 1.f : 0.f);
-        p[x] = (__bf16)__builtin_amdgcn_exp2f(score - m);
+        const bool hidden = sees.hidden(8 * j + x);
+        seen[x] = (__bf16)(hidden ? 0.f : 1.f);
+        p[x] = (__bf16)(hidden ? 0.f : __builtin_amdgcn_exp2f(s[8 * j + x] - m));
       }
       o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p, o, 0, 0, 0);
 #pragma unroll
@@ -158,6 +262,54 @@ __device__ __forceinline__ void redo_scored(const Ctx& c, const ScoreParams& sp,
   }
 }
 
+// The two products of a tile, their LDS operands AHEAD fragments in front of the product that takes them: left to itself the compiler
+// reads each fragment right before its product and waits, 16 times the latency of LDS for a tile.
+// q_of(rb, ks): the Q fragment; S^T of RB row blocks of 32 against KB blocks of 32 keys.
+template <int HD, int KB, int RB, int AHEAD, typename Q>
+__device__ __forceinline__ void score_products(const char* k_lds, uint32_t koff, f32x16 (&s)[RB][KB], Q&& q_of) {
+  constexpr int N = Geo<HD>::KS * KB;
+  bf16x8 kf[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) kf[i] = read_k_frag<HD>(k_lds, koff, i % KB, i / KB);
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[rb][kb][r] = 0.f;
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+      s[rb][i % KB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % AHEAD], q_of(rb, i / KB), s[rb][i % KB], 0, 0, 0);
+    if (i + AHEAD < N) kf[i % AHEAD] = read_k_frag<HD>(k_lds, koff, (i + AHEAD) % KB, (i + AHEAD) / KB);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+template <int HD, int AHEAD>
+struct ValueFrags {
+  bf16x8 vf[AHEAD];
+  __device__ __forceinline__ void first(const char* v_lds, uint32_t voff) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) vf[i] = read_v_frag<HD>(v_lds, voff, i / Geo<HD>::DB, i % Geo<HD>::DB);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  // O^T += V^T P^T of RB row blocks
+  template <int KB, int RB>
+  __device__ __forceinline__ void products(const char* v_lds, uint32_t voff, const uint32_t (&pw)[RB][KB][8], f32x16 (&o)[RB][Geo<HD>::DB]) {
+    constexpr int DB = Geo<HD>::DB, N = 2 * KB * DB;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+        o[rb][i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % AHEAD], weight_frag<KB>(pw[rb], i / DB), o[rb][i % DB], 0, 0, 0);
+      if (i + AHEAD < N) vf[i % AHEAD] = read_v_frag<HD>(v_lds, voff, (i + AHEAD) / DB, (i + AHEAD) % DB);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+};
+
 template <typename F>
 __device__ __forceinline__ uint32_t bad_rows(F&& any) {
   const uint64_t b = __builtin_amdgcn_ballot_w64(any);
@@ -174,17 +326,19 @@ constexpr int ROWS_KT = 64;  // keys per tile of the rows kernel
 template <int HD>
 struct RowsGeo {
   static constexpr int TILE_BYTES = ROWS_KT * Geo<HD>::ROW;
-  static constexpr int STAGE_BYTES = 2 * TILE_BYTES;
-  static constexpr int STAGES = HD == 128 ? 2 : 4;  // 64 KiB of LDS either way
-  static constexpr int LDS_BYTES = STAGES * STAGE_BYTES;
-  static constexpr int LOADS = STAGE_BYTES / 1024 / 4;  // 1 KiB requests per wavefront and tile
+  static constexpr int K_STAGES = 2, V_STAGES = 3;  // 80 KiB of LDS with 128-wide heads: two workgroups fill a compute unit's 160
+  static constexpr int V_OFFSET = K_STAGES * TILE_BYTES;
+  static constexpr int LDS_BYTES = V_OFFSET + V_STAGES * TILE_BYTES;
+  static constexpr int LOADS = TILE_BYTES / 1024 / 4;  // 1 KiB requests per wavefront for a tile's K, as many for its V
 };
 
 }  // namespace
 
 // Many rows: a workgroup owns 128 packed query rows of one KV head (4 wavefronts x 32) and walks the keys of its item in tiles
-// of 64 that the wavefronts share through an LDS ring, two workgroups to a compute unit, as in the block kernel.
-// Workgroup w: item w / n_kv_heads, KV head w % n_kv_heads.
+// of 64 that the wavefronts share through LDS, two workgroups to a compute unit.  Step t turns the products of tile t into weights with
+// the products of tile t + 1 among the instructions of the vector unit, which with capped scores has more to do than the matrix
+// cores: 28 of its cycles for a cap and 16 for the rest against 32 for a score's two products (128-wide heads).
+// K of a tile is requested a step ahead, V two.  Workgroup w: item w / n_kv_heads, KV head w % n_kv_heads.
 template <int HD, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void scored_rows_kernel(InlineBlob blob, Ctx c, ScoreParams sp) {
   typedef Geo<HD> G;
@@ -215,112 +369,101 @@ __global__ __launch_bounds__(256, 2) void scored_rows_kernel(InlineBlob blob, Ct
   {
     const __bf16* qp = c.q + ((int64_t)(e.tok0 + tok) * c.n_q_heads + head) * HD + 8 * h;
 #pragma unroll
-    for (int ks = 0; ks < G::KS; ++ks) qf[ks] = *(const bf16x8*)(qp + ks * 16);
+    for (int ks = 0; ks < G::KS; ++ks) qf[ks] = signed_q(*(const bf16x8*)(qp + ks * 16), sp.flip);
   }
 
   KvCursor<G::ROW> cur{c.segs, e.seg_begin, e.seg_end, it.kv_lo, it.kv_hi};
-  int cnt[B::STAGES] = {}, pos[B::STAGES] = {};  // tiles requested and not yet computed, oldest first
-  int stage_wr = 0;
+  int cnt[3], pos[3];  // of tiles t, t + 1 and t + 2 (0 keys: none)
+  int v_wr = 0;
   KvTile t;
-  auto request = [&](int slot) {
+  const auto request = [&](int slot, int k_stage) __attribute__((always_inline)) {
     cnt[slot] = 0;
     if (!cur.next(c, g, ROWS_KT, t)) return;
     cnt[slot] = t.cnt;
     pos[slot] = t.pos;
-    char* kl = smem + stage_wr * B::STAGE_BYTES;
-    char* vl = kl + B::TILE_BYTES;
+    char* kl = smem + k_stage * B::TILE_BYTES;
+    char* vl = smem + B::V_OFFSET + v_wr * B::TILE_BYTES;
 #pragma unroll
-    for (int b = 0; b < B::LOADS / 2; ++b) load_kib<false, HD>(t.k, t.stride, t.cnt, kl, b * 4 + wave, lane);
+    for (int b = 0; b < B::LOADS; ++b) load_kib<false, HD>(t.k, t.stride, t.cnt, kl, b * 4 + wave, lane);
 #pragma unroll
-    for (int b = 0; b < B::LOADS / 2; ++b) load_kib<true, HD>(t.v, t.stride, t.cnt, vl, b * 4 + wave, lane);
-    stage_wr = stage_wr + 1 == B::STAGES ? 0 : stage_wr + 1;
+    for (int b = 0; b < B::LOADS; ++b) load_kib<true, HD>(t.v, t.stride, t.cnt, vl, b * 4 + wave, lane);
+    v_wr = v_wr + 1 == B::V_STAGES ? 0 : v_wr + 1;
   };
-#pragma unroll
-  for (int s = 0; s < B::STAGES - 1; ++s) request(s);
+  request(0, 0);
+  request(1, 1);
 #pragma unroll
   for (int ks = 0; ks < G::KS; ++ks) asm volatile("" ::"v"(qf[ks]));  // Q is waited for here, once
   asm volatile("" ::"v"(rr.from), "v"(slope));
 
-  f32x16 o[G::DB];
+  f32x16 o[1][G::DB];
   float m = -INFINITY, l = 0.f;
 #pragma unroll
   for (int db = 0; db < G::DB; ++db)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) o[db][r] = 0.f;
+    for (int r = 0; r < 16; ++r) o[0][db][r] = 0.f;
+  const auto sees = [&](int slot) { return active && cnt[slot] > 0 && pos[slot] <= wr.any_last && pos[slot] + cnt[slot] - 1 >= wr.any_from; };
 
-  int stage_rd = 0;
-  while (cnt[0] > 0) {
-    int younger = 0;
-#pragma unroll
-    for (int s = 1; s < B::STAGES - 1; ++s) younger += cnt[s] > 0;
-    if (B::STAGES > 3 && younger == 2) wait_vmcnt<2 * B::LOADS>();
-    else if (B::STAGES > 2 && younger == 1) wait_vmcnt<B::LOADS>();
+  // S^T of tile 0: behind its K come its V and tile 1
+  f32x16 sa[1][2], sb[1][2];
+  if (cnt[1] > 0) wait_vmcnt<3 * B::LOADS>();
+  else wait_vmcnt<0>();
+  scored_barrier();
+  if (sees(0)) score_products<HD, 2, 1, 8>(smem, koff, sa, [&](int, int ks) { return qf[ks]; });
+
+  int v_rd = 0;
+  const auto step = [&](auto k_stage, f32x16 (&s)[1][2], f32x16 (&next)[1][2]) __attribute__((always_inline)) {
+    constexpr int KST = decltype(k_stage)::value;  // where K of this tile was, and K of the tile after the next goes
+    if (cnt[1] > 0) wait_vmcnt<B::LOADS>();  // only V of the next tile may be out
     else wait_vmcnt<0>();
-    scored_barrier();  // landed for every wavefront, and the tile before it is finished everywhere
-    request(B::STAGES - 1);
-    const char* k_lds = smem + stage_rd * B::STAGE_BYTES;
-    const char* v_lds = k_lds + B::TILE_BYTES;
-    stage_rd = stage_rd + 1 == B::STAGES ? 0 : stage_rd + 1;
+    scored_barrier();  // landed for every wavefront; K of this tile and V of the one before have been read everywhere
+    request(2, KST);
+    const char* k_lds = smem + (1 - KST) * B::TILE_BYTES;
+    const char* v_lds = smem + B::V_OFFSET + v_rd * B::TILE_BYTES;
+    v_rd = v_rd + 1 == B::V_STAGES ? 0 : v_rd + 1;
     const int tcnt = cnt[0], tpos = pos[0];
-#pragma unroll
-    for (int s = 0; s < B::STAGES - 1; ++s) {
-      cnt[s] = cnt[s + 1];
-      pos[s] = pos[s + 1];
+    const bool has = sees(0), has_next = sees(1);
+    cnt[0] = cnt[1];
+    pos[0] = pos[1];
+    cnt[1] = cnt[2];
+    pos[1] = pos[2];
+    if (!has) {
+      if (has_next) score_products<HD, 2, 1, 8>(k_lds, koff, next, [&](int, int ks) { return qf[ks]; });
+      return;
     }
-    if (!active || tpos > wr.any_last || tpos + tcnt - 1 < wr.any_from) continue;  // no row of this wavefront sees the tile
-
-    f32x16 s[2];
+    asm volatile("s_nop 11" : "+v"(s[0][0]), "+v"(s[0][1]));  // (inline assembly reads them, which the compiler does not wait for)
+    const bool whole = tcnt == ROWS_KT && tpos >= wr.all_from && tpos + ROWS_KT - 1 <= wr.all_last;
+    uint32_t pw[1][2][8];
+    const auto rescale = [&](float alpha) {
+#pragma unroll
+      for (int db = 0; db < G::DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[0][db][r] *= alpha;
+    };
+    // (the next tile's products are computed whether a row sees it or not: a wavefront's tiles are nearly always all seen)
+    constexpr int N = 2 * G::KS, AHEAD = 4;
+    bf16x8 kf[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) kf[i] = read_k_frag<HD>(k_lds, koff, i % 2, i / 2);
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < G::KS; ++ks)
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_k_frag<HD>(k_lds, koff, kb, ks), qf[ks], s[kb], 0, 0, 0);
-    const bool whole = tcnt == ROWS_KT && tpos >= wr.all_from && tpos + ROWS_KT - 1 <= wr.all_last;
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      const int at = tpos + 32 * kb + 4 * h;
-      change_scores<CAP, BIAS>(sp, slope, (float)(at - rr.pos), s[kb]);
-      if (!whole) hide_scores(rr.from - at, min(tpos + tcnt - 1, rr.last) - at, s[kb]);
-    }
-    float mx = max3(s[0][0], s[1][0], s[0][1]);
-    mx = fmaxf(mx, s[1][1]);
-#pragma unroll
-    for (int r = 2; r < 16; ++r) mx = max3(mx, s[0][r], s[1][r]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    // the reference maximum is only raised when the tile outgrows it by more than the slack
-    if (__builtin_amdgcn_ballot_w64(mx > m + SCORED_RESCALE_SLACK) != 0) {
-      const float mn = fmaxf(m, mx);
-      const float alpha = __builtin_amdgcn_exp2f(m - ((mn == -INFINITY) ? 0.f : mn));
-      m = mn;
-      l *= alpha;
-#pragma unroll
-      for (int db = 0; db < G::DB; ++db)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
-    }
-    const float ms = (m == -INFINITY) ? 0.f : m;
-    float rs[2] = {0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      typedef __attribute__((ext_vector_type(4))) uint32_t words;
-      words p;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float p0 = __builtin_amdgcn_exp2f(s[j >> 1][8 * (j & 1) + 2 * w] - ms);
-        const float p1 = __builtin_amdgcn_exp2f(s[j >> 1][8 * (j & 1) + 2 * w + 1] - ms);
-        rs[w & 1] += p0 + p1;
-        p[w] = pack_pair(p0, p1);
-      }
-      const bf16x8 pf = __builtin_bit_cast(bf16x8, p);
-#pragma unroll
-      for (int db = 0; db < G::DB; ++db)
-        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_v_frag<HD>(v_lds, voff, j, db), pf, o[db], 0, 0, 0);
-    }
-    l += rs[0] + rs[1];
+      for (int r = 0; r < 16; ++r) next[0][kb][r] = 0.f;
+    weigh<CAP, BIAS, 2>(sp, rr, slope, tpos, tcnt, h, whole, s[0], m, l, pw[0], rescale, [&](int i) __attribute__((always_inline)) {
+      if (16 / N * (i / (16 / N)) != i) return;  // (64-wide heads: every other time)
+      const int n = i / (16 / N);
+      __builtin_amdgcn_sched_barrier(0);
+      next[0][n % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[n % AHEAD], qf[n / 2], next[0][n % 2], 0, 0, 0);
+      if (n + AHEAD < N) kf[n % AHEAD] = read_k_frag<HD>(k_lds, koff, (n + AHEAD) % 2, (n + AHEAD) / 2);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    ValueFrags<HD, 4> values;
+    values.first(v_lds, voff);
+    values.template products<2, 1>(v_lds, voff, pw, o);
+  };
+  while (cnt[0] > 0) {
+    step(std::integral_constant<int, 0>(), sa, sb);
+    if (cnt[0] <= 0) break;
+    step(std::integral_constant<int, 1>(), sb, sa);
   }
   if (!active) return;
   const float lt = l + __shfl_xor(l, 32);
@@ -330,8 +473,8 @@ __global__ __launch_bounds__(256, 2) void scored_rows_kernel(InlineBlob blob, Ct
     f32x4 quads[4];
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      quads[r >> 2][r & 3] = o[db][r];
-      z = __builtin_fmaf(o[db][r], 0.f, z);
+      quads[r >> 2][r & 3] = o[0][db][r];
+      z = __builtin_fmaf(o[0][db][r], 0.f, z);
     }
     store_quads<HD, true>(c, e, it, g, wave * 32 + (lane & 31), db * 32 + 4 * h, quads, lt == 0.f ? 1.f : lt);
   }
@@ -393,6 +536,8 @@ __global__ __launch_bounds__(256, 2) void scored_few_kernel(InlineBlob blob, Ctx
   KvCursor<G::ROW> cur{c.segs, e.seg_begin, e.seg_end, lo, hi};
   // tiles t (slot 0), t + 1 (slot 1) and, from the middle of step t on, t + 2
   KvTile tiles[3];
+  // (the requests' offsets are kept from tile to tile where there are registers for them)
+  constexpr bool KEEP = RB == 1;
   uint32_t offk[8], offv[8], off_stride = 0;
   int off_cnt = 0;
   const auto offsets = [&](const KvTile& t) __attribute__((always_inline)) {
@@ -405,18 +550,27 @@ __global__ __launch_bounds__(256, 2) void scored_few_kernel(InlineBlob blob, Ctx
       offv[b] = kib_biased_off<true, HD>(t.stride, t.cnt, b, lane);
     }
   };
+  const auto request = [&](auto is_v, const KvTile& t, int stage) __attribute__((always_inline)) {
+    constexpr bool V = decltype(is_v)::value;
+    if (t.cnt == 0) return;
+    const char* from = V ? t.v : t.k;
+    const uint32_t to = mine_addr + stage * 16384 + (V ? 8192 : 0);
+    if constexpr (KEEP) {
+      offsets(t);
+      load_eight_kib<false>(from, V ? offv : offk, to);
+    } else {
+      int at = lane;
+      asm volatile("" : "+v"(at));
+      uint32_t off[8];
+#pragma unroll
+      for (int b = 0; b < 8; ++b) off[b] = kib_biased_off<V, HD>(t.stride, t.cnt, b, at);
+      load_eight_kib<false>(from, off, to);
+    }
+  };
+  const auto request_k = [&](const KvTile& t, int stage) __attribute__((always_inline)) { request(std::false_type(), t, stage); };
+  const auto request_v = [&](const KvTile& t, int stage) __attribute__((always_inline)) { request(std::true_type(), t, stage); };
   const auto take = [&](KvTile& t) __attribute__((always_inline)) {
     if (!cur.next(c, g, F::KT, t)) t.cnt = 0;
-  };
-  const auto request_k = [&](const KvTile& t, int stage) __attribute__((always_inline)) {
-    if (t.cnt == 0) return;
-    offsets(t);
-    load_eight_kib<false>(t.k, offk, mine_addr + stage * 16384);
-  };
-  const auto request_v = [&](const KvTile& t, int stage) __attribute__((always_inline)) {
-    if (t.cnt == 0) return;
-    offsets(t);
-    load_eight_kib<false>(t.v, offv, mine_addr + stage * 16384 + 8192);
   };
   take(tiles[0]);
   request_k(tiles[0], 0);
@@ -438,8 +592,8 @@ __global__ __launch_bounds__(256, 2) void scored_few_kernel(InlineBlob blob, Ctx
     const __bf16* qp = c.q + ((int64_t)(e.tok0 + tok) * c.n_q_heads + head) * HD + 8 * h;
 #pragma unroll
     for (int ks = 0; ks < G::KS; ++ks) {
-      if (!Q_IN_LDS) qf[ks] = *(const bf16x8*)(qp + ks * 16);
-      else if (ks % 4 == wave) q_lds[(rb * G::KS + ks) * 64] = *(const bf16x8*)(qp + ks * 16);
+      if (!Q_IN_LDS) qf[ks] = signed_q(*(const bf16x8*)(qp + ks * 16), sp.flip);
+      else if (ks % 4 == wave) q_lds[(rb * G::KS + ks) * 64] = signed_q(*(const bf16x8*)(qp + ks * 16), sp.flip);
     }
   }
 #pragma unroll
@@ -477,21 +631,7 @@ __global__ __launch_bounds__(256, 2) void scored_few_kernel(InlineBlob blob, Ctx
     const char* k_lds = mine + stage * 16384;
     const char* v_lds = k_lds + 8192;
     f32x16 s[RB][F::KB];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-      for (int kb = 0; kb < F::KB; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[rb][kb][r] = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < G::KS; ++ks)
-#pragma unroll
-      for (int kb = 0; kb < F::KB; ++kb) {
-        const bf16x8 kf = read_k_frag<HD>(k_lds, koff, kb, ks);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-          s[rb][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, Q_IN_LDS ? q_lds[(rb * G::KS + ks) * 64] : qf[ks], s[rb][kb], 0, 0, 0);
-      }
+    score_products<HD, F::KB, RB, RB == 1 ? 4 : 2>(k_lds, koff, s, [&](int rb, int ks) { return Q_IN_LDS ? q_lds[(rb * G::KS + ks) * 64] : qf[ks]; });
     // K has been read.  (The products are waited for here, on this side of the branches that follow: the compiler's own wait, on
     // the far side, counts the states of the longest way there.)
 #pragma unroll
@@ -506,56 +646,22 @@ __global__ __launch_bounds__(256, 2) void scored_few_kernel(InlineBlob blob, Ctx
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       const bool whole = tcnt == F::KT && tpos >= wr[rb].all_from && tpos + F::KT - 1 <= wr[rb].all_last;
-#pragma unroll
-      for (int kb = 0; kb < F::KB; ++kb) {
-        const int at = tpos + 32 * kb + 4 * h;
-        change_scores<CAP, BIAS>(sp, slope[rb], (float)(at - rr[rb].pos), s[rb][kb]);
-        if (!whole) hide_scores(rr[rb].from - at, min(tpos + tcnt - 1, rr[rb].last) - at, s[rb][kb]);
-      }
-      float mx = s[rb][0][0];
-#pragma unroll
-      for (int kb = 0; kb < F::KB; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; r += 2) mx = max3(mx, s[rb][kb][r], s[rb][kb][r + 1]);
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
-      if (__builtin_amdgcn_ballot_w64(mx > m[rb] + SCORED_RESCALE_SLACK) != 0) {
-        const float mn = fmaxf(m[rb], mx);
-        const float alpha = __builtin_amdgcn_exp2f(m[rb] - ((mn == -INFINITY) ? 0.f : mn));
-        m[rb] = mn;
-        l[rb] *= alpha;
+      weigh<CAP, BIAS, F::KB>(sp, rr[rb], slope[rb], tpos, tcnt, h, whole, s[rb], m[rb], l[rb], pw[rb], [&](float alpha) {
 #pragma unroll
         for (int db = 0; db < G::DB; ++db)
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[rb][db][r] *= alpha;
-      }
-      const float ms = (m[rb] == -INFINITY) ? 0.f : m[rb];
-      float rs[2] = {0.f, 0.f};
-#pragma unroll
-      for (int kb = 0; kb < F::KB; ++kb)
-#pragma unroll
-        for (int w = 0; w < 8; ++w) {
-          const float p0 = __builtin_amdgcn_exp2f(s[rb][kb][2 * w] - ms), p1 = __builtin_amdgcn_exp2f(s[rb][kb][2 * w + 1] - ms);
-          rs[w & 1] += p0 + p1;
-          pw[rb][kb][w] = pack_pair(p0, p1);
-        }
-      l[rb] += rs[0] + rs[1];
+      }, [](int) {
+        if (RB > 1) __builtin_amdgcn_sched_barrier(0);  // (one group of weights at a time: the registers are full)
+      });
     }
     // requests younger than V of this tile: K and V of the next one, K of the one after
     if (one_more && tiles[2].cnt > 0) wait_vmcnt<24>();
     else if (one_more) wait_vmcnt<16>();
     else wait_vmcnt<0>();
-#pragma unroll
-    for (int j = 0; j < 2 * F::KB; ++j)
-#pragma unroll
-      for (int db = 0; db < G::DB; ++db) {
-        const bf16x8 vf = read_v_frag<HD>(v_lds, voff, j, db);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          typedef __attribute__((ext_vector_type(4))) uint32_t words;
-          const uint32_t* w = &pw[rb][j >> 1][4 * (j & 1)];
-          o[rb][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, words{w[0], w[1], w[2], w[3]}), o[rb][db], 0, 0, 0);
-        }
-      }
+    ValueFrags<HD, RB == 1 ? 4 : 2> values;
+    values.first(v_lds, voff);
+    values.template products<F::KB, RB>(v_lds, voff, pw, o);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V has been read
     request_v(tiles[2], stage);
     tiles[0] = tiles[1];

@@ -113,7 +113,8 @@ hipError_t launch_attend_merge(const AttendArgs& a, const DkMerge* merges, int32
 
 // Attention with changed scores.
 struct ScoreParams {
-  float c = 0.f;    // raw product to score in log2 units; capped: to the exponent of u, 2 log2(e) scale / cap
+  float c = 0.f;      // raw product to score in log2 units; capped: to the exponent of u, 2 log2(e) scale / cap (bf16: positive)
+  uint32_t flip = 0;  // bf16: the sign bits of a pair of Q's elements, where the scale is negative
   float cap = 0.f;  // log2 units
   bool capped = false, has_first = false, f32 = false;
   bool in_args = false;           // descriptors travel in the kernel arguments: pointers to them are offsets
