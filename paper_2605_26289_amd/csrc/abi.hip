@@ -266,6 +266,7 @@ int32_t dk_pool_create(const dk_pool_desc* desc, dk_pool** pool_out) {
     p->scored_cfg.n_kv_heads = desc->n_kv_heads;
     p->scored_cfg.head_dim = desc->head_dim;
     p->scored_cfg.bf16 = desc->dtype == DK_BF16;
+    p->scored_cfg.once_cells = p->cfg.once_cells;
     p->arrival_slice = take_slice();
     *pool_out = p;
     return DK_OK;

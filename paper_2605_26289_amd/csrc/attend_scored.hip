@@ -112,6 +112,7 @@ __device__ __forceinline__ void weigh(const ScoreParams& sp, const RowRange& rr,
     const int at = tpos + 32 * kb + 4 * h;
     if constexpr (BIAS) change_scores<CAP, BIAS>(sp, slope, (float)(at - rr.pos), s[kb]);
     if (!whole) hide_scores(seen_of(rr, at, tpos + tcnt), s[kb]);
+    asm volatile("" : "+v"(s[kb]));  // (the way around the branch and the way through it meet in the same registers)
   }
   float mx = max16(s[0]);
   if constexpr (KB == 2) mx = fmaxf(mx, max16(s[KB - 1]));
@@ -521,7 +522,7 @@ __global__ __launch_bounds__(256, 2) void scored_few_kernel(InlineBlob blob, Ctx
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5;
-  const uint32_t koff = k_lane_off<HD>(lane), voff = v_lane_off<HD>(lane);
+  uint32_t koff = k_lane_off<HD>(lane), voff = v_lane_off<HD>(lane);
   char* mine = smem + wave * F::WAVE_BYTES;
   const uint32_t mine_addr = (uint32_t)(uintptr_t)(lds_void_ptr)mine;
 
@@ -536,8 +537,7 @@ __global__ __launch_bounds__(256, 2) void scored_few_kernel(InlineBlob blob, Ctx
   KvCursor<G::ROW> cur{c.segs, e.seg_begin, e.seg_end, lo, hi};
   // tiles t (slot 0), t + 1 (slot 1) and, from the middle of step t on, t + 2
   KvTile tiles[3];
-  // (the requests' offsets are kept from tile to tile where there are registers for them)
-  constexpr bool KEEP = RB == 1;
+  // (the requests' offsets are the same for all whole tiles of a segment)
   uint32_t offk[8], offv[8], off_stride = 0;
   int off_cnt = 0;
   const auto offsets = [&](const KvTile& t) __attribute__((always_inline)) {
@@ -555,17 +555,9 @@ __global__ __launch_bounds__(256, 2) void scored_few_kernel(InlineBlob blob, Ctx
     if (t.cnt == 0) return;
     const char* from = V ? t.v : t.k;
     const uint32_t to = mine_addr + stage * 16384 + (V ? 8192 : 0);
-    if constexpr (KEEP) {
-      offsets(t);
-      load_eight_kib<false>(from, V ? offv : offk, to);
-    } else {
-      int at = lane;
-      asm volatile("" : "+v"(at));
-      uint32_t off[8];
-#pragma unroll
-      for (int b = 0; b < 8; ++b) off[b] = kib_biased_off<V, HD>(t.stride, t.cnt, b, at);
-      load_eight_kib<false>(from, off, to);
-    }
+    offsets(t);
+    if (t.once) load_eight_kib<true>(from, V ? offv : offk, to);
+    else load_eight_kib<false>(from, V ? offv : offk, to);
   };
   const auto request_k = [&](const KvTile& t, int stage) __attribute__((always_inline)) { request(std::false_type(), t, stage); };
   const auto request_v = [&](const KvTile& t, int stage) __attribute__((always_inline)) { request(std::true_type(), t, stage); };
@@ -631,7 +623,9 @@ __global__ __launch_bounds__(256, 2) void scored_few_kernel(InlineBlob blob, Ctx
     const char* k_lds = mine + stage * 16384;
     const char* v_lds = k_lds + 8192;
     f32x16 s[RB][F::KB];
-    score_products<HD, F::KB, RB, RB == 1 ? 4 : 2>(k_lds, koff, s, [&](int rb, int ks) { return Q_IN_LDS ? q_lds[(rb * G::KS + ks) * 64] : qf[ks]; });
+    // (computed anew from here on in every step: kept across steps, the addresses of the fragments cost more registers than there are)
+    if constexpr (RB > 1) asm volatile("" : "+v"(koff), "+v"(voff));
+    score_products<HD, F::KB, RB, 4>(k_lds, koff, s, [&](int rb, int ks) { return Q_IN_LDS ? q_lds[(rb * G::KS + ks) * 64] : qf[ks]; });
     // K has been read.  (The products are waited for here, on this side of the branches that follow: the compiler's own wait, on
     // the far side, counts the states of the longest way there.)
 #pragma unroll
@@ -651,15 +645,13 @@ __global__ __launch_bounds__(256, 2) void scored_few_kernel(InlineBlob blob, Ctx
         for (int db = 0; db < G::DB; ++db)
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[rb][db][r] *= alpha;
-      }, [](int) {
-        if (RB > 1) __builtin_amdgcn_sched_barrier(0);  // (one group of weights at a time: the registers are full)
-      });
+      }, [](int) {});
     }
     // requests younger than V of this tile: K and V of the next one, K of the one after
     if (one_more && tiles[2].cnt > 0) wait_vmcnt<24>();
     else if (one_more) wait_vmcnt<16>();
     else wait_vmcnt<0>();
-    ValueFrags<HD, RB == 1 ? 4 : 2> values;
+    ValueFrags<HD, 4> values;
     values.first(v_lds, voff);
     values.template products<F::KB, RB>(v_lds, voff, pw, o);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V has been read

@@ -512,34 +512,7 @@ void unmark_once(AttendPlan* p) {
 // By the size of the K/V (decoding sessions of 4000 tokens; the same pass again and again, K/V that appends have just
 // written, after 600 MB of other writes): 125 MB 27.7 / 31.4, 32.4 / 42.6, 60 / 35; 250 MB 43.6 / 49.8, 64.4 / 59.2, 104 / 54;
 // 281 MB 48.7 / 50.9, 69.7 / 64.2, 112 / 55; 312 MB 54.4 / 53.1, 75.3 / 69.8, 119 / 57; 500 MB 96 / 87, 132 / 113, 160 / 90.
-// A segment is taken for shared if another entry has one that starts at the same cell (an aliased prefix does).
-void mark_once(AttendPlan* p, const PlanConfig& cfg) {
-  int64_t cells = 0;
-  size_t n = 0;
-  for (const DkSeg& s : p->segs) cells += s.src == 0 ? s.len : 0;
-  if (cfg.once_cells <= 0 || cells < cfg.once_cells) return;
-  size_t size = 16;
-  while (size < 2 * p->segs.size()) size *= 2;
-  std::vector<int32_t>& table = p->seg_table;  // open addressing by start cell
-  table.assign(size, -1);
-  for (DkSeg& s : p->segs) {
-    const int32_t i = (int32_t)n++;
-    if (s.src != 0) continue;
-    s.once = 1;
-    size_t at = (size_t)((uint64_t)s.start * 0x9E3779B97F4A7C15ull >> 32) & (size - 1);
-    while (table[at] >= 0 && p->segs[(size_t)table[at]].start != s.start) at = (at + 1) & (size - 1);
-    if (table[at] < 0) {
-      table[at] = i;
-      continue;
-    }
-    DkSeg& other = p->segs[(size_t)table[at]];
-    cells -= std::min(s.len, other.len);
-    s.once = other.once = 0;
-    if (s.len > other.len) table[at] = i;
-  }
-  p->once = true;
-  if (cells < cfg.once_cells) unmark_once(p);
-}
+void mark_once(AttendPlan* p, const PlanConfig& cfg) { p->once = mark_unshared(&p->segs, &p->seg_table, cfg.once_cells); }
 
 // Merging inside the streaming kernel: nothing else has split rows, every workgroup has one unit, every (row tile, KV
 // head) a counter of its own, and the last workgroup of a row tile reads all of its partial rows in a round or two --
@@ -667,6 +640,35 @@ bool scalar_is_cheaper(const AttendPlan& p, const PlanConfig& cfg, size_t row_ti
          c.matrix + c.wave * std::max(0.0, waves - 1.0) + (c.keys + c.wave_keys * waves) * (double)n / 128.0 + c.upload;
 }
 }  // namespace
+
+bool mark_unshared(std::vector<DkSeg>* segs, std::vector<int32_t>* by_start, int64_t once_cells) {
+  int64_t cells = 0;
+  size_t n = 0;
+  for (const DkSeg& s : *segs) cells += s.src == 0 ? s.len : 0;
+  if (once_cells <= 0 || cells < once_cells) return false;
+  size_t size = 16;
+  while (size < 2 * segs->size()) size *= 2;
+  std::vector<int32_t>& table = *by_start;  // open addressing by start cell
+  table.assign(size, -1);
+  for (DkSeg& s : *segs) {
+    const int32_t i = (int32_t)n++;
+    if (s.src != 0) continue;
+    s.once = 1;
+    size_t at = (size_t)((uint64_t)s.start * 0x9E3779B97F4A7C15ull >> 32) & (size - 1);
+    while (table[at] >= 0 && (*segs)[(size_t)table[at]].start != s.start) at = (at + 1) & (size - 1);
+    if (table[at] < 0) {
+      table[at] = i;
+      continue;
+    }
+    DkSeg& other = (*segs)[(size_t)table[at]];
+    cells -= std::min(s.len, other.len);
+    s.once = other.once = 0;
+    if (s.len > other.len) table[at] = i;
+  }
+  if (cells >= once_cells) return true;
+  for (DkSeg& s : *segs) s.once = 0;
+  return false;
+}
 
 int32_t build_plan(Pool& pool, const PlanConfig& cfg, int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta,
                    bool staged, AttendPlan* p, bool with_cells) {

@@ -162,4 +162,9 @@ struct AttendPlan {
 int32_t build_plan(Pool& pool, const PlanConfig& cfg, int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta,
                    bool staged, AttendPlan* plan, bool with_cells = false);
 
+// Marks (DkSeg::once) the segments in the pool that no two entries share, if those of the batch come to once_cells or more, and
+// tells whether it did.  A segment is taken for shared if another entry has one that starts at the same cell (an aliased
+// prefix does).  by_start is scratch memory.
+bool mark_unshared(std::vector<DkSeg>* segs, std::vector<int32_t>* by_start, int64_t once_cells);
+
 }  // namespace dk

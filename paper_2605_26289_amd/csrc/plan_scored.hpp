@@ -23,6 +23,7 @@ struct ScoredConfig {
   int32_t few_rows = 64;     // bf16: entries of at most this many packed rows go to the kernel for few rows
   int32_t few_chunk = 256;   // smallest key range worth a work item there
   int32_t rows_chunk = 256;  // and in the rows kernels
+  int64_t once_cells = 0;    // few rows that read at least this many cells read them past the caches (0: never)
 };
 
 // May be reused from call to call: planning a batch like the previous one allocates next to nothing.
@@ -31,6 +32,7 @@ struct ScoredPlan {
     int32_t entry, row0, nrows, lo, hi;
   };
   std::vector<Extent> ext;
+  std::vector<int32_t> seg_table;
   std::vector<Tile> few_tiles, row_tiles;
   std::vector<DkEntry> entries;  // pad[0]: the entry's prefix
   std::vector<DkSeg> segs;

@@ -220,6 +220,12 @@ def test_infinities_that_some_rows_see(dtype, d, n, delta):
         assert ok.all(), (i, np.argwhere(~ok)[:4], out[i][~ok][:4], want[~ok][:4])
 
 
+@pytest.mark.parametrize("delta,masks", [([1, 9], dict(cap=5.0)), ([40, 3], dict(window=32990))], ids=["few", "two_blocks"])
+def test_batches_that_no_cache_holds(delta, masks):
+    # 66 thousand cells of 4 KiB: read past the caches
+    Batch(12, 8, 8, 128, "bf16", hist=[33000, 33000], delta=delta).check(**masks)
+
+
 def test_without_changes_it_agrees_with_delta_attend():
     b = Batch(10, 8, 2, 128, "bf16", hist=[500, 30], delta=[40, 3])
     got, lse = b.run(dk.Scores(), False, 0.1)
