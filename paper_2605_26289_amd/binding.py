@@ -417,9 +417,10 @@ class Rotary:
 
 def _heads(t, where: str):
     """(address, elements from token to token) of [tokens, heads, head_dim] rows whose tokens are contiguous"""
-    if t.dim() != 3 or (t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]))):
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 3 or ((strides[2] != 1 or (strides[1] != shape[2] and shape[1] > 1)) and t.numel()):
         raise DeltaKVError(-1, where, "rows are [tokens, heads, head_dim], each token's contiguous")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2])
+    return t.data_ptr(), (strides[0] if shape[0] > 1 else shape[1] * shape[2])
 
 
 def rotate_append(pool, slots, cu_delta, q, k, v, rotary: Rotary, q_out, stream=None) -> None:
