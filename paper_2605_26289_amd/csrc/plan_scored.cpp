@@ -1,6 +1,7 @@
 #include "plan_scored.hpp"
 
 #include <algorithm>
+#include <functional>
 
 #include "plan.hpp"
 
@@ -9,6 +10,15 @@ namespace dk {
 namespace {
 
 typedef ScoredPlan::Tile Tile;
+
+constexpr int64_t FEW_ROUNDS = 3;    // more rounds of workgroups even out by themselves
+constexpr int64_t FIXED_KEYS = 512;  // what starting a work item and merging it cost, in keys
+// Entries of few rows join the rows kernel's launch where there is one, unless they are most of the batch and come from HBM, which
+// the kernel of their own reads faster.  Measured, us, on their own / joined, capped scores (K/V cells of the few; of the row tiles):
+// 12 single tokens on 500-1000 beside 32 tokens (9 thousand; 1) 28.5 / 22.9, one on 6000 beside 128 (6; 24) 52.6 / 41.3, 40 sessions
+// of up to 9 on 4000-8000 beside 512 (240; 96) 285 / 235, 60 on 6000-9000 beside 2 x 512 (450; 240) 481 / 467, beside 256
+// (450; 60) 361 / 375, beside 32 (450; 8) 322 / 357.
+constexpr int64_t JOIN_RATIO = 4;
 
 // The positions that some row of the tile sees.
 void see(const ScoreMasks& masks, const DkEntry& e, int32_t group, const std::vector<int32_t>& first, Tile* t) {
@@ -28,19 +38,70 @@ void see(const ScoreMasks& masks, const DkEntry& e, int32_t group, const std::ve
   t->hi = hi;
 }
 
+struct Pieces {
+  int32_t n;
+  int64_t keys;  // of each (the last may have fewer)
+};
+Pieces pieces_of(int64_t keys, int64_t chunk) {
+  int64_t n = std::max<int64_t>(1, (keys + chunk - 1) / chunk);
+  if (n > 1 && keys - (n - 1) * chunk < chunk / 4) --n;  // no sliver at the end
+  const int64_t each = ((keys + n - 1) / n + 63) / 64 * 64;
+  return {(int32_t)std::max<int64_t>(1, (keys + each - 1) / std::max<int64_t>(each, 1)), each};
+}
+
+// Keys that the busiest of `at_once` workgroups walks if the pieces are taken longest first, a start counted as `fixed` keys.
+int64_t busiest(const std::vector<Tile>& tiles, int64_t chunk, int64_t fixed, int32_t at_once, std::vector<int64_t>* pieces, std::vector<int64_t>* heap) {
+  pieces->clear();
+  for (const Tile& t : tiles) {
+    const Pieces cuts = pieces_of(t.hi - t.lo, chunk);
+    for (int32_t i = 0; i < cuts.n; ++i) pieces->push_back(std::min(cuts.keys, t.hi - t.lo - i * cuts.keys) + fixed);
+  }
+  std::sort(pieces->begin(), pieces->end(), std::greater<int64_t>());
+  heap->assign((size_t)at_once, 0);
+  for (const int64_t k : *pieces) {
+    std::pop_heap(heap->begin(), heap->end(), std::greater<int64_t>());
+    heap->back() += k;
+    std::push_heap(heap->begin(), heap->end(), std::greater<int64_t>());
+  }
+  return *std::max_element(heap->begin(), heap->end());
+}
+
 // Work items of tiles whose workgroups run `at_once` at a time per KV head: key ranges are cut where the longest would outlast an
-// equal share, in pieces of no less than min_chunk; longest first.
+// equal share, in pieces of no less than min_chunk; longest first.  Tiles that can all run at once are cut into the shortest pieces
+// that still do; a few more than that, into the shortest that are done in as many rounds, if the rounds get shorter by more than the
+// cuts cost.
 void cut(const std::vector<Tile>& tiles, int32_t at_once, int32_t min_chunk, ScoredPlan* p, std::vector<DkItem>* items) {
-  int64_t total = 0;
-  for (const Tile& t : tiles) total += t.hi - t.lo;
+  int64_t total = 0, longest = 0;
+  for (const Tile& t : tiles) {
+    total += t.hi - t.lo;
+    longest = std::max<int64_t>(longest, t.hi - t.lo);
+  }
   int64_t chunk = std::max<int64_t>(min_chunk, (total + at_once - 1) / at_once);
   chunk = (chunk + 63) / 64 * 64;
+  const int64_t rounds = ((int64_t)tiles.size() + at_once - 1) / at_once;
+  if (rounds >= 1 && rounds <= FEW_ROUNDS) {
+    const auto fits = [&](int64_t c) {
+      int64_t n = 0;
+      for (const Tile& t : tiles) n += pieces_of(t.hi - t.lo, c).n;
+      return n <= rounds * at_once;
+    };
+    int64_t least = std::max<int64_t>(min_chunk, (total + rounds * at_once - 1) / (rounds * at_once));
+    least = (least + 63) / 64 * 64;
+    int64_t most = std::max(least, (longest + 63) / 64 * 64);
+    while (least < most) {
+      const int64_t mid = (least + most) / 128 * 64;
+      if (fits(mid)) most = mid;
+      else least = mid + 64;
+    }
+    if (rounds == 1 || 10 * busiest(tiles, least, FIXED_KEYS, at_once, &p->scratch[0], &p->scratch[1]) <
+                           9 * busiest(tiles, chunk, FIXED_KEYS, at_once, &p->scratch[0], &p->scratch[1]))
+      chunk = least;
+  }
   for (const Tile& t : tiles) {
     const int64_t keys = t.hi - t.lo;
-    int32_t ns = (int32_t)std::max<int64_t>(1, (keys + chunk - 1) / chunk);
-    if (ns > 1 && keys - (int64_t)(ns - 1) * chunk < chunk / 4) --ns;  // no sliver at the end
-    const int64_t each = ((keys + ns - 1) / ns + 63) / 64 * 64;
-    ns = (int32_t)std::max<int64_t>(1, (keys + each - 1) / std::max<int64_t>(each, 1));
+    const Pieces cuts = pieces_of(keys, chunk);
+    const int32_t ns = cuts.n;
+    const int64_t each = cuts.keys;
     int32_t part0 = -1;
     if (ns > 1) {
       part0 = (int32_t)p->part_rows;
@@ -122,10 +183,16 @@ int32_t build_scored_plan(Pool& pool, const ScoredConfig& cfg, int32_t n_seqs, c
       (few ? p->few_tiles : p->row_tiles).push_back(t);
     }
   }
-  // (64 verifying sessions of 4096 visible keys, 1.08 GB: 210 us through the caches, 190 past them.  What the rows kernel reads
-  // too may be marked as well: it takes no notice.)
-  int64_t cells = 0;
+  int64_t cells = 0, row_cells = 0;
   for (const Tile& t : p->few_tiles) cells += t.hi - t.lo;
+  for (const Tile& t : p->row_tiles) row_cells += t.hi - t.lo;
+  if (!p->row_tiles.empty() && (cells < cfg.once_cells || cells <= JOIN_RATIO * row_cells)) {
+    p->row_tiles.insert(p->row_tiles.end(), p->few_tiles.begin(), p->few_tiles.end());
+    p->few_tiles.clear();
+    p->few_rows = 0;
+    cells = 0;
+  }
+  // (64 verifying sessions of 4096 visible keys, 1.08 GB: 210 us through the caches, 190 past them.)
   if (cells >= cfg.once_cells) mark_unshared(&p->segs, &p->seg_table, cfg.once_cells);
   cut(p->few_tiles, std::max(1, 256 / cfg.n_kv_heads), cfg.few_chunk, p, &p->few);
   cut(p->row_tiles, std::max(1, (cfg.bf16 ? 512 : 256) / cfg.n_kv_heads), cfg.rows_chunk, p, &p->rows);

@@ -33,6 +33,7 @@ struct ScoredPlan {
   };
   std::vector<Extent> ext;
   std::vector<int32_t> seg_table;
+  std::vector<int64_t> scratch[2];
   std::vector<Tile> few_tiles, row_tiles;
   std::vector<DkEntry> entries;  // pad[0]: the entry's prefix
   std::vector<DkSeg> segs;

@@ -114,7 +114,7 @@ def _masks(batch, spec):
     m = dict(spec)
     rng = np.random.default_rng(77)
     if m.get("slopes"):
-        m["slopes"] = SLOPES[:batch.shape[0]]
+        m["slopes"] = (SLOPES * 2)[:batch.shape[0]]
     if m.get("prefix"):
         m["prefix"] = [[0, batch.share + n + new, batch.share + n + 1, 10 ** 9, n // 2][b % 5] for b, (n, new) in enumerate(zip(batch.hist, batch.delta))]
     if m.get("first"):
@@ -220,10 +220,26 @@ def test_infinities_that_some_rows_see(dtype, d, n, delta):
         assert ok.all(), (i, np.argwhere(~ok)[:4], out[i][~ok][:4], want[~ok][:4])
 
 
-@pytest.mark.parametrize("delta,masks", [([1, 9], dict(cap=5.0)), ([40, 3], dict(window=32990))], ids=["few", "two_blocks"])
-def test_batches_that_no_cache_holds(delta, masks):
-    # 66 thousand cells of 4 KiB: read past the caches
-    Batch(12, 8, 8, 128, "bf16", hist=[33000, 33000], delta=delta).check(**masks)
+@pytest.mark.parametrize("staged", [False, True], ids=["appended", "staged"])
+@pytest.mark.parametrize("kind", list(MASKS))
+@pytest.mark.parametrize("most", [4, 9], ids=["one_block", "two_blocks"])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (8, 2, 64), (14, 2, 128)])
+def test_batches_of_few_rows(hq, hkv, d, most, kind, staged):
+    b = Batch(13, hq, hkv, d, "bf16", hist=[0, 1, 130, 63, 1400, 17], delta=[3, 1, most, 0, 1, 4], granule=48, share=70)
+    b.check(staged, **_masks(b, MASKS[kind]))
+
+
+# 66 thousand cells of 4 KiB, read past the caches; in the last batch by a launch of their own beside a prefill chunk's
+@pytest.mark.parametrize("hist,delta,masks", [([33000, 33000], [1, 9], dict(cap=5.0)), ([33000, 33000], [40, 3], dict(window=32990)),
+                                              ([33000, 40, 33000], [5, 90, 3], dict(cap=5.0))], ids=["few", "two_blocks", "chunk"])
+def test_batches_that_no_cache_holds(hist, delta, masks):
+    Batch(12, 8, 8, 128, "bf16", hist=hist, delta=delta).check(**masks)
+
+
+# beside a prefill chunk, short entries are in its launch; more row tiles than run at a time are cut once more
+def test_short_entries_beside_chunks():
+    Batch(14, 32, 1, 64, "bf16", hist=[300, 5, 2000, 0, 900], delta=[40, 1, 2, 270, 1]).check(cap=20.0, window=700)
+    Batch(15, 8, 8, 128, "bf16", hist=[500, 700, 900, 600], delta=[700, 900, 1, 800]).check(cap=20.0)
 
 
 def test_without_changes_it_agrees_with_delta_attend():
