@@ -449,6 +449,9 @@ __global__ __launch_bounds__(256, 2) void scored_rows_kernel(InlineBlob blob, Ct
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int r = 0; r < 16; ++r) next[0][kb][r] = 0.f;
+    // (a wavefront with a cap's exponentials to do goes before one in its second products: 16 capped turns 577 -> 557 us; without a cap
+    // it does not pay, 467 -> 475)
+    if constexpr (CAP && !BIAS) __builtin_amdgcn_s_setprio(1);
     weigh<CAP, BIAS, 2>(sp, rr, slope, tpos, tcnt, h, whole, s[0], m, l, pw[0], rescale, [&](int i) __attribute__((always_inline)) {
       if (16 / N * (i / (16 / N)) != i) return;  // (64-wide heads: every other time)
       const int n = i / (16 / N);
@@ -459,6 +462,7 @@ __global__ __launch_bounds__(256, 2) void scored_rows_kernel(InlineBlob blob, Ct
     });
     ValueFrags<HD, 4> values;
     values.first(v_lds, voff);
+    if constexpr (CAP && !BIAS) __builtin_amdgcn_s_setprio(0);
     values.template products<2, 1>(v_lds, voff, pw, o);
   };
   while (cnt[0] > 0) {
