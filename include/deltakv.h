@@ -261,7 +261,8 @@ int32_t dk_delta_attend_noalloc(dk_pool* pool, int32_t n_seqs, const int32_t* sl
  *   first    HOST int64 [cu_delta[n_seqs]] or NULL, each >= 0: the row of that token sees no position below it (the start of
  *            its document; past the end of the sequence: a padding row that sees nothing)
  * The arrays are read at call time.  Everything else is as in dk_delta_attend, with these differences: scale may be any
- * finite number; lse is that of s''; q, out, k_new and v_new are 16-byte aligned (else DK_ERR_UNSUPPORTED); a call whose
+ * finite number; lse is that of s''; q, out, k_new and v_new are 16-byte aligned (else DK_ERR_UNSUPPORTED) and out
+ * overlaps none of the others (DK_ERR_INVALID); a call whose
  * descriptors do not fit the kernel arguments (about 3 KiB: 48 bytes a sequence, 32 for each of its runs of cells and for
  * each work item, 4 a token where `first` is given) cannot be captured into a graph (DK_ERR_UNSUPPORTED); the workspace is at
  * least dk_scored_workspace_bytes() for the same batch, lengths, mode (staged = 0 or 1) and masks.

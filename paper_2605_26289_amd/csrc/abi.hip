@@ -822,6 +822,16 @@ int32_t dk_last_plan(dk_pool* pool, int64_t* fields_out) {
 
 namespace {
 
+// Memory of n_tok rows.
+struct Span {
+  uintptr_t lo = 0, hi = 0;
+};
+Span span_of(const void* p, int64_t n_tok, int64_t stride, int64_t row, int64_t elem) {
+  if (!p || n_tok <= 0) return {};
+  return {(uintptr_t)p, (uintptr_t)p + (uintptr_t)(((n_tok - 1) * stride + row) * elem)};
+}
+bool overlap(const Span& a, const Span& b) { return a.lo < b.hi && b.lo < a.hi; }
+
 // Masks of a call, if its description is one.
 int32_t score_masks(const dk_scores* scores, dk::ScoreMasks* out) {
   if (!scores || !(scores->cap >= 0.f) || !(scores->cap <= FLT_MAX) || scores->window < 0) return DK_ERR_INVALID;
@@ -872,6 +882,13 @@ int32_t dk_scored_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)k_new | (uintptr_t)v_new) & 15) return DK_ERR_UNSUPPORTED;
     // and a staged one is found by a 24-bit multiplication
     if ((int64_t)pool->desc.n_kv_heads * pool->desc.head_dim * 4 >= (1 << 24)) return DK_ERR_UNSUPPORTED;
+    // (rows of V that are not finite have Q read again when their output has been written once)
+    const int64_t elem = pool->desc.dtype == DK_BF16 ? 2 : 4, q_row = (int64_t)pool->desc.n_q_heads * pool->desc.head_dim,
+                  k_row = (int64_t)pool->desc.n_kv_heads * pool->desc.head_dim;
+    const Span to = span_of(out, plan.total_tokens, q_row, q_row, elem);
+    if (overlap(to, span_of(q, plan.total_tokens, q_row, q_row, elem)) || overlap(to, span_of(k_new, plan.total_tokens, k_row, k_row, elem)) ||
+        overlap(to, span_of(v_new, plan.total_tokens, k_row, k_row, elem)))
+      return DK_ERR_INVALID;
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < (int64_t)plan.total_bytes) return DK_ERR_WORKSPACE;
     const bool inline_blob = plan.blob_bytes <= (size_t)dk::INLINE_BLOB_BYTES;
     // a captured upload would be replayed from a staging buffer that has other descriptors by then
@@ -956,15 +973,6 @@ int32_t rotary_ok(const dk_rotary* r, int32_t head_dim) {
   if (((uintptr_t)r->q_weight | (uintptr_t)r->k_weight) & 15) return DK_ERR_UNSUPPORTED;
   return DK_OK;
 }
-
-struct Span {
-  uintptr_t lo = 0, hi = 0;
-};
-Span span_of(const void* p, int64_t n_tok, int64_t stride, int64_t row, int64_t elem) {
-  if (!p || n_tok <= 0) return {};
-  return {(uintptr_t)p, (uintptr_t)p + (uintptr_t)(((n_tok - 1) * stride + row) * elem)};
-}
-bool overlap(const Span& a, const Span& b) { return a.lo < b.hi && b.lo < a.hi; }
 
 // Checks rows of `heads` heads a token: `in`, strided, and `out`, contiguous.
 int32_t rotary_rows_ok(const void* in, int64_t stride, const void* out, int64_t row, int64_t elem) {

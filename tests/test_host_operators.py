@@ -20,7 +20,7 @@ def _i32(*values):
     return np.asarray(values, dtype=np.int32).tobytes()
 
 
-def _attend(pool, scores, slots=(0,), cu=(0, 2), q=4096, k=None, v=None, scale=1.0, out=8192, ws=1 << 16, ws_bytes=1 << 20):
+def _attend(pool, scores, slots=(0,), cu=(0, 2), q=1 << 40, k=None, v=None, scale=1.0, out=2 << 40, ws=1 << 16, ws_bytes=1 << 20):
     return dk.lib().dk_scored_attend(pool, len(slots), _i32(*slots), _i32(*cu), q, k, v, scale, scores.address if scores else None,
                                      out, None, ws, ws_bytes, None)
 
@@ -64,6 +64,15 @@ def test_scored_attend_refuses_bad_calls(pool):
     assert need > 0 and _attend(pool, s, ws_bytes=need - 1) == -7
     assert dk.seq_len(pool, 0) == 10
     assert _attend(pool, s, cu=(0, 0), q=None, out=None, ws=None) == 0  # no rows
+
+
+def test_scored_attend_refuses_an_output_over_its_inputs(pool):
+    s, row = dk.Scores(cap=30.0), 8 * 64 * 2
+    assert _attend(pool, s, out=1 << 40) == -1 and _attend(pool, s, out=(1 << 40) + 2 * row - 16) == -1
+    new = dict(k=4 << 40, v=5 << 40)
+    for at in new.values():
+        assert _attend(pool, s, out=at, **new) == -1 and _attend(pool, s, out=at - 2 * row + 16, **new) == -1
+    assert _attend(pool, s, out=(1 << 40) + 2 * row, ws=None) == -7  # next to them is fine
 
 
 def test_scored_attend_without_staging_memory_refuses_what_needs_an_upload(pool):
