@@ -340,6 +340,10 @@ struct RowsGeo {
 // the products of tile t + 1 among the instructions of the vector unit, which with capped scores has more to do than the matrix
 // cores: 28 of its cycles for a cap and 16 for the rest against 32 for a score's two products (128-wide heads).
 // K of a tile is requested a step ahead, V two.  Workgroup w: item w / n_kv_heads, KV head w % n_kv_heads.
+// 16 turns of 64 to 512 tokens on 1k to 8k keys, capped, 414 GFLOP: 545 to 572 us, 720 to 760 TFLOP/s (without a cap 460).  No one
+// part of the step bounds it: without the cap's and the weights' exponentials it took 488, without the first or the second products 462
+// and 457, without requests past the first tiles 498.  Weights of 32 keys between both products of their neighbours, in the same
+// registers, took as long; 64 rows per wavefront, one wavefront per SIMD, 707.
 template <int HD, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void scored_rows_kernel(InlineBlob blob, Ctx c, ScoreParams sp) {
   typedef Geo<HD> G;
@@ -512,6 +516,8 @@ struct FewGeo {
 // is requested as soon as K of tile t has been read, V likewise: 16 to 32 KiB in flight per wavefront.  Two row blocks keep their Q
 // in LDS, in the order of the fragments: registers are held to 256 (the bound on occupancy says so), since beyond that the
 // accumulators move to the other half of the register file, and the compiler copies all of them back for every tile.
+// 64 sessions verifying up to 9 tokens over 4096 visible keys each, 1.08 GB: 187 us with a cap, 179 without, 5.8 and 6.0 TB/s.
+// One token on 3000 keys of 8 heads: 7.4 us, and 3.4 for the merge.
 template <int HD, int RB, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void scored_few_kernel(InlineBlob blob, Ctx c, ScoreParams sp) {
   typedef Geo<HD> G;

@@ -21,8 +21,10 @@ struct ScoredConfig {
   int32_t n_q_heads = 0, n_kv_heads = 0, head_dim = 0;
   bool bf16 = true;
   int32_t few_rows = 64;     // bf16: entries of at most this many packed rows go to the kernel for few rows
-  int32_t few_chunk = 256;   // smallest key range worth a work item there
-  int32_t rows_chunk = 256;  // and in the rows kernels
+  // Smallest key range worth a work item there, and in the rows kernels.  Measured, us, 128 / 256 / 512: one fp32 token on 5000 cached
+  // 17.4 / 17.2 / 21.7, nine on 1000 13.2 / 15.2 / 20.8, short fp32 documents 32.8 / 31.4 / 29.8; one bf16 token on 3000 12.9 / 12.2 / -.
+  int32_t few_chunk = 256;
+  int32_t rows_chunk = 256;
   int64_t once_cells = 0;    // few rows that read at least this many cells read them past the caches (0: never)
 };
 

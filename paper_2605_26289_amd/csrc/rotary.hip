@@ -8,8 +8,9 @@
 // token's heads, HEADS of them per workgroup, several requested at a time.  Angles are products in fp64, reduced to a part of a turn
 // there: a position of 2^30 times a frequency leaves 2^-23 turns in fp64 and nothing in fp32.
 // Bound by HBM: every element is read once and written once; an append of 8192 tokens of 32 + 2 x 8 heads of 128 in bf16, 201 MB,
-// takes 35.2 us, 5.7 TB/s (a copy of 2 GiB on the same card 4.9; one wavefront per head, as it was first, 178 us; loads past the
-// caches 41.9, stores past them 35.1).
+// takes 35.2 us, 5.7 TB/s, where the Infinity Cache has the rows and 48.6 us, 4.1 TB/s, where it has not (a copy of 2 GiB on the same
+// card 4.9 TB/s; one wavefront per head, as it was first, 178 us).  Loads past the caches 41.9 and 47.6, stores past them 35.1 and 46.3:
+// the rows come from the projection just before and go to the attention just behind, so both go through the caches.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
