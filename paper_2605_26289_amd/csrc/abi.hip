@@ -955,6 +955,11 @@ int32_t dk_scored_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     items.merges = (const DkMerge*)(desc + plan.off_merges);
     items.n_merges = (int32_t)plan.merges.size();
     items.merge_rows = plan.merge_rows;
+    // (a captured launch may be replayed beside later calls of this pool, or after it is gone: it does not count)
+    if (plan.merges_inside && pool->arrival_slice >= 0 && !capturing(st)) {
+      sp.arrival_slice = pool->arrival_slice;
+      items.n_merges = 0;
+    }
     const hipError_t e = dk::launch_attend_scored(a, sp, items, st);
     return e == hipSuccess ? DK_OK : pool->hip_fail(e);
   });

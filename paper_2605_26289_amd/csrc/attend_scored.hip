@@ -253,7 +253,7 @@ __device__ __forceinline__ void redo_scored(const Ctx& c, const ScoreParams& sp,
     for (int r = 0; r < 4; ++r) x[r] = with_non_finite(o[4 * i + r], odd[0][4 * i + r], odd[1][4 * i + r], odd[2][4 * i + r]);
     const int depth = 32 * db + 8 * i + 4 * h;
     if (it.part_row0 >= 0) {
-      *(f32x4*)(c.parts + ((int64_t)(it.part_row0 + rl0 + col) * c.n_kv_heads + g) * HD + depth) = x;
+      store_for_others((f32x4*)(c.parts + ((int64_t)(it.part_row0 + rl0 + col) * c.n_kv_heads + g) * HD + depth), x);
     } else {
       bf16x4 y;
 #pragma unroll
@@ -499,6 +499,9 @@ __global__ __launch_bounds__(256, 2) void scored_rows_kernel(InlineBlob blob, Ct
 
 namespace {
 
+// Arrival counters, as those of the streaming kernel: zero whenever no kernel that uses them runs.
+__device__ uint32_t g_scored_arrivals[ARRIVAL_SLICES * ARRIVALS_PER_SLICE];
+
 template <int HD>
 struct FewGeo {
   static constexpr int KT = 8192 / Geo<HD>::ROW;  // keys per tile: 8 KiB of K, 8 KiB of V
@@ -517,7 +520,7 @@ struct FewGeo {
 // in LDS, in the order of the fragments: registers are held to 256 (the bound on occupancy says so), since beyond that the
 // accumulators move to the other half of the register file, and the compiler copies all of them back for every tile.
 // 64 sessions verifying up to 9 tokens over 4096 visible keys each, 1.08 GB: 187 us with a cap, 179 without, 5.8 and 6.0 TB/s.
-// One token on 3000 keys of 8 heads: 7.4 us, and 3.4 for the merge.
+// One token on 3000 keys of 8 heads: 10.6 us a call, the merge inside (with a launch for it 12.2: 7.4 us and 3.4).
 template <int HD, int RB, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void scored_few_kernel(InlineBlob blob, Ctx c, ScoreParams sp) {
   typedef Geo<HD> G;
@@ -679,6 +682,7 @@ __global__ __launch_bounds__(256, 2) void scored_few_kernel(InlineBlob blob, Ctx
   const int quad0 = wave * NQ;
   uint32_t bad[RB];
   float mm[RB], lsum[RB];
+  const bool merges = RB == 1 && sp.arrival_slice >= 0 && it.merge != 0;  // see merge_if_last
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     const float lt = l[rb] + __shfl_xor(l[rb], 32);
@@ -710,9 +714,9 @@ __global__ __launch_bounds__(256, 2) void scored_few_kernel(InlineBlob blob, Ctx
 #pragma unroll
       for (int i = 0; i < NQ; ++i) acc[i] += f * xo[(w * 4 * G::DB + quad0 + i) * 64 + lane];
     }
-    store_quads<HD, true>(c, e, it, g, rb * 32 + (lane & 31), quad0 * 8 + 4 * h, acc, lsum[rb] == 0.f ? 1.f : lsum[rb]);
+    store_quads<HD, true>(c, e, it, g, rb * 32 + (lane & 31), quad0 * 8 + 4 * h, acc, lsum[rb] == 0.f ? 1.f : lsum[rb], merges);
     const float lt1[1] = {lsum[rb]}, m1[1] = {mm[rb]};
-    if (wave == 0) store_ml<1, true>(c, e, it, g, rb * 32, lane, m1, lt1);
+    if (wave == 0) store_ml<1, true>(c, e, it, g, rb * 32, lane, m1, lt1, merges);
     float z = 0.f;
 #pragma unroll
     for (int i = 0; i < NQ; ++i)
@@ -726,6 +730,10 @@ __global__ __launch_bounds__(256, 2) void scored_few_kernel(InlineBlob blob, Ctx
     if (which != 0)
       redo_scored<HD, CAP, BIAS>(c, sp, first, e, it, g, rb * 32, which, rb == 0 ? mm[0] : mm[RB - 1], rb == 0 ? lsum[0] : lsum[RB - 1], lane,
                                  quad0 / 4, quad0 % 4, NQ);
+  }
+  if constexpr (RB == 1) {
+    if (merges)
+      merge_if_last<HD, true, true>(c, e, it, g, g_scored_arrivals + sp.arrival_slice * ARRIVALS_PER_SLICE, smem, F::ML_OFFSET);
   }
 }
 

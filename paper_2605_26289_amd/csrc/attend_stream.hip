@@ -447,87 +447,6 @@ __device__ __forceinline__ void lds_barrier() {
 // Arrival counters: zero whenever no kernel that uses them runs (the last arrival takes its counter back to zero).
 __device__ uint32_t g_arrivals[ARRIVAL_SLICES * ARRIVALS_PER_SLICE];
 
-// Split rows of a small batch, merged by the workgroup that finishes the last of the splits (every workgroup has one unit):
-// a merge launch costs the stream 5 us and the host 4 more, of 14 and 16 for one decoding session on 3000 tokens.  The
-// partial rows were written by workgroups on other XCDs, whose L2 is not this one's: they are stored through to memory and
-// loaded from there (agent scope, see store_for_others), every wavefront waits until its own stores have arrived, the workgroup
-// meets, and one lane counts.  The last one to count merges.  Nobody waits for anybody: a workgroup that is not the last one
-// ends.  (With ordinary stores, the count a release that writes the L2 back and an acquire that invalidates the caches, the one
-// session's step took 11.2 us instead of 10.2.)
-// D / 4 lanes take a row; with few rows the splits of one row are spread over several lane groups, whose sums meet in LDS.
-// The order of the additions depends on the plan alone, not on who comes last.
-template <int HD, bool GEN>
-__device__ __forceinline__ void merge_if_last(const Ctx& c, const DkEntry& e, const DkItem& it, int g, uint32_t* arrivals,
-                                              char* smem) {
-  constexpr int LANES = HD / 4, GROUPS = 256 / LANES, AHEAD = 8;
-  const int nsplit = it.merge & 255;
-  uint32_t* counter = arrivals + (it.merge >> 8) * c.n_kv_heads + g;
-  uint32_t* seen = (uint32_t*)(smem + STREAM_NEXT_OFFSET);
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    const uint32_t before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    *seen = before;
-    if (before == (uint32_t)nsplit - 1) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  __syncthreads();
-  if (*seen != (uint32_t)nsplit - 1) return;
-
-  int spread = 1;  // lane groups per row
-  while (2 * spread * it.nrows <= GROUPS) spread *= 2;
-  const int lane = threadIdx.x % LANES, grp = threadIdx.x / LANES;
-  const int first = grp % spread;
-  f32x4* xo = (f32x4*)smem;                       // [lane group][lane]
-  float2* xml = (float2*)(smem + 256 * 16);       // [lane group]
-  const int64_t srow = (int64_t)it.nrows * c.n_kv_heads;  // partial rows from one split of a row to the next
-  for (int r0 = 0; r0 < it.nrows; r0 += GROUPS / spread) {
-    const int rl = r0 + grp / spread;
-    const int64_t prow = (int64_t)(it.part_base + min(rl, it.nrows - 1)) * c.n_kv_heads + g;
-    const f32x4* p = (const f32x4*)(c.parts + prow * HD) + lane;
-    const float2* ml = (const float2*)c.parts_ml + prow;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    float l = 0.f, m = -INFINITY;
-    const auto add = [&](float wm, float wl, const f32x4& v) {
-      const float mn = fmaxf(m, wm);
-      const float ms = (mn == -INFINITY) ? 0.f : mn;
-      const float a = __builtin_amdgcn_exp2f(m - ms), f = __builtin_amdgcn_exp2f(wm - ms);
-      m = mn;
-      l = l * a + f * wl;
-      acc = acc * a + f * v;
-    };
-    for (int s0 = first; s0 < nsplit; s0 += spread * AHEAD) {
-      f32x4 v[AHEAD];
-      float2 w[AHEAD];
-#pragma unroll
-      for (int k = 0; k < AHEAD; ++k) {  // (a split past the end repeats the last one and is left out below)
-        const int64_t at = min(s0 + k * spread, nsplit - 1) * srow;
-        w[k] = load_of_others(ml + at);
-        v[k] = load_of_others(p + at * LANES);
-      }
-#pragma unroll
-      for (int k = 0; k < AHEAD; ++k)
-        if (s0 + k * spread < nsplit) add(w[k].x, w[k].y, v[k]);
-    }
-    if (spread > 1) {  // (one round: the rows fit the lane groups)
-      xo[threadIdx.x] = acc;
-      if (lane == 0) xml[grp] = make_float2(m, l);
-      __syncthreads();
-      if (first == 0)
-        for (int k = 1; k < spread; ++k) add(xml[grp + k].x, xml[grp + k].y, xo[threadIdx.x + k * LANES]);
-    }
-    if (first != 0 || rl >= it.nrows) continue;
-    const int row = it.row0 + rl;
-    const int tok = row_token<GEN>(c, row);
-    const int64_t orow = (int64_t)(e.tok0 + tok) * c.n_q_heads + g * c.group + row_head<GEN>(c, row, tok);
-    const float inv = 1.f / l;
-    bf16x4 o;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) o[u] = (__bf16)(acc[u] * inv);
-    *(bf16x4*)(c.out + orow * HD + lane * 4) = o;
-    if (c.lse && lane == 0) c.lse[orow] = (m + log2f(l)) * 0.6931471805599453f;
-  }
-}
-
 // What a workgroup does whose units have at most MB 32-row blocks.
 // SINGLE: it has one unit and ends.  (A form of its own, because around a loop over units the compiler makes all of the
 // loop's constants first: 1230 instructions in front of the first product instead of 850.  One 150-token turn on 800 cached
@@ -882,7 +801,7 @@ __device__ __forceinline__ void stream_units(const Ctx& c, const int32_t* links,
     e = next_e;
     g = next_g;
   }
-  if (SINGLE && arrival_slice >= 0 && it.merge != 0) merge_if_last<HD, GEN>(c, e, it, g, g_arrivals + arrival_slice * ARRIVALS_PER_SLICE, smem);
+  if (SINGLE && arrival_slice >= 0 && it.merge != 0) merge_if_last<HD, GEN, false>(c, e, it, g, g_arrivals + arrival_slice * ARRIVALS_PER_SLICE, smem, STREAM_NEXT_OFFSET);
 }
 
 // INLINE: the descriptors arrive inside the kernel arguments (first argument) and the descriptor pointers are byte

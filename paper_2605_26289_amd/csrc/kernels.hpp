@@ -121,6 +121,7 @@ struct ScoreParams {
   int32_t window = 0;             // > 0: a row sees its own position and window - 1 before it
   const float* slopes = nullptr;  // [n_q_heads]: bias by distance
   const int32_t* first = nullptr;  // with has_first (a descriptor): [tokens], first position that the row sees
+  int32_t arrival_slice = -1;      // >= 0: the kernel for few rows merges split rows itself, with this slice of its counters
 };
 // Work items by kernel (descriptors).
 struct ScoredItems {

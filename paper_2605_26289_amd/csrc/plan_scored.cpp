@@ -19,6 +19,9 @@ constexpr int64_t FIXED_KEYS = 512;  // what starting a work item and merging it
 // of up to 9 on 4000-8000 beside 512 (240; 96) 285 / 235, 60 on 6000-9000 beside 2 x 512 (450; 240) 481 / 467, beside 256
 // (450; 60) 361 / 375, beside 32 (450; 8) 322 / 357.
 constexpr int64_t JOIN_RATIO = 4;
+// Most rows, and partial rows, of a merge by the last workgroup of its splits.  Merge launch / inside, us: one token on 3000 cached
+// 12.2 / 10.6, on 600 11.5 / 9.9, with 64-wide heads 10.3 / 9.3, with two KV heads 11.2 / 9.8, four tokens on 2000 each 12.3 / 11.7.
+constexpr int32_t INSIDE_ROWS = 8, INSIDE_PARTS = 64;
 
 // The positions that some row of the tile sees.
 void see(const ScoreMasks& masks, const DkEntry& e, int32_t group, const std::vector<int32_t>& first, Tile* t) {
@@ -117,6 +120,10 @@ void cut(const std::vector<Tile>& tiles, int32_t at_once, int32_t min_chunk, Sco
       it.kv_lo = t.lo + (int32_t)(sp * each);
       it.kv_hi = sp + 1 == ns ? t.hi : t.lo + (int32_t)((sp + 1) * each);
       it.part_row0 = ns > 1 ? part0 + sp * t.nrows : -1;
+      if (ns > 1 && ns < 256 && p->merges.size() <= 256) {
+        it.merge = 256 * (int32_t)(p->merges.size() - 1) + ns;
+        it.part_base = part0;
+      }
       items->push_back(it);
     }
   }
@@ -196,6 +203,11 @@ int32_t build_scored_plan(Pool& pool, const ScoredConfig& cfg, int32_t n_seqs, c
   if (cells >= cfg.once_cells) mark_unshared(&p->segs, &p->seg_table, cfg.once_cells);
   cut(p->few_tiles, std::max(1, 256 / cfg.n_kv_heads), cfg.few_chunk, p, &p->few);
   cut(p->row_tiles, std::max(1, (cfg.bf16 ? 512 : 256) / cfg.n_kv_heads), cfg.rows_chunk, p, &p->rows);
+  // Merging inside the kernel for few rows, under the streaming kernel's conditions (see merges_inside there).
+  // (Its form for more than 32 rows does not.)
+  p->merges_inside = p->rows.empty() && p->few_rows <= 32 && !p->merges.empty() &&
+                     p->merges.size() * (size_t)cfg.n_kv_heads <= (size_t)ARRIVALS_PER_SLICE;
+  for (const DkMerge& m : p->merges) p->merges_inside &= m.nrows <= INSIDE_ROWS && m.nsplit * m.nrows <= INSIDE_PARTS && m.nsplit < 256;
   const auto section = [](size_t& at, size_t bytes) {
     const size_t off = at;
     at = (at + bytes + 15) / 16 * 16;

@@ -44,6 +44,7 @@ struct ScoredPlan {
   std::vector<DkMerge> merges;
   int64_t total_tokens = 0, part_rows = 0;
   int32_t few_rows = 0, tile_rows = 0, merge_rows = 0;  // most rows of an item, of a merge
+  bool merges_inside = false;                           // the kernel for few rows can merge all of them itself
   size_t off_entries = 0, off_segs = 0, off_first = 0, off_few = 0, off_rows = 0, off_merges = 0;
   size_t blob_bytes = 0, off_parts = 0, total_bytes = 0;
 };

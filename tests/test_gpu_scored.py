@@ -242,6 +242,41 @@ def test_short_entries_beside_chunks():
     Batch(15, 8, 8, 128, "bf16", hist=[500, 700, 900, 600], delta=[700, 900, 1, 800]).check(cap=20.0)
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (8, 2, 64), (3, 3, 128)])
+def test_few_rows_over_long_caches_are_merged_again_and_again(hq, hkv, d):
+    """Split rows, some without a visible key, merged by the last workgroup of their splits: every call, with others in between."""
+    b = Batch(16, hq, hkv, d, "bf16", hist=[5000, 900, 3], delta=[2, 1, 1])
+    first = [0, 2 ** 40, 600, 0]
+    want = b.check(cap=20.0, first=first)
+    s = dk.Scores(cap=20.0, first=first)
+    q, ones = _dev(b.q, "bf16"), [slice(0, 2), slice(2, 3), slice(3, 4)]
+    for i in range(6):
+        for j, r in enumerate(ones):  # alone each is cut more finely: as exact, not the same bits
+            got = b.pool.scored_attend([b.slots[j]], [0, r.stop - r.start], q[r], d ** -0.5, dk.Scores(cap=20.0, first=first[r]))
+            assert np.allclose(got.float().cpu().numpy(), want[r], rtol=2.0 ** -6, atol=2.0 ** -6)
+        again = b.pool.scored_attend(b.slots, b.cu, q, d ** -0.5, s)
+        assert np.array_equal(again.float().cpu().numpy(), want), i
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64)])
+def test_infinities_in_a_long_cache(dtype, d):
+    """One infinity and one NaN of V in different pieces of a long cache that a single token sees."""
+    n = 3000
+    b = Batch(17, 4, 2, d, dtype, hist=[n], delta=[1])
+    clean = b.v[0].copy()
+    b.v[0][200, 0, 5], b.v[0][2500, 1, 9] = -INF, NAN
+    b.pool.trim(b.slots[0], 0)
+    b.pool.append([b.slots[0]], [0, n], _dev(b.k[0][:n], dtype), _dev(b.v[0][:n], dtype))
+    out, _ = b.run(dk.Scores(cap=9.0), False, 0.2)
+    ref = oracle.scored_attend(b.q, b.k[0], clean, n, 0.2, 9.0)
+    tol, _ = _bounds(ref, dtype, n + 1, d, 9.0, 0.0)
+    want = ref[0].copy()
+    want[:, :2, 5], want[:, 2:, 9] = -INF, NAN
+    with np.errstate(invalid="ignore"):
+        ok = (out == want) | (np.isnan(out) & np.isnan(want)) | (np.isfinite(want) & (np.abs(out - want) <= tol))
+    assert ok.all(), (np.argwhere(~ok)[:4], out[~ok][:4], want[~ok][:4])
+
+
 def test_without_changes_it_agrees_with_delta_attend():
     b = Batch(10, 8, 2, 128, "bf16", hist=[500, 30], delta=[40, 3])
     got, lse = b.run(dk.Scores(), False, 0.1)
