@@ -236,6 +236,13 @@ def test_batches_that_no_cache_holds(hist, delta, masks):
     Batch(12, 8, 8, 128, "bf16", hist=hist, delta=delta).check(**masks)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kind", ["cap", "all", "first"])
+def test_many_rows_in_fp32(d, kind):
+    b = Batch(18, 16, 4, d, "f32", hist=[60, 200], delta=[330, 320])  # 328 items of 32 rows
+    b.check(True, **_masks(b, MASKS[kind]))
+
+
 # beside a prefill chunk, short entries are in its launch; more row tiles than run at a time are cut once more
 def test_short_entries_beside_chunks():
     Batch(14, 32, 1, 64, "bf16", hist=[300, 5, 2000, 0, 900], delta=[40, 1, 2, 270, 1]).check(cap=20.0, window=700)
