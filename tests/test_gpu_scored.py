@@ -340,6 +340,33 @@ def test_captured_and_replayed_beside_other_work():
         assert np.array_equal(out.float().cpu().numpy(), want) and not torch.equal(out, other)
 
 
+def test_two_graphs_share_a_workspace():
+    b = Batch(19, 8, 2, 128, "bf16", hist=[4000, 2500], delta=[1, 12])
+    calls = [(0, slice(0, 1), dk.Scores(cap=25.0)), (1, slice(1, 13), dk.Scores(window=2000))]
+    kn, vn = b.new(b.k), b.new(b.v)
+    b.pool.append(b.slots, b.cu, kn, vn)
+    q = _dev(b.q, "bf16")
+    graphs, outs, want = [], [], []
+    for j, r, s in calls:  # (eager once: the workspace is as large as it gets)
+        want.append(b.pool.scored_attend([b.slots[j]], [0, r.stop - r.start], q[r].clone(), 0.1, s))
+    torch.cuda.synchronize()
+    for j, r, s in calls:
+        rows = q[r].clone()
+        outs.append(torch.zeros_like(rows))
+        graphs.append((torch.cuda.CUDAGraph(), rows))
+        with torch.cuda.graph(graphs[-1][0], stream=torch.cuda.Stream()):
+            b.pool.scored_attend([b.slots[j]], [0, r.stop - r.start], rows, 0.1, s, out=outs[-1])
+    for order in ((0, 1), (1, 0), (0, 0, 1), (1, 1, 0)):
+        for o in outs:
+            o.zero_()
+        for g in order:
+            graphs[g][0].replay()
+        eager = b.pool.scored_attend([b.slots[0]], [0, 1], q[:1].clone(), 0.1, calls[0][2])
+        torch.cuda.synchronize()
+        for got, ref in zip(outs + [eager], want + [want[0]]):  # merged by a launch or inside: the same sums in another order
+            assert torch.allclose(got.float(), ref.float(), rtol=2.0 ** -7, atol=1e-6), order
+
+
 def test_a_call_that_needs_an_upload_is_not_captured():
     hist = [20] * 100
     b = Batch(14, 4, 1, 64, "bf16", hist=hist, delta=[1] * 100)
