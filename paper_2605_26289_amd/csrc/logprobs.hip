@@ -373,24 +373,27 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_finish_kernel(Logpr
   const float c = a.scale * LOG2E;
   const Part* mine = parts + (int64_t)row * n_chunks;
   const Pick* top = tops + (int64_t)row * n_chunks * a.n_top;
+  // (the thread's first chunk, asked for before all else: rows seldom have more chunks than threads)
+  const Part own = tid < n_chunks ? mine[tid] : Part{-INFINITY, 0.f, 0.f, 0};
   if constexpr (TOP)
     for (int k = tid; k < n_chunks + 8; k += threads) heads[k] = k < n_chunks ? top[(int64_t)k * a.n_top] : 0;
   const int32_t token = a.tokens ? a.tokens[row] : -1;
   const bool given = token >= 0 && token < a.vocab;
   const int64_t at = (int64_t)row * a.row_stride + (given ? token : 0);
   const float x = a.dtype == 1 ? logit_at((const uint16_t*)a.logits, at) : logit_at((const float*)a.logits, at);
-  float m = -INFINITY;
-  for (int k = tid; k < n_chunks; k += threads) m = fmaxf(m, mine[k].m);
+  float m = own.m;
+  for (int k = tid + threads; k < n_chunks; k += threads) m = fmaxf(m, mine[k].m);
   m = block_fold(m, fbuf, [](float p, float q) { return fmaxf(p, q); });
   float s0 = 0.f, s1 = 0.f;
   int32_t above = 0;
-  for (int k = tid; k < n_chunks; k += threads) {
-    const Part o = mine[k];
+  const auto take = [&](const Part& o) {
     const float d = o.m == m ? 0.f : (o.m - m) * c, f = __builtin_amdgcn_exp2f(d);
     s0 += f * o.s0;
     s1 += f * (o.s1 + fmaxf(d, -200.f) * o.s0);
     above += o.above;
-  }
+  };
+  take(own);
+  for (int k = tid + threads; k < n_chunks; k += threads) take(mine[k]);
   const auto add = [](auto p, auto q) { return p + q; };
   s0 = block_fold(s0, fbuf, add);
   s1 = block_fold(s1, fbuf, add);
