@@ -117,9 +117,13 @@ __device__ __forceinline__ void weigh(const ScoreParams& sp, const RowRange& rr,
   float mx = max16(s[0]);
   if constexpr (KB == 2) mx = fmaxf(mx, max16(s[KB - 1]));
   mx = fmaxf(mx, __shfl_xor(mx, 32));
-  if constexpr (!BIAS) {
-    const float t = CAP ? __builtin_fmaf(-2.f * sp.cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(mx * sp.c)), sp.cap) : mx * sp.c;
-    mx = mx == -INFINITY ? mx : t;
+  if constexpr (CAP && !BIAS) {
+    // (A product of -infinity may well be one that the row sees, of score -cap: whether it sees any is a matter of positions.)
+    const bool sees = max(rr.from, tpos) < min(rr.last + 1, tpos + tcnt);
+    const float t = __builtin_fmaf(-2.f * sp.cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(mx * sp.c)), sp.cap);
+    mx = sees ? t : -INFINITY;
+  } else if constexpr (!BIAS) {
+    mx *= sp.c;  // (the scale is positive: -infinity, of a row that sees nothing of the tile, stays what it is)
   }
   if (__builtin_amdgcn_ballot_w64(mx > m + SCORED_RESCALE_SLACK) != 0) {
     const float mn = fmaxf(m, mx);
