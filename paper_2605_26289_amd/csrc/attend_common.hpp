@@ -613,6 +613,12 @@ __device__ __forceinline__ void store_ml(const Ctx& c, const DkEntry& e, const D
   }
 }
 
+// The weight of a piece of a split row in the whole row, for its partial sum: never zero, but fp32's smallest number where there are
+// no digits for it (the piece's largest score is some hundred units below the row's).  An infinity or a NaN of V in the piece then
+// stays what it is, as in a row whose keys are not cut; times zero the infinity would be a NaN.  Finite sums gain at most 2^-149 of
+// the piece's.  (A choice for each element instead: 0.3 us of one token's 10.7.)
+__device__ __forceinline__ float piece_weight(float weight) { return fmaxf(weight, 0x1p-149f); }
+
 // Split rows of a small batch, merged by the workgroup that finishes the last of the splits (every workgroup has one unit):
 // a merge launch costs the stream 5 us and the host 4 more, of 14 and 16 for one decoding session on 3000 tokens.  The
 // partial rows were written by workgroups on other XCDs, whose L2 is not this one's: they are stored through to memory and
@@ -622,7 +628,8 @@ __device__ __forceinline__ void store_ml(const Ctx& c, const DkEntry& e, const D
 // session's step took 11.2 us instead of 10.2.)
 // D / 4 lanes take a row; with few rows the splits of one row are spread over several lane groups, whose sums meet in LDS.
 // The order of the additions depends on the plan alone, not on who comes last.
-// smem: 4 KiB and 256 bytes of LDS, and a word at seen_offset behind them.  EMPTY: there may be rows that no split has a key for.
+// smem: 4 KiB and 256 bytes of LDS, and a word at seen_offset behind them.  EMPTY: of changed scores; there may be rows that no split
+// has a key for, and weights of splits that vanish are ordinary.
 template <int HD, bool GEN, bool EMPTY>
 __device__ __forceinline__ void merge_if_last(const Ctx& c, const DkEntry& e, const DkItem& it, int g, uint32_t* arrivals,
                                               char* smem, int seen_offset) {
@@ -660,7 +667,8 @@ __device__ __forceinline__ void merge_if_last(const Ctx& c, const DkEntry& e, co
       const float a = __builtin_amdgcn_exp2f(m - ms), f = __builtin_amdgcn_exp2f(wm - ms);
       m = mn;
       l = l * a + f * wl;
-      acc = acc * a + f * v;
+      if constexpr (EMPTY) acc = acc * piece_weight(a) + piece_weight(f) * v;
+      else acc = acc * a + f * v;
     };
     for (int s0 = first; s0 < nsplit; s0 += spread * AHEAD) {
       f32x4 v[AHEAD];

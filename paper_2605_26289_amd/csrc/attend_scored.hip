@@ -775,13 +775,13 @@ __global__ __launch_bounds__(256) void scored_merge_kernel(InlineBlob blob, Ctx 
     const float a = __builtin_amdgcn_exp2f(m - ms);
     m = mn;
     l *= a;
-    acc *= a;
+    acc *= piece_weight(a);
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
       if (s0 + k >= mg.nsplit) continue;
       const float f = __builtin_amdgcn_exp2f(ml[k].x - ms);
       l += f * ml[k].y;
-      acc += f * v[k];
+      acc += piece_weight(f) * v[k];
     }
   }
   const int row = mg.row0 + rl;
