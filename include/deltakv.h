@@ -297,7 +297,8 @@ int32_t dk_scored_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
  * dk_rotate_append is dk_kv_append with that: token i of entry b is at position len(slot_b) + i, its Q goes to q_out, its
  *   K -- turned -- and V -- as it is -- into the slot's next cells.  Batch, errors and bookkeeping as for dk_kv_append without
  *   n_accept.  Appends that go to more than 300 runs of consecutive cells upload a table of them through the staging memory
- *   (DK_ERR_BUSY, DK_ERR_WORKSPACE as for dk_kv_append) and cannot be captured into a graph (DK_ERR_UNSUPPORTED).
+ *   (DK_ERR_BUSY, DK_ERR_WORKSPACE as for dk_kv_append) and cannot be captured into a graph (DK_ERR_UNSUPPORTED).  At most
+ *   2^26 tokens a call (DK_ERR_UNSUPPORTED).
  * dk_rotate_rows turns rows at positions given by DEVICE int64 [n_tokens] (negative ones turn back) without a pool: Q and K
  *   for a staged call.  Either head count may be 0 (its pointers are not looked at).  n_tokens < 2^31.  No state.
  * dk_rotary_freqs (HOST) writes the inverse frequencies of a scaled rotation, float [rotary_dim / 2], to be copied to the

@@ -1023,6 +1023,7 @@ int32_t dk_rotate_append(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     }
     const int64_t total = n_seqs > 0 ? cu_delta[n_seqs] : 0;
     if (total == 0) return DK_OK;
+    if (total > dk::ROTARY_MAX_APPEND) return DK_ERR_UNSUPPORTED;
     const int64_t elem = d.dtype == DK_BF16 ? 2 : 4, q_row = (int64_t)d.n_q_heads * d.head_dim, k_row = (int64_t)d.n_kv_heads * d.head_dim;
     if ((rc = rotary_rows_ok(q, q_stride, q_out, q_row, elem)) != DK_OK) return rc;
     if ((rc = rotary_rows_ok(k, k_stride, d.k_arena, k_row, elem)) != DK_OK) return rc;

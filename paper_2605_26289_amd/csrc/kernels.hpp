@@ -166,6 +166,8 @@ hipError_t launch_token_logprobs(const LogprobArgs& a, void* workspace, hipStrea
 // Norms and rotation of Q and K.  Appends carry the runs of consecutive cells and positions that their tokens go to in the
 // kernel arguments, at most this many of them: run r is tokens tok[r] .. tok[r + 1] - 1, from cell[r] and pos[r] on.
 constexpr int32_t ROTARY_INLINE_MAX_RUNS = 300;
+// Most tokens of an append: 2^22 workgroups along the tokens, of 16 at least.
+constexpr int64_t ROTARY_MAX_APPEND = int64_t(1) << 26;
 struct RotaryRuns {
   int32_t tok[ROTARY_INLINE_MAX_RUNS + 1];
   int32_t cell[ROTARY_INLINE_MAX_RUNS];

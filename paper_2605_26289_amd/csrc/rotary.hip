@@ -270,9 +270,10 @@ hipError_t launch_layout(const RotaryArgs& a, const RotaryRuns& runs, int32_t n_
   const int64_t y = (n_heads + per - 1) / per;
   if (y > 65535) return hipErrorInvalidValue;
   constexpr int64_t MOST = int64_t(1) << 22;  // workgroups of a launch along the tokens
+  static_assert(MOST * TOKENS >= ROTARY_MAX_APPEND, "appends, whose places are counted from the launch's first token, take one launch");
+  if (S != ROWS && groups > MOST) return hipErrorInvalidValue;
   for (int64_t g = 0; g < groups; g += MOST) {
     const int64_t some = std::min(MOST, groups - g);
-    if (S == RUNS && g > 0) return hipErrorInvalidValue;  // (2^26 tokens: the host has turned them down)
     rotate_kernel<T, D, L, S><<<dim3((unsigned)some, (unsigned)y), ROT_THREADS, 0, stream>>>(
         runs, n_runs, where, tok_base + g * TOKENS, std::min<int64_t>(n_tok - g * TOKENS, some * TOKENS), a, (int32_t)per);
   }
