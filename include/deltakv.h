@@ -296,8 +296,9 @@ int32_t dk_scored_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
  *               overlap of an output with an input or another output is DK_ERR_INVALID
  * dk_rotate_append is dk_kv_append with that: token i of entry b is at position len(slot_b) + i, its Q goes to q_out, its
  *   K -- turned -- and V -- as it is -- into the slot's next cells.  Batch, errors and bookkeeping as for dk_kv_append without
- *   n_accept.  Appends that go to more than 300 runs of consecutive cells upload a table of them through the staging memory
- *   (DK_ERR_BUSY, DK_ERR_WORKSPACE as for dk_kv_append) and cannot be captured into a graph (DK_ERR_UNSUPPORTED).  At most
+ *   n_accept.  Appends that go to more than 300 runs of consecutive cells upload a table of them, 8 bytes a token, through the
+ *   staging memory and cannot be captured into a graph (DK_ERR_UNSUPPORTED).  The table may take several buffers of it:
+ *   DK_ERR_WORKSPACE if the pool has not as many, DK_ERR_BUSY, with nothing enqueued, while one of them is in flight.  At most
  *   2^26 tokens a call (DK_ERR_UNSUPPORTED).
  * dk_rotate_rows turns rows at positions given by DEVICE int64 [n_tokens] (negative ones turn back) without a pool: Q and K
  *   for a staged call.  Either head count may be 0 (its pointers are not looked at).  n_tokens < 2^31.  No state.

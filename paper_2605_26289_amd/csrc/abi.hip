@@ -152,6 +152,21 @@ struct dk_pool {
     return DK_OK;
   }
 
+  // Whether stage() will give the next n buffers: DK_ERR_BUSY if the upload that last used one of them is under way, DK_ERR_WORKSPACE
+  // if there are not as many.
+  int32_t stages_free(int64_t n) {
+    if (n > ring_size) return DK_ERR_WORKSPACE;
+    for (int k = 0; k < (int)n; ++k) {
+      Staging& s = ring[(ring_next + k) % ring_size];
+      if (!s.in_flight) continue;
+      const hipError_t e = hipEventQuery(s.done);
+      if (e == hipErrorNotReady) return DK_ERR_BUSY;
+      if (e != hipSuccess) return hip_fail(e);
+      s.in_flight = false;
+    }
+    return DK_OK;
+  }
+
   int32_t upload(Staging* s, void* dev, size_t bytes, hipStream_t stream) {
     hipError_t e = hipMemcpyAsync(dev, s->host, bytes, hipMemcpyHostToDevice, stream);
     if (e != hipSuccess) return hip_fail(e);
@@ -1072,6 +1087,9 @@ int32_t dk_rotate_append(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     if (per_launch <= 0) return undo(DK_ERR_WORKSPACE);
     // a captured upload would be replayed from a staging buffer that has other descriptors by then
     if (capturing(st)) return undo(DK_ERR_UNSUPPORTED);
+    // All uploads or none: Q may be turned over itself, and a caller who is told to come again would have its first rows turned twice.
+    rc = pool->stages_free((total + per_launch - 1) / per_launch);
+    if (rc != DK_OK) return undo(rc);
     size_t r = 0;
     int32_t b = 0;
     for (int64_t base = 0; base < total; base += per_launch) {
