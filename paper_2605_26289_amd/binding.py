@@ -180,6 +180,37 @@ def _stream(stream) -> Optional[int]:
     return h or None
 
 
+_DTYPES = None
+
+
+def _dtypes():
+    """(what F32 and BF16 are in torch, int32, int64)"""
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = ((torch.float32, torch.bfloat16), torch.int32, torch.int64)
+    return _DTYPES
+
+
+def _buffer(t, dtype, least: int, device: int, where: str, what: str) -> Optional[int]:
+    """The address of a contiguous tensor of at least `least` elements, on the GPU of the call's other tensors: what the library is
+    handed are bare pointers."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() < least or not t.is_contiguous() or t.get_device() != device or device < 0:
+        raise DeltaKVError(-1, where, f"{what}: {least} or more contiguous elements of {dtype} on the GPU of the others")
+    return t.data_ptr()
+
+
+def _tokens(s_arr, c_arr, where: str) -> int:
+    """New tokens of a batch, whose offsets are one more than its sequences."""
+    if not len(s_arr):
+        return 0
+    if len(c_arr) <= len(s_arr):
+        raise DeltaKVError(-1, where, "cu_delta has one element more than there are sequences")
+    return int(c_arr[len(s_arr)])
+
+
 # --------------------------------------------------------------------------- pool
 def meta_bytes(desc: PoolDesc) -> int:
     out = C.c_int64()
@@ -213,9 +244,16 @@ def staging_wait(pool) -> None:
     _check(lib().dk_staging_wait(pool), "staging_wait", pool)
 
 
-def pool_create(desc: PoolDesc) -> C.c_void_p:
-    out = C.c_void_p()
+class Pool(C.c_void_p):
+    """A pool's handle, with the shape and type that rows of its calls have: (query heads, KV heads, head width, dtype)."""
+
+    shape = None
+
+
+def pool_create(desc: PoolDesc) -> Pool:
+    out = Pool()
     _check(lib().dk_pool_create(C.byref(desc), C.byref(out)), "pool_create")
+    out.shape = (desc.n_q_heads, desc.n_kv_heads, desc.head_dim, desc.dtype)
     return out
 
 
@@ -365,6 +403,10 @@ class Scores:
     slopes: float32 device tensor, one per query head; prefix: one position per sequence; first: one per new token."""
 
     def __init__(self, cap: float = 0.0, slopes=None, window: int = 0, prefix=None, first=None):
+        if slopes is not None and (slopes.dtype is not _dtypes()[0][F32] or not slopes.is_contiguous()):
+            raise DeltaKVError(-1, "scores", "slopes are contiguous float32")
+        if not -1 << 31 <= window < 1 << 31:
+            raise DeltaKVError(-1, "scores", "a window is an int32")
         self.slopes = slopes
         self.prefix = None if prefix is None else np.ascontiguousarray(prefix, dtype=np.int64)
         self.first = None if first is None else np.ascontiguousarray(first, dtype=np.int64)
@@ -382,7 +424,7 @@ class Scores:
 def scored_workspace_bytes(pool, slots, cu_delta, staged, scores: Scores) -> int:
     s_arr, s_p = _array(slots)
     c_arr, c_p = _array(cu_delta)
-    scores.check(len(s_arr), int(c_arr[-1]) if len(s_arr) else 0)
+    scores.check(len(s_arr), _tokens(s_arr, c_arr, "scored_workspace_bytes"))
     out = C.c_int64()
     _check(lib().dk_scored_workspace_bytes(pool, len(s_arr), s_p, c_p, int(staged), scores.address, C.byref(out)),
            "scored_workspace_bytes", pool)
@@ -391,13 +433,23 @@ def scored_workspace_bytes(pool, slots, cu_delta, staged, scores: Scores) -> int
 
 def scored_attend(pool, slots, cu_delta, q, out, scale: float, scores: Scores, k_new=None, v_new=None, lse=None,
                   workspace=None, stream=None) -> None:
+    """Rows are contiguous and of the pool's type: q, out [tokens, query heads, head_dim], k_new, v_new [tokens, KV heads, head_dim]."""
+    where = "scored_attend"
     s_arr, s_p = _array(slots)
     c_arr, c_p = _array(cu_delta)
-    scores.check(len(s_arr), int(c_arr[-1]) if len(s_arr) else 0, q.shape[1])
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _launch(lib().dk_scored_attend, (pool, len(s_arr), s_p, c_p, _ptr(q), _ptr(k_new), _ptr(v_new), float(scale),
-                                     scores.address, _ptr(out), _ptr(lse), _ptr(workspace), ws_bytes, _stream(stream)),
-            "scored_attend", pool)
+    n = _tokens(s_arr, c_arr, where)
+    hq, hkv, d, code = pool.shape
+    scores.check(len(s_arr), n, hq)
+    kind, dev = _dtypes()[0], q.get_device()
+    if scores.slopes is not None and scores.slopes.get_device() != dev:
+        raise DeltaKVError(-1, where, "slopes are on the GPU of the others")
+    args = [pool, len(s_arr), s_p, c_p, _buffer(q, kind[code], n * hq * d, dev, where, "q"),
+            _buffer(k_new, kind[code], n * hkv * d, dev, where, "k_new"), _buffer(v_new, kind[code], n * hkv * d, dev, where, "v_new"),
+            float(scale), scores.address, _buffer(out, kind[code], n * hq * d, dev, where, "out"),
+            _buffer(lse, kind[F32], n * hq, dev, where, "lse"), None, 0, _stream(stream)]
+    if workspace is not None:
+        args[11:13] = _buffer(workspace, workspace.dtype, 0, dev, where, "workspace"), workspace.numel() * workspace.element_size()
+    _launch(lib().dk_scored_attend, args, where, pool)
 
 
 class Rotary:

@@ -3,6 +3,7 @@
 Nothing here launches: every call is turned down before it would."""
 import numpy as np
 import pytest
+import torch
 
 from paper_2605_26289_amd import binding as dk
 
@@ -23,3 +24,76 @@ def test_rotate_append_refuses_more_tokens_than_a_launch_holds(d):
         assert rc == -6
         assert dk.pool_stats(pool) == held and all(dk.seq_len(pool, s) == 0 for s in slots)
     dk.pool_destroy(pool)
+
+
+class OnGpu(torch.Tensor):
+    """Host memory that says it is on a GPU: what the binding would hand on goes to `calls`, not to the library."""
+
+    gpu = 0
+
+    def get_device(self):
+        return self.gpu
+
+
+def _gpu(*shape, dtype=torch.bfloat16, at=0):
+    t = torch.zeros(shape, dtype=dtype).as_subclass(OnGpu)
+    t.gpu = at
+    return t
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    made = []
+    monkeypatch.setattr(dk, "_launch", lambda call, args, where, pool: made.append(args))
+    return made
+
+
+@pytest.fixture
+def pool():
+    p = dk.pool_create(dk.PoolDesc(4, 0, 4096, 16, 8, 2, 64, dk.BF16, 256 * 10, 256 * 20, 256 * 30, 1 << 20))
+    yield p
+    dk.pool_destroy(p)
+
+
+def _refused(call, **kw):
+    with pytest.raises(dk.DeltaKVError) as e:
+        call(**kw)
+    assert e.value.status == -1
+
+
+F32, BF16, I32, I64 = torch.float32, torch.bfloat16, torch.int32, torch.int64
+
+
+def test_scores_are_of_their_types():
+    dk.Scores(slopes=_gpu(8, dtype=F32))
+    for slopes in (_gpu(8), _gpu(8, dtype=torch.float64), _gpu(16, dtype=F32)[::2]):
+        _refused(dk.Scores, slopes=slopes)
+    for window in (1 << 31, 1 << 32, -(1 << 40)):  # (an int32 argument would take the lower half)
+        _refused(dk.Scores, window=window)
+
+
+def test_scored_attend_takes_rows_as_the_pool_has_them(pool, calls):
+    def call(q=_gpu(5, 8, 64), out=_gpu(5, 8, 64), slopes=None, cu=(0, 2, 5), **kw):
+        dk.scored_attend(pool, [0, 1], cu, q, out, 1.0, dk.Scores(slopes=slopes), stream=0, **kw)
+
+    new = dict(k_new=_gpu(5, 2, 64), v_new=_gpu(5, 2, 64))
+    call()
+    call(slopes=_gpu(8, dtype=F32), lse=_gpu(5, 8, dtype=F32), workspace=_gpu(1 << 12, dtype=torch.uint8), **new)
+    call(q=_gpu(7, 8, 64), out=_gpu(6, 512))  # rows behind the batch's
+    assert len(calls) == 3 and calls[1][12] == 1 << 12
+    fused = _gpu(5, 12, 64)
+    for q in (_gpu(4, 8, 64), _gpu(5, 8, 64, dtype=F32), _gpu(5, 8, 64, dtype=torch.float16), fused[:, :8], _gpu(8, 5, 64).transpose(0, 1),
+              torch.zeros((5, 8, 64), dtype=BF16)):
+        _refused(call, q=q)
+        _refused(call, out=q)
+    for k in (_gpu(5, 1, 64), _gpu(5, 2, 64, dtype=F32), fused[:, 8:10], _gpu(5, 2, 64, at=1)):
+        _refused(call, **{**new, "k_new": k})
+        _refused(call, **{**new, "v_new": k})
+    for lse in (_gpu(5, 8), _gpu(4, 8, dtype=F32), torch.zeros((5, 8))):
+        _refused(call, lse=lse)
+    _refused(call, slopes=_gpu(7, dtype=F32))
+    _refused(call, slopes=torch.zeros(8))
+    _refused(call, workspace=torch.zeros(1 << 12, dtype=torch.uint8))
+    _refused(call, cu=(0, 5))  # offsets of one sequence for two
+    _refused(dk.scored_workspace_bytes, pool=pool, slots=[0, 1], cu_delta=[0, 5], staged=False, scores=dk.Scores())
+    assert len(calls) == 3
