@@ -204,11 +204,22 @@ def _buffer(t, dtype, least: int, device: int, where: str, what: str) -> Optiona
 
 def _tokens(s_arr, c_arr, where: str) -> int:
     """New tokens of a batch, whose offsets are one more than its sequences."""
-    if not len(s_arr):
+    n = len(s_arr)
+    if not n:
         return 0
-    if len(c_arr) <= len(s_arr):
+    if len(c_arr) <= n:
         raise DeltaKVError(-1, where, "cu_delta has one element more than there are sequences")
-    return int(c_arr[len(s_arr)])
+    return c_arr.item(n)
+
+
+def _stream_on(device: int, stream, where: str) -> Optional[int]:
+    """The stream of a call whose tensors are on that GPU: work goes to the current one."""
+    if stream is not None:
+        return _stream(stream)
+    import torch
+    if torch._C._cuda_getDevice() != device:
+        raise DeltaKVError(-1, where, "the tensors are not on the current GPU")
+    return torch._C._cuda_getCurrentRawStream(device) or None
 
 
 # --------------------------------------------------------------------------- pool
@@ -446,7 +457,7 @@ def scored_attend(pool, slots, cu_delta, q, out, scale: float, scores: Scores, k
     args = [pool, len(s_arr), s_p, c_p, _buffer(q, kind[code], n * hq * d, dev, where, "q"),
             _buffer(k_new, kind[code], n * hkv * d, dev, where, "k_new"), _buffer(v_new, kind[code], n * hkv * d, dev, where, "v_new"),
             float(scale), scores.address, _buffer(out, kind[code], n * hq * d, dev, where, "out"),
-            _buffer(lse, kind[F32], n * hq, dev, where, "lse"), None, 0, _stream(stream)]
+            _buffer(lse, kind[F32], n * hq, dev, where, "lse"), None, 0, _stream_on(dev, stream, where)]
     if workspace is not None:
         args[11:13] = _buffer(workspace, workspace.dtype, 0, dev, where, "workspace"), workspace.numel() * workspace.element_size()
     _launch(lib().dk_scored_attend, args, where, pool)
@@ -459,29 +470,61 @@ class Rotary:
 
     def __init__(self, rotary_dim: int, inv_freq=None, pairs: bool = False, amplitude: float = 1.0,
                  norm_eps: Optional[float] = None, q_weight=None, k_weight=None):
-        if inv_freq is not None and (inv_freq.numel() < rotary_dim // 2 or inv_freq.element_size() != 4):
-            raise DeltaKVError(-1, "rotary", "inv_freq is float32 [rotary_dim / 2]")
+        if inv_freq is not None and (inv_freq.numel() < rotary_dim // 2 or inv_freq.dtype is not _dtypes()[0][F32]
+                                     or not inv_freq.is_contiguous()):
+            raise DeltaKVError(-1, "rotary", "inv_freq is contiguous float32 [rotary_dim / 2]")
+        if not -1 << 31 <= rotary_dim < 1 << 31:
+            raise DeltaKVError(-1, "rotary", "rotary_dim is an int32")
+        weights = [w for w in (q_weight, k_weight) if w is not None] if norm_eps is not None else []
+        if any(not w.is_contiguous() or w.dtype is not weights[0].dtype for w in weights):
+            raise DeltaKVError(-1, "rotary", "weights are contiguous and of one type")
         self.tensors = (inv_freq, q_weight, k_weight)
+        # what rows have to be: their type where there are weights, a head no wider than the weights, on this GPU
+        self.dtype = weights[0].dtype if weights else None
+        self.widest = min((w.numel() for w in weights), default=1 << 30)
+        on = {t.get_device() for t in ([] if inv_freq is None else [inv_freq]) + weights}
+        if len(on) > 1:
+            raise DeltaKVError(-1, "rotary", "frequencies and weights are on one GPU")
+        self.device = on.pop() if on else None
         self.desc = RotaryDesc(rotary_dim, int(pairs), _ptr(inv_freq), amplitude, int(norm_eps is not None), norm_eps or 0.0,
                                _ptr(q_weight), _ptr(k_weight))
         self.address = C.addressof(self.desc)
 
+    def check(self, dtype, head_dim: int, device: int, where: str) -> None:
+        """Whether frequencies and weights fit a call's rows, which the library cannot see."""
+        if (self.dtype is not None and self.dtype is not dtype) or self.widest < head_dim or (self.device is not None and self.device != device):
+            raise DeltaKVError(-1, where, "weights are head_dim elements of the rows' type, on their GPU as the frequencies are")
 
-def _heads(t, where: str):
-    """(address, elements from token to token) of [tokens, heads, head_dim] rows whose tokens are contiguous"""
+
+def _heads(t, where: str, dtype=None, tokens: int = 0, elements: int = 0, device: int = 0):
+    """(address, elements from token to token) of [tokens, heads, head_dim] rows whose tokens are contiguous, with `elements` each
+    of `dtype` where that is given"""
     shape, strides = t.shape, t.stride()
-    if len(shape) != 3 or ((strides[2] != 1 or (strides[1] != shape[2] and shape[1] > 1)) and t.numel()):
+    if len(shape) != 3:
         raise DeltaKVError(-1, where, "rows are [tokens, heads, head_dim], each token's contiguous")
-    return t.data_ptr(), (strides[0] if shape[0] > 1 else shape[1] * shape[2])
+    n, heads, width = shape
+    step, head_step, one = strides
+    if (one != 1 or (head_step != width and heads > 1)) and t.numel():
+        raise DeltaKVError(-1, where, "rows are [tokens, heads, head_dim], each token's contiguous")
+    if dtype is not None and (t.dtype is not dtype or n < tokens or heads * width != elements or t.get_device() != device or device < 0):
+        raise DeltaKVError(-1, where, f"rows are {tokens} or more tokens of {elements} elements of {dtype}, on one GPU")
+    return t.data_ptr(), (step if n > 1 else heads * width)
 
 
 def rotate_append(pool, slots, cu_delta, q, k, v, rotary: Rotary, q_out, stream=None) -> None:
-    """q, k, v: [tokens, heads, head_dim], strided over tokens; q_out contiguous."""
+    """q, k, v: [tokens, heads, head_dim] of the pool's type, strided over tokens; q_out contiguous."""
+    where = "rotate_append"
     s_arr, s_p = _array(slots)
     c_arr, c_p = _array(cu_delta)
-    _launch(lib().dk_rotate_append, (pool, len(s_arr), s_p, c_p, rotary.address, *_heads(q, "rotate_append"),
-                                     *_heads(k, "rotate_append"), *_heads(v, "rotate_append"), _ptr(q_out), _stream(stream)),
-            "rotate_append", pool)
+    n = _tokens(s_arr, c_arr, where)
+    hq, hkv, d, code = pool.shape
+    dtype, dev = _dtypes()[0][code], q.get_device()
+    rotary.check(dtype, d, dev, where)
+    _launch(lib().dk_rotate_append, (pool, len(s_arr), s_p, c_p, rotary.address, *_heads(q, where, dtype, n, hq * d, dev),
+                                     *_heads(k, where, dtype, n, hkv * d, dev), *_heads(v, where, dtype, n, hkv * d, dev),
+                                     _buffer(q_out, dtype, n * hq * d, dev, where, "q_out"),
+                                     _stream_on(dev, stream, where)),
+            where, pool)
 
 
 def rotate_rows(positions, q, k, rotary: Rotary, q_out, k_out, stream=None) -> None:

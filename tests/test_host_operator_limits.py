@@ -97,3 +97,54 @@ def test_scored_attend_takes_rows_as_the_pool_has_them(pool, calls):
     _refused(call, cu=(0, 5))  # offsets of one sequence for two
     _refused(dk.scored_workspace_bytes, pool=pool, slots=[0, 1], cu_delta=[0, 5], staged=False, scores=dk.Scores())
     assert len(calls) == 3
+
+
+def test_a_rotary_is_of_types_that_fit():
+    w = _gpu(64)
+    dk.Rotary(64, _gpu(32, dtype=F32), norm_eps=1e-6, q_weight=w, k_weight=w)
+    for freqs in (_gpu(31, dtype=F32), _gpu(32), _gpu(32, dtype=I32), _gpu(64, dtype=F32)[::2]):
+        _refused(dk.Rotary, rotary_dim=64, inv_freq=freqs)
+    for other in (_gpu(64, dtype=F32), _gpu(128)[::2], _gpu(64, at=1)):
+        _refused(dk.Rotary, rotary_dim=0, norm_eps=1e-6, q_weight=w, k_weight=other)
+    _refused(dk.Rotary, rotary_dim=0, inv_freq=_gpu(32, dtype=F32, at=1), norm_eps=1e-6, q_weight=w)
+    _refused(dk.Rotary, rotary_dim=(1 << 32) + 64)
+
+
+def test_rotate_append_takes_rows_as_the_pool_has_them(pool, calls):
+    fused = _gpu(5, 12, 64)
+    rows = dict(q=fused[:, :8], k=fused[:, 8:10], v=fused[:, 10:])
+
+    def call(q_out=_gpu(5, 8, 64), rotary=dk.Rotary(0), cu=(0, 2, 5), **kw):
+        dk.rotate_append(pool, [0, 1], cu, *{**rows, **kw}.values(), rotary, q_out, stream=0)
+
+    call()
+    call(q_out=_gpu(5, 512), rotary=dk.Rotary(64, _gpu(32, dtype=F32), norm_eps=0.0, q_weight=_gpu(64)))
+    call(q=_gpu(6, 8, 64), k=_gpu(9, 2, 64))
+    call(rotary=dk.Rotary(0, q_weight=_gpu(64, dtype=F32)))  # (without a norm no weight is looked at)
+    assert len(calls) == 4
+    for name, heads in (("q", 8), ("k", 2), ("v", 2)):
+        for bad in (_gpu(4, heads, 64), _gpu(5, heads, 64, dtype=F32), _gpu(5, heads, 64, dtype=torch.float16), _gpu(5, heads + 1, 64),
+                    _gpu(5, heads, 128), torch.zeros((5, heads, 64), dtype=BF16), _gpu(5, heads, 128)[:, :, ::2]):
+            _refused(call, **{name: bad})
+    for bad in (_gpu(4, 8, 64), _gpu(5, 8, 64, dtype=F32), fused[:, :8], torch.zeros((5, 8, 64), dtype=BF16), _gpu(5, 8, 64, at=1)):
+        _refused(call, q_out=bad)
+    for kw in (dict(q_weight=_gpu(64, dtype=F32)), dict(k_weight=_gpu(32)), dict(q_weight=torch.zeros(64, dtype=BF16)),
+               dict(inv_freq=torch.zeros(32), rotary_dim=64)):
+        _refused(call, rotary=dk.Rotary(**{"rotary_dim": 0, "norm_eps": 0.0, **kw}))
+    _refused(call, cu=(0, 5))
+    assert len(calls) == 4
+
+
+def test_tensors_of_another_gpu_than_the_current_one_are_refused(pool, calls, monkeypatch):
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 77, raising=False)
+    for at in (0, 1):
+        def attend():
+            dk.scored_attend(pool, [0], [0, 5], _gpu(5, 8, 64, at=at), _gpu(5, 8, 64, at=at), 1.0, dk.Scores())
+
+        def append():
+            dk.rotate_append(pool, [0], [0, 5], _gpu(5, 8, 64, at=at), *[_gpu(5, 2, 64, at=at)] * 2, dk.Rotary(0), _gpu(5, 8, 64, at=at))
+
+        for call in (attend, append):
+            _refused(call) if at else call()
+    assert [args[-1] for args in calls] == [77, 77]
