@@ -496,9 +496,8 @@ class Rotary:
             raise DeltaKVError(-1, where, "weights are head_dim elements of the rows' type, on their GPU as the frequencies are")
 
 
-def _heads(t, where: str, dtype=None, tokens: int = 0, elements: int = 0, device: int = 0):
-    """(address, elements from token to token) of [tokens, heads, head_dim] rows whose tokens are contiguous, with `elements` each
-    of `dtype` where that is given"""
+def _heads(t, where: str):
+    """(tokens, heads, head width, address, elements from token to token) of rows whose tokens are contiguous"""
     shape, strides = t.shape, t.stride()
     if len(shape) != 3:
         raise DeltaKVError(-1, where, "rows are [tokens, heads, head_dim], each token's contiguous")
@@ -506,9 +505,15 @@ def _heads(t, where: str, dtype=None, tokens: int = 0, elements: int = 0, device
     step, head_step, one = strides
     if (one != 1 or (head_step != width and heads > 1)) and t.numel():
         raise DeltaKVError(-1, where, "rows are [tokens, heads, head_dim], each token's contiguous")
-    if dtype is not None and (t.dtype is not dtype or n < tokens or heads * width != elements or t.get_device() != device or device < 0):
+    return n, heads, width, t.data_ptr(), (step if n > 1 else heads * width)
+
+
+def _pool_rows(t, dtype, tokens: int, elements: int, device: int, where: str):
+    """(address, elements from token to token) of at least that many tokens of so many elements each, as the pool has them"""
+    n, heads, width, address, step = _heads(t, where)
+    if t.dtype is not dtype or n < tokens or heads * width != elements or t.get_device() != device or device < 0:
         raise DeltaKVError(-1, where, f"rows are {tokens} or more tokens of {elements} elements of {dtype}, on one GPU")
-    return t.data_ptr(), (step if n > 1 else heads * width)
+    return address, step
 
 
 def rotate_append(pool, slots, cu_delta, q, k, v, rotary: Rotary, q_out, stream=None) -> None:
@@ -520,22 +525,36 @@ def rotate_append(pool, slots, cu_delta, q, k, v, rotary: Rotary, q_out, stream=
     hq, hkv, d, code = pool.shape
     dtype, dev = _dtypes()[0][code], q.get_device()
     rotary.check(dtype, d, dev, where)
-    _launch(lib().dk_rotate_append, (pool, len(s_arr), s_p, c_p, rotary.address, *_heads(q, where, dtype, n, hq * d, dev),
-                                     *_heads(k, where, dtype, n, hkv * d, dev), *_heads(v, where, dtype, n, hkv * d, dev),
-                                     _buffer(q_out, dtype, n * hq * d, dev, where, "q_out"),
-                                     _stream_on(dev, stream, where)),
+    _launch(lib().dk_rotate_append, (pool, len(s_arr), s_p, c_p, rotary.address, *_pool_rows(q, dtype, n, hq * d, dev, where),
+                                     *_pool_rows(k, dtype, n, hkv * d, dev, where), *_pool_rows(v, dtype, n, hkv * d, dev, where),
+                                     _buffer(q_out, dtype, n * hq * d, dev, where, "q_out"), _stream_on(dev, stream, where)),
             where, pool)
 
 
 def rotate_rows(positions, q, k, rotary: Rotary, q_out, k_out, stream=None) -> None:
-    """positions: int64 device tensor; q or k may be None."""
-    some = q if q is not None else k
-    dtype = BF16 if some.element_size() == 2 else F32
-    args = []
-    for x, out in ((q, q_out), (k, k_out)):
-        args += [0, None, 0, None] if x is None else [x.shape[1], *_heads(x, "rotate_rows"), _ptr(out)]
-    _check(lib().dk_rotate_rows(dtype, some.shape[2], some.shape[0], _ptr(positions), rotary.address, *args, _stream(stream)),
-           "rotate_rows")
+    """positions: contiguous int64 device tensor; q, k: [tokens, heads, head_dim] of one type, strided over tokens, or None; outputs
+    contiguous."""
+    where = "rotate_rows"
+    (f32, bf16), _, int64 = _dtypes()
+    args, dtype, dev, tokens, d = [], None, -1, 0, 0
+    for x, out, what in ((q, q_out, "q_out"), (k, k_out, "k_out")):
+        if x is None:
+            args += (0, None, 0, None)
+            continue
+        n, heads, width, address, step = _heads(x, where)
+        kind, on = x.dtype, x.get_device()
+        if dtype is None:
+            if kind is not f32 and kind is not bf16:
+                raise DeltaKVError(-1, where, "rows are float32 or bfloat16")
+            dtype, dev, tokens, d = kind, on, n, width
+        elif kind is not dtype or on != dev or n != tokens or width != d:
+            raise DeltaKVError(-1, where, "q and k are rows of the same tokens, of one type and width")
+        args += (heads, address, step, _buffer(out, dtype, n * heads * width, dev, where, what))
+    if dtype is None:
+        raise DeltaKVError(-1, where, "rows of q, k or both")
+    rotary.check(dtype, d, dev, where)
+    _check(lib().dk_rotate_rows(BF16 if dtype is bf16 else F32, d, tokens, _buffer(positions, int64, tokens, dev, where, "positions"),
+                                rotary.address, *args, _stream_on(dev, stream, where)), where)
 
 
 ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_BANDS, ROTARY_RAMP = range(5)

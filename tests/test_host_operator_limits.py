@@ -148,3 +148,43 @@ def test_tensors_of_another_gpu_than_the_current_one_are_refused(pool, calls, mo
         for call in (attend, append):
             _refused(call) if at else call()
     assert [args[-1] for args in calls] == [77, 77]
+
+
+class _Recorder:
+    """A library whose calls are kept and succeed."""
+
+    def __init__(self, **answers):
+        self.made, self.answers = [], answers
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.made.append(args)
+            return 0
+        return call
+
+
+def test_rotate_rows_takes_rows_of_one_kind(monkeypatch):
+    lib = _Recorder()
+    monkeypatch.setattr(dk, "lib", lambda: lib)
+    fused = _gpu(5, 12, 64)
+
+    def call(positions=_gpu(5, dtype=I64), q=fused[:, :8], k=fused[:, 8:], q_out=_gpu(5, 8, 64), k_out=_gpu(5, 4, 64), rotary=dk.Rotary(0)):
+        dk.rotate_rows(positions, q, k, rotary, q_out, k_out, stream=0)
+
+    call()
+    call(q=None, q_out=None)
+    call(k=None, k_out=None, rotary=dk.Rotary(64, _gpu(32, dtype=F32), norm_eps=0.0, q_weight=_gpu(64)))
+    call(q=_gpu(5, 8, 64, dtype=F32), k=None, q_out=_gpu(5, 8, 64, dtype=F32), positions=_gpu(7, dtype=I64))
+    assert [a[0] for a in lib.made] == [dk.BF16, dk.BF16, dk.BF16, dk.F32] and lib.made[1][5:9] == (0, None, 0, None)
+    for positions in (_gpu(5, dtype=I32), _gpu(4, dtype=I64), _gpu(10, dtype=I64)[::2], torch.zeros(5, dtype=I64), _gpu(5, dtype=F32)):
+        _refused(call, positions=positions)
+    for k in (_gpu(4, 4, 64), _gpu(6, 4, 64), _gpu(5, 2, 128), _gpu(5, 4, 64, dtype=F32), _gpu(5, 256), torch.zeros((5, 4, 64), dtype=BF16)):
+        _refused(call, k=k)
+    half = _gpu(5, 8, 64, dtype=torch.float16)
+    _refused(call, q=half, k=None, q_out=half)
+    _refused(call, q=None, k=None)
+    for bad in (_gpu(4, 8, 64), _gpu(5, 8, 64, dtype=F32), fused[:, :8], torch.zeros((5, 8, 64), dtype=BF16)):
+        _refused(call, q_out=bad)
+        _refused(call, k_out=bad[:, :3])
+    _refused(call, rotary=dk.Rotary(0, norm_eps=0.0, k_weight=_gpu(64, dtype=F32)))
+    assert len(lib.made) == 4
