@@ -181,14 +181,15 @@ def _stream(stream) -> Optional[int]:
 
 
 _DTYPES = None
+_torch = None  # the module, from the first call that needs it on (host-only use of the binding does not)
 
 
 def _dtypes():
     """(what F32 and BF16 are in torch, int32, int64)"""
-    global _DTYPES
+    global _DTYPES, _torch
     if _DTYPES is None:
         import torch
-        _DTYPES = ((torch.float32, torch.bfloat16), torch.int32, torch.int64)
+        _DTYPES, _torch = ((torch.float32, torch.bfloat16), torch.int32, torch.int64), torch
     return _DTYPES
 
 
@@ -216,10 +217,19 @@ def _stream_on(device: int, stream, where: str) -> Optional[int]:
     """The stream of a call whose tensors are on that GPU: work goes to the current one."""
     if stream is not None:
         return _stream(stream)
-    import torch
-    if torch._C._cuda_getDevice() != device:
+    cuda = _torch._C
+    if cuda._cuda_getDevice() != device:
         raise DeltaKVError(-1, where, "the tensors are not on the current GPU")
-    return torch._C._cuda_getCurrentRawStream(device) or None
+    return cuda._cuda_getCurrentRawStream(device) or None
+
+
+def _room(workspace, device: int, where: str):
+    """(address, bytes) of a workspace"""
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        raise DeltaKVError(-1, where, "the workspace is contiguous, on the GPU of the others")
+    return workspace.data_ptr(), workspace.nbytes
 
 
 # --------------------------------------------------------------------------- pool
@@ -454,12 +464,10 @@ def scored_attend(pool, slots, cu_delta, q, out, scale: float, scores: Scores, k
     kind, dev = _dtypes()[0], q.get_device()
     if scores.slopes is not None and scores.slopes.get_device() != dev:
         raise DeltaKVError(-1, where, "slopes are on the GPU of the others")
-    args = [pool, len(s_arr), s_p, c_p, _buffer(q, kind[code], n * hq * d, dev, where, "q"),
+    args = (pool, len(s_arr), s_p, c_p, _buffer(q, kind[code], n * hq * d, dev, where, "q"),
             _buffer(k_new, kind[code], n * hkv * d, dev, where, "k_new"), _buffer(v_new, kind[code], n * hkv * d, dev, where, "v_new"),
             float(scale), scores.address, _buffer(out, kind[code], n * hq * d, dev, where, "out"),
-            _buffer(lse, kind[F32], n * hq, dev, where, "lse"), None, 0, _stream_on(dev, stream, where)]
-    if workspace is not None:
-        args[11:13] = _buffer(workspace, workspace.dtype, 0, dev, where, "workspace"), workspace.numel() * workspace.element_size()
+            _buffer(lse, kind[F32], n * hq, dev, where, "lse"), *_room(workspace, dev, where), _stream_on(dev, stream, where))
     _launch(lib().dk_scored_attend, args, where, pool)
 
 
@@ -580,12 +588,28 @@ def logprobs_workspace_bytes(total_rows: int, vocab: int, dtype: int, n_top: int
 def token_logprobs(total_rows: int, logits, dtype: int, vocab: int, row_stride: int, tokens, logprob_out, workspace,
                    scale: float = 1.0, rank_out=None, entropy_out=None, n_top: int = 0, top_ids_out=None,
                    top_logprobs_out=None, stream=None) -> None:
-    """All tensors are device tensors; nothing is synchronised."""
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().dk_token_logprobs(int(total_rows), _ptr(logits), int(dtype), int(vocab), int(row_stride), float(scale),
-                                   _ptr(tokens), _ptr(logprob_out), _ptr(rank_out), _ptr(entropy_out), int(n_top),
-                                   _ptr(top_ids_out), _ptr(top_logprobs_out), _ptr(workspace), ws_bytes, _stream(stream)),
-           "token_logprobs")
+    """All tensors are device tensors, contiguous but for logits, whose rows are row_stride elements apart; nothing is synchronised."""
+    where = "token_logprobs"
+    rows, n_top = int(total_rows), int(n_top)
+    kinds, int32, _ = _dtypes()
+    shape, dev = logits.shape, logits.get_device()
+    if len(shape) == 2:
+        step, one = logits.stride()
+        fits = shape[0] >= rows and shape[1] >= vocab and (one == 1 or vocab == 1) and (rows <= 1 or step == row_stride)
+    else:
+        fits = logits.is_contiguous() and (rows == 0 or logits.numel() >= (rows - 1) * row_stride + vocab)
+    if not fits or dev < 0:
+        raise DeltaKVError(-1, where, "logits are [total_rows, vocab] on a GPU, row_stride elements from row to row")
+    if dtype in (F32, BF16) and logits.dtype is not kinds[dtype]:
+        raise DeltaKVError(-1, where, "logits are of the type that dtype says")
+    f32 = kinds[F32]
+    _check(lib().dk_token_logprobs(rows, logits.data_ptr(), int(dtype), int(vocab), int(row_stride), float(scale),
+                                   _buffer(tokens, int32, rows, dev, where, "tokens"), _buffer(logprob_out, f32, rows, dev, where, "logprob_out"),
+                                   _buffer(rank_out, int32, rows, dev, where, "rank_out"),
+                                   _buffer(entropy_out, f32, rows, dev, where, "entropy_out"), n_top,
+                                   _buffer(top_ids_out, int32, rows * n_top, dev, where, "top_ids_out"),
+                                   _buffer(top_logprobs_out, f32, rows * n_top, dev, where, "top_logprobs_out"),
+                                   *_room(workspace, dev, where), _stream_on(dev, stream, where)), where)
 
 
 # -- host-only: radix prefix cache, prompt lookup, scheduler helpers ---------------------------------------

@@ -188,3 +188,36 @@ def test_rotate_rows_takes_rows_of_one_kind(monkeypatch):
         _refused(call, k_out=bad[:, :3])
     _refused(call, rotary=dk.Rotary(0, norm_eps=0.0, k_weight=_gpu(64, dtype=F32)))
     assert len(lib.made) == 4
+
+
+def test_token_logprobs_takes_logits_and_outputs_as_they_are_described(monkeypatch):
+    lib = _Recorder()
+    monkeypatch.setattr(dk, "lib", lambda: lib)
+    good = dict(logits=_gpu(3, 104)[:, :100], tokens=_gpu(3, dtype=I32), logprob_out=_gpu(3, dtype=F32), workspace=_gpu(4096, dtype=torch.uint8),
+                rank_out=_gpu(3, dtype=I32), entropy_out=_gpu(3, dtype=F32), top_ids_out=_gpu(3, 2, dtype=I32), top_logprobs_out=_gpu(3, 2, dtype=F32))
+
+    def call(rows=3, dtype=dk.BF16, vocab=100, row_stride=104, n_top=2, **kw):
+        t = {**good, **kw}
+        logits, rest = t.pop("logits"), t
+        dk.token_logprobs(rows, logits, dtype, vocab, row_stride, n_top=n_top, stream=0, **rest)
+
+    call()
+    call(logits=_gpu(3 * 104))
+    call(logits=_gpu(4, 104))
+    call(rows=1, logits=_gpu(100), row_stride=104)
+    call(rows=0, logits=_gpu(0, 100), row_stride=104)
+    call(tokens=None, logprob_out=None, rank_out=None)
+    assert len(lib.made) == 6 and lib.made[0][14] == 4096
+    for logits in (_gpu(2, 104), _gpu(3, 96), _gpu(3, 112), _gpu(104, 3).t(), _gpu(3, 208)[:, ::2], _gpu(3, 104, dtype=F32),
+                   _gpu(3, 104, dtype=torch.float16), torch.zeros((3, 104), dtype=BF16), _gpu(2 * 104 + 99)):
+        _refused(call, logits=logits)
+    _refused(call, dtype=dk.F32)
+    for name in ("tokens", "rank_out", "logprob_out", "entropy_out", "top_ids_out", "top_logprobs_out"):
+        t = good[name]
+        other = I64 if t.dtype is I32 else torch.float64
+        for bad in (t[:2], t.to(other), t.to(F32 if t.dtype is I32 else I32), torch.zeros(t.shape, dtype=t.dtype),
+                    _gpu(6 * t.numel(), dtype=t.dtype)[::2], _gpu(*t.shape, dtype=t.dtype, at=1)):
+            _refused(call, **{name: bad})
+    _refused(call, workspace=torch.zeros(4096, dtype=torch.uint8))
+    _refused(call, n_top=3)  # longer lists than there is room for
+    assert len(lib.made) == 6
