@@ -477,14 +477,15 @@ int32_t dk_seq_stats(dk_pool* pool, int32_t slot, int64_t* segments_out, int64_t
 int32_t dk_staging_wait(dk_pool* pool);
 
 /*
- * What the last attention call that was enqueued, or the last dk_attend_workspace_bytes() (which leaves no short sequences to
+ * What the last attention call that was enqueued (dk_scored_attend among them), or the last dk_attend_workspace_bytes() (which leaves no short sequences to
  * the scalar kernel), of this pool planned: HOST int64 [DK_PLAN_FIELDS].  DK_ERR_INVALID before the first of them.
  */
-enum { DK_ROUTE_SCALAR = 0, DK_ROUTE_TILE = 1, DK_ROUTE_GENERAL = 2, DK_ROUTE_F32 = 3 };
+enum { DK_ROUTE_SCALAR = 0, DK_ROUTE_TILE = 1, DK_ROUTE_GENERAL = 2, DK_ROUTE_F32 = 3, DK_ROUTE_SCORED = 4 };
 enum {
-  DK_PLAN_ROUTE = 0,        /* scalar kernel; tile, general or fp32 kernel, each of the first two beside the streaming kernel */
-  DK_PLAN_ROW_ITEMS = 1,    /* work items of the tile, block or fp32 kernel */
-  DK_PLAN_STREAM_ITEMS = 2, /* work items of the streaming kernel */
+  DK_PLAN_ROUTE = 0,        /* scalar kernel; tile, general or fp32 kernel, each of the first two beside the streaming kernel;
+                               the kernels of dk_scored_attend */
+  DK_PLAN_ROW_ITEMS = 1,    /* work items of the tile, block or fp32 kernel; of dk_scored_attend's kernel for many rows */
+  DK_PLAN_STREAM_ITEMS = 2, /* work items of the streaming kernel; of dk_scored_attend's kernel for few rows */
   DK_PLAN_MERGES = 3,       /* row tiles whose key range is split */
   DK_PLAN_BYTES = 4,        /* workspace */
   DK_PLAN_FIELDS = 5
@@ -524,7 +525,7 @@ int32_t dk_set_attend_variant(dk_pool* pool, int32_t variant);
 int32_t dk_set_tuning(dk_pool* pool, const char* name, double value);
 /*
  * Device time of the attention work (tile, streaming and merge kernels; not the descriptor upload) of recent
- * dk_delta_attend calls on this pool, measured with HIP events recorded on the call's stream.
+ * dk_delta_attend, dk_append_attend and dk_scored_attend calls on this pool, measured with HIP events recorded on the call's stream.
  * dk_set_attend_timing(pool, n): keep the last n calls (0 <= n <= 256; 0 switches recording off).
  * dk_attend_times: waits for the recorded work, then writes the durations in milliseconds, oldest
  * first, of the last min(cap, recorded) calls to ms_out (HOST float [cap]); *n_out receives the count.
@@ -537,7 +538,8 @@ int32_t dk_last_attend_ms(dk_pool* pool, float* ms_out);
 /*
  * Host time the launching calls of this pool have spent, by phase, in microseconds since the last reset
  * (a profiling probe: a few clock reads per call).  us_out HOST double [DK_HOST_PHASES] indexed by the
- * enum below, calls_out HOST int64 [2]: number of dk_delta_attend(_noalloc) and of dk_kv_append calls.
+ * enum below, calls_out HOST int64 [2]: number of attention calls (dk_scored_attend among them, under delta_attend below) and
+ * of appends (dk_rotate_append among them, under kv_append below).
  * Each pointer nullable; reset != 0 clears the sums.
  */
 enum {

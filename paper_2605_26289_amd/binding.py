@@ -380,7 +380,7 @@ def append_attend(pool, slots, cu_delta, q, k_new, v_new, out, scale: float, lse
                                      _ptr(lse), _ptr(workspace), ws_bytes, _stream(stream)), "append_attend", pool)
 
 
-ROUTES = ("scalar", "tile", "general", "f32")
+ROUTES = ("scalar", "tile", "general", "f32", "scored")
 
 
 def last_plan(pool) -> dict:
@@ -729,7 +729,7 @@ HOST_PHASES = ("plan", "stage", "upload", "launch", "append_bookkeeping", "appen
 
 
 def host_times(pool, reset: bool = False):
-    """({phase: microseconds}, (delta_attend calls, kv_append calls)) since the last reset"""
+    """({phase: microseconds}, (attention calls, appends)) since the last reset"""
     us = (C.c_double * len(HOST_PHASES))()
     calls = (C.c_int64 * 2)()
     _check(lib().dk_host_times(pool, int(reset), us, calls), "host_times")

@@ -78,7 +78,7 @@ struct dk_pool {
   int32_t last_hip = 0;
   // host time spent inside launching calls, by phase (see dk_host_times)
   double host_us[DK_HOST_PHASES] = {};
-  int64_t host_calls[2] = {0, 0};  // dk_delta_attend*, dk_kv_append
+  int64_t host_calls[2] = {0, 0};  // attention calls, appends
   std::mutex launch_mu;  // serialises GPU-launching calls (shared staging ring, dev_meta and plan)
   dk::AttendPlan plan;   // reused from call to call so that steady-state planning allocates nothing
   int64_t last_plan[DK_PLAN_FIELDS] = {-1};  // see dk_last_plan
@@ -128,6 +128,14 @@ struct dk_pool {
     last_plan[DK_PLAN_STREAM_ITEMS] = (int64_t)plan.stream_items.size();
     last_plan[DK_PLAN_MERGES] = (int64_t)plan.merges.size();
     last_plan[DK_PLAN_BYTES] = (int64_t)plan.total_bytes;
+  }
+
+  void keep_scored_plan() {
+    last_plan[DK_PLAN_ROUTE] = DK_ROUTE_SCORED;
+    last_plan[DK_PLAN_ROW_ITEMS] = (int64_t)scored_plan.rows.size();
+    last_plan[DK_PLAN_STREAM_ITEMS] = (int64_t)scored_plan.few.size();
+    last_plan[DK_PLAN_MERGES] = (int64_t)scored_plan.merges.size();
+    last_plan[DK_PLAN_BYTES] = (int64_t)scored_plan.total_bytes;
   }
 
   int32_t hip_fail(hipError_t e) {
@@ -881,6 +889,7 @@ int32_t dk_scored_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
   if (!pool || (k_new == nullptr) != (v_new == nullptr) || !(scale >= -FLT_MAX && scale <= FLT_MAX)) return DK_ERR_INVALID;
   return guarded([&]() -> int32_t {
     std::lock_guard<std::mutex> launch(pool->launch_mu);
+    PhaseClock clk;
     hipStream_t st = (hipStream_t)stream;
     dk::ScoredPlan& plan = pool->scored_plan;
     dk::ScoreMasks masks;
@@ -908,6 +917,7 @@ int32_t dk_scored_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     const bool inline_blob = plan.blob_bytes <= (size_t)dk::INLINE_BLOB_BYTES;
     // a captured upload would be replayed from a staging buffer that has other descriptors by then
     if (!inline_blob && pool->ring_size > 0 && capturing(st)) return DK_ERR_UNSUPPORTED;
+    pool->host_us[DK_HOST_PLAN] += clk.lap();
     dk::InlineBlob blob_args{};
     char* h = (char*)&blob_args;
     Staging* s = nullptr;
@@ -923,10 +933,12 @@ int32_t dk_scored_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     put(plan.off_rows, plan.rows.data(), plan.rows.size() * sizeof(DkItem));
     put(plan.off_merges, plan.merges.data(), plan.merges.size() * sizeof(DkMerge));
     put(plan.off_first, plan.first.data(), plan.first.size() * sizeof(int32_t));
+    pool->host_us[DK_HOST_STAGE] += clk.lap();
     if (!inline_blob) {
       rc = pool->upload(s, workspace, plan.blob_bytes, st);
       if (rc != DK_OK) return rc;
     }
+    pool->host_us[DK_HOST_UPLOAD] += clk.lap();
     const uintptr_t desc = inline_blob ? 0 : (uintptr_t)workspace;
     dk::AttendArgs a;
     a.inline_blob = inline_blob ? &blob_args : nullptr;
@@ -975,8 +987,17 @@ int32_t dk_scored_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
       sp.arrival_slice = pool->arrival_slice;
       items.n_merges = 0;
     }
-    const hipError_t e = dk::launch_attend_scored(a, sp, items, st);
-    return e == hipSuccess ? DK_OK : pool->hip_fail(e);
+    const bool timing = !pool->ev0.empty();
+    const size_t ev_slot = timing ? (size_t)(pool->ev_calls % (int64_t)pool->ev0.size()) : 0;
+    hipError_t e = timing ? hipEventRecord(pool->ev0[ev_slot], st) : hipSuccess;
+    if (e == hipSuccess) e = dk::launch_attend_scored(a, sp, items, st);
+    if (e == hipSuccess && timing) e = hipEventRecord(pool->ev1[ev_slot], st);
+    if (e != hipSuccess) return pool->hip_fail(e);
+    pool->ev_calls += timing;
+    pool->keep_scored_plan();
+    pool->host_us[DK_HOST_LAUNCH] += clk.lap();
+    ++pool->host_calls[0];
+    return DK_OK;
   });
 }
 
@@ -1028,6 +1049,7 @@ int32_t dk_rotate_append(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
   if (!pool) return DK_ERR_INVALID;
   return guarded([&]() -> int32_t {
     std::lock_guard<std::mutex> launch(pool->launch_mu);
+    PhaseClock clk;
     const dk_pool_desc& d = pool->desc;
     int32_t rc = rotary_ok(rotary, d.head_dim);
     if (rc != DK_OK) return rc;
@@ -1070,6 +1092,8 @@ int32_t dk_rotate_append(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     a.v_out = d.v_arena;
     a.arena_cells = pool->meta_arena_cells;
     hipStream_t st = (hipStream_t)stream;
+    pool->host_us[DK_HOST_APPEND_BOOK] += clk.lap();
+    ++pool->host_calls[1];
     // The runs of cells and positions travel in the kernel arguments where they fit; else a table of every token's is uploaded.
     if (runs_of.size() <= (size_t)dk::ROTARY_INLINE_MAX_RUNS) {
       dk::RotaryRuns runs;
@@ -1082,6 +1106,7 @@ int32_t dk_rotate_append(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
       }
       runs.tok[n_runs] = (int32_t)total;
       const hipError_t e = dk::launch_rotate_append(a, runs, n_runs, (int32_t)total, st);
+      pool->host_us[DK_HOST_APPEND_LAUNCH] += clk.lap();
       return e == hipSuccess ? DK_OK : undo(pool->hip_fail(e));
     }
     if (per_launch <= 0) return undo(DK_ERR_WORKSPACE);
@@ -1110,6 +1135,7 @@ int32_t dk_rotate_append(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
       const hipError_t e = dk::launch_rotate_append_table(a, (const int32_t*)d.dev_meta, (int32_t)base, n, st);
       if (e != hipSuccess) return undo(pool->hip_fail(e));
     }
+    pool->host_us[DK_HOST_APPEND_LAUNCH] += clk.lap();
     return DK_OK;
   });
 }
