@@ -152,10 +152,15 @@ int32_t build_scored_plan(Pool& pool, const ScoredConfig& cfg, int32_t n_seqs, c
   for (int32_t b = 0; b < n_seqs; ++b) most = std::max<int64_t>(most, (int64_t)cu_delta[b + 1] - cu_delta[b]);
   // packed row numbers are divided by the group by a multiplication that is exact while row * (group - 1) < 2^32
   if (most >= (int64_t(1) << 31) / (group * group)) return ERR_UNSUPPORTED;
-  // fp32: items of 32 rows read K and V half as often, items of 16 end in smaller steps where there are little more than one for every
-  // compute unit.  Measured, us, 32 / 16 rows: 268 tiles of 32 rows, documents 32.4 / 28.0, a window of 200 39.5 / 35.2, all of 1300 keys
-  // 107.6 / 108.6; 320 tiles, the window 38.2 / 36.6; 405 tiles, the window 42.9 / 45.1, all keys 133 / 158.
-  p->tile_rows = cfg.bf16 ? 128 : (p->total_tokens * group + 31) / 32 * cfg.n_kv_heads >= 320 ? 32 : 16;
+  // fp32: a compute unit has one workgroup at a time.  Items of 32 rows read K and V half as often, items of 16 take shorter rounds: 32
+  // where that halves the rounds, 16 where rows have starts of their own unless there are many (32 of them see the union of more
+  // documents).  Measured, us, 16 / 32 rows, a window of 200 and all of 1300 keys, by tiles of 32 rows:
+  //   128  12.8 / 20.2   41 / 49      160  22.3 / 20.4   67 / 68      256  27.6 / 22.2   85 / 68      288  36.0 / 37.4  117 / 105
+  //   320  36.6 / 38.4  119 / 121     384  37.2 / 42.8  124 / 129     400  45.3 / 42.9  155 / 130     512  46.5 / 43.4  166 / 137
+  // and documents: 160  19.0 / 24.0, 254  24.7 / 29.6, 360  31.8 / 34.9, 400  36.6 / 34.5, 440  39.5 / 35.8.
+  const int64_t tiles = (p->total_tokens * group + 31) / 32 * cfg.n_kv_heads;
+  const bool halves = tiles > 384 || (tiles > 128 && tiles <= 256 && !masks.first);
+  p->tile_rows = cfg.bf16 ? 128 : halves ? 32 : 16;
   for (int32_t b = 0; b < n_seqs; ++b) {
     const int32_t delta = cu_delta[b + 1] - cu_delta[b];
     int64_t len = 0;

@@ -21,8 +21,10 @@ struct ScoredConfig {
   int32_t n_q_heads = 0, n_kv_heads = 0, head_dim = 0;
   bool bf16 = true;
   int32_t few_rows = 64;     // bf16: entries of at most this many packed rows go to the kernel for few rows
-  // Smallest key range worth a work item there, and in the rows kernels.  Measured, us, 128 / 256 / 512: one fp32 token on 5000 cached
-  // 17.4 / 17.2 / 21.7, nine on 1000 13.2 / 15.2 / 20.8, short fp32 documents 32.8 / 31.4 / 29.8; one bf16 token on 3000 12.9 / 12.2 / -.
+  // Smallest key range worth a work item there, and in the rows kernels.  Measured, us, 128 / 256 / 512: one bf16 token on 600 9.0 / 9.9 /
+  // 10.8, on 3000 13.5 / 10.8 / 12.4, on 10 000 19.6 / 19.5 / 17.8, of 64-wide heads on 3000 12.1 / 9.4 / 10.2; one fp32 token on 5000
+  // 18.1 / 17.7 / 22.1, nine on 1000 13.8 / 16.1 / 21.3, fp32 documents 28.1 / 27.7 / 27.5, two short ones 18.9 / 13.7 / 13.6; a bf16 chunk
+  // of 64 on 1000 19.3 / 19.7 / 24.7, of 128 on 3000 31.1 / 31.1 / 30.8.
   int32_t few_chunk = 256;
   int32_t rows_chunk = 256;
   int64_t once_cells = 0;    // few rows that read at least this many cells read them past the caches (0: never)
