@@ -252,7 +252,10 @@ int32_t dk_delta_attend_noalloc(dk_pool* pool, int32_t n_seqs, const int32_t* sl
  *   s''= s' - slopes[h] * |p - k|       if slopes
  * and the row sees the positions max(first, p - window + 1) .. max(p, prefix - 1) that exist (window, prefix and first where
  * given; otherwise 0 .. p, as in dk_delta_attend).  A row that sees nothing gets zeros, and -infinity as its log-sum-exp.
- * K and V at positions a row does not see have no influence on it, whatever they hold.
+ * K and V at positions a row does not see have no influence on it, whatever they hold.  In bf16 pools every softmax weight is rounded
+ * once to bf16 before it meets V (half a step, 2^-8 of the weighted mean of |V|), for all head widths and group sizes; dk_delta_attend
+ * does so too where its tile kernel runs, but keeps weights exact to 16 bits in its general route (64-wide heads, groups that are no
+ * power of two): a layer without changed scores is more exact there.
  *   cap      0: scores are not capped; else 1/1024 .. 1024 (DK_ERR_UNSUPPORTED for other positive values)
  *   slopes   DEVICE float [n_q_heads] or NULL, finite
  *   window   >= 0; 0: no window

@@ -6,6 +6,12 @@
 //
 // Scores are kept in log2 units t = s log2(e).  With u = 2^(2 log2(e) scale q.k / cap), tanh = 1 - 2 / (1 + u): one exponential,
 // one reciprocal, and an infinite or vanishing u ends at the cap by itself.
+// A weight is rounded once to bf16, the type of V, for the product with V; its row's sum is of the unrounded ones, in fp32.  That is off by
+// at most half a step, 2^-8 of the weighted mean of |V|.  Keeping the rest of a weight for a second product with V, as the block kernel
+// does for dk_delta_attend, would be half as many matrix instructions again, and in long turns those add to the time of the exponentials
+// (see scored_rows_kernel).  Error against 64 bits, of the result's norm, normal inputs: bf16 store alone 1.6e-3; here one and nine
+// tokens on 3000 1.7e-3 with 64-wide heads, 2.0e-3 with 128, 300 tokens on 2000 2.2e-3; dk_delta_attend 2.0e-3 to 2.3e-3 in the tile
+// kernel, which rounds alike, 1.6e-3 to 1.7e-3 in the block kernel.
 #include <hip/hip_runtime.h>
 
 #include <mutex>
@@ -344,9 +350,10 @@ struct RowsGeo {
 // the products of tile t + 1 among the instructions of the vector unit, which with capped scores has more to do than the matrix
 // cores: 28 of its cycles for a cap and 16 for the rest against 32 for a score's two products (128-wide heads).
 // K of a tile is requested a step ahead, V two.  Workgroup w: item w / n_kv_heads, KV head w % n_kv_heads.
-// 16 turns of 64 to 512 tokens on 1k to 8k keys, capped, 414 GFLOP: 545 to 572 us, 720 to 760 TFLOP/s (without a cap 460).  No one
-// part of the step bounds it: without the cap's and the weights' exponentials it took 488, without the first or the second products 462
-// and 457, without requests past the first tiles 498.  Weights of 32 keys between both products of their neighbours, in the same
+// 16 turns of 64 to 512 tokens on 1k to 8k keys, capped, 414 GFLOP: 545 to 572 us, 720 to 760 TFLOP/s (without a cap 460).  By counters
+// the vector unit is busy 63 % of the SIMDs' cycles and the matrix pipe 34 %: the two run nearly one after the other.  Without the cap's
+// and the weights' exponentials it took 488, without the first or the second products 462 and 457, without requests past the first
+// tiles 498.  Weights of 32 keys between both products of their neighbours, in the same
 // registers, took as long; 64 rows per wavefront, one wavefront per SIMD, 707.
 template <int HD, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void scored_rows_kernel(InlineBlob blob, Ctx c, ScoreParams sp) {

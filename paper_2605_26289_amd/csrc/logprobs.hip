@@ -15,6 +15,8 @@
 // all from T on; where those are many, all above T and of those equal to T the first n in the order of their ids -- go to LDS and are
 // put in order by counting, for each, those before it.
 //
+// Sums are in fp32: a thread's of at most 64 terms, then pairwise over the workgroup, then the chunks': 1e-7 of a log probability or an
+// entropy against 64 bits (sums in fp64 would be 1e-8).
 // Ties go to the lowest id; a NaN counts as +infinity there and makes the sums NaN.
 #include <hip/hip_runtime.h>
 
