@@ -480,8 +480,9 @@ int32_t dk_seq_stats(dk_pool* pool, int32_t slot, int64_t* segments_out, int64_t
 int32_t dk_staging_wait(dk_pool* pool);
 
 /*
- * What the last attention call that was enqueued (dk_scored_attend among them), or the last dk_attend_workspace_bytes() (which leaves no short sequences to
- * the scalar kernel), of this pool planned: HOST int64 [DK_PLAN_FIELDS].  DK_ERR_INVALID before the first of them.
+ * What the last attention call that was enqueued (dk_scored_attend among them), or the last dk_attend_workspace_bytes()
+ * (which leaves no short sequences to the scalar kernel), of this pool planned: HOST int64 [DK_PLAN_FIELDS].  DK_ERR_INVALID
+ * before the first of them.
  */
 enum { DK_ROUTE_SCALAR = 0, DK_ROUTE_TILE = 1, DK_ROUTE_GENERAL = 2, DK_ROUTE_F32 = 3, DK_ROUTE_SCORED = 4 };
 enum {

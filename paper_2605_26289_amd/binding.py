@@ -1,4 +1,5 @@
-"""ctypes binding of libdeltakv: argument marshalling only.
+"""ctypes binding of libdeltakv: argument marshalling, and for scored attention, rotations and log probabilities the checks of
+types, sizes and layout that the library, handed bare pointers, cannot make.
 
 Function names mirror the C ABI (include/deltakv.h) without the dk_ prefix.  Device memory and
 streams come from PyTorch; nothing is computed here.  If the shared library has not been built,
@@ -189,7 +190,7 @@ def _dtypes():
     global _DTYPES, _torch
     if _DTYPES is None:
         import torch
-        _DTYPES, _torch = ((torch.float32, torch.bfloat16), torch.int32, torch.int64), torch
+        _torch, _DTYPES = torch, ((torch.float32, torch.bfloat16), torch.int32, torch.int64)  # (in this order: other threads look at the second)
     return _DTYPES
 
 
