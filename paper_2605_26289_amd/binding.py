@@ -199,7 +199,7 @@ def _buffer(t, dtype, least: int, device: int, where: str, what: str) -> Optiona
     handed are bare pointers."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.numel() < least or not t.is_contiguous() or t.get_device() != device or device < 0:
+    if t.dtype is not dtype or t.numel() < least or not t.is_contiguous() or t.get_device() != device:
         raise DeltaKVError(-1, where, f"{what}: {least} or more contiguous elements of {dtype} on the GPU of the others")
     return t.data_ptr()
 
@@ -212,6 +212,14 @@ def _tokens(s_arr, c_arr, where: str) -> int:
     if len(c_arr) <= n:
         raise DeltaKVError(-1, where, "cu_delta has one element more than there are sequences")
     return c_arr.item(n)
+
+
+def _gpu_of(t, where: str) -> int:
+    """The GPU that a call's first tensor is on"""
+    device = t.get_device()
+    if device < 0:
+        raise DeltaKVError(-1, where, "tensors are on a GPU")
+    return device
 
 
 def _stream_on(device: int, stream, where: str) -> Optional[int]:
@@ -462,7 +470,7 @@ def scored_attend(pool, slots, cu_delta, q, out, scale: float, scores: Scores, k
     n = _tokens(s_arr, c_arr, where)
     hq, hkv, d, code = pool.shape
     scores.check(len(s_arr), n, hq)
-    kind, dev = _dtypes()[0], q.get_device()
+    kind, dev = _dtypes()[0], _gpu_of(q, where)
     if scores.slopes is not None and scores.slopes.get_device() != dev:
         raise DeltaKVError(-1, where, "slopes are on the GPU of the others")
     args = (pool, len(s_arr), s_p, c_p, _buffer(q, kind[code], n * hq * d, dev, where, "q"),
@@ -495,14 +503,19 @@ class Rotary:
         if len(on) > 1:
             raise DeltaKVError(-1, "rotary", "frequencies and weights are on one GPU")
         self.device = on.pop() if on else None
+        self.fits = None  # what check() has found it to fit last
         self.desc = RotaryDesc(rotary_dim, int(pairs), _ptr(inv_freq), amplitude, int(norm_eps is not None), norm_eps or 0.0,
                                _ptr(q_weight), _ptr(k_weight))
         self.address = C.addressof(self.desc)
 
     def check(self, dtype, head_dim: int, device: int, where: str) -> None:
         """Whether frequencies and weights fit a call's rows, which the library cannot see."""
+        rows = (dtype, head_dim, device)
+        if self.fits == rows:
+            return
         if (self.dtype is not None and self.dtype is not dtype) or self.widest < head_dim or (self.device is not None and self.device != device):
             raise DeltaKVError(-1, where, "weights are head_dim elements of the rows' type, on their GPU as the frequencies are")
+        self.fits = rows
 
 
 def _heads(t, where: str):
@@ -519,10 +532,15 @@ def _heads(t, where: str):
 
 def _pool_rows(t, dtype, tokens: int, elements: int, device: int, where: str):
     """(address, elements from token to token) of at least that many tokens of so many elements each, as the pool has them"""
-    n, heads, width, address, step = _heads(t, where)
-    if t.dtype is not dtype or n < tokens or heads * width != elements or t.get_device() != device or device < 0:
-        raise DeltaKVError(-1, where, f"rows are {tokens} or more tokens of {elements} elements of {dtype}, on one GPU")
-    return address, step
+    shape, strides = t.shape, t.stride()
+    if len(shape) == 3:
+        n, heads, width = shape
+        step, head_step, one = strides
+        if ((one == 1 and (head_step == width or heads == 1)) or not t.numel()) and t.dtype is dtype and n >= tokens \
+                and heads * width == elements and t.get_device() == device:
+            return t.data_ptr(), (step if n > 1 else elements)
+    raise DeltaKVError(-1, where, f"rows are [tokens, heads, head_dim], {tokens} or more tokens of {elements} contiguous elements of "
+                                  f"{dtype}, on one GPU")
 
 
 def rotate_append(pool, slots, cu_delta, q, k, v, rotary: Rotary, q_out, stream=None) -> None:
@@ -532,7 +550,7 @@ def rotate_append(pool, slots, cu_delta, q, k, v, rotary: Rotary, q_out, stream=
     c_arr, c_p = _array(cu_delta)
     n = _tokens(s_arr, c_arr, where)
     hq, hkv, d, code = pool.shape
-    dtype, dev = _dtypes()[0][code], q.get_device()
+    dtype, dev = _dtypes()[0][code], _gpu_of(q, where)
     rotary.check(dtype, d, dev, where)
     _launch(lib().dk_rotate_append, (pool, len(s_arr), s_p, c_p, rotary.address, *_pool_rows(q, dtype, n, hq * d, dev, where),
                                      *_pool_rows(k, dtype, n, hkv * d, dev, where), *_pool_rows(v, dtype, n, hkv * d, dev, where),
@@ -551,7 +569,7 @@ def rotate_rows(positions, q, k, rotary: Rotary, q_out, k_out, stream=None) -> N
             args += (0, None, 0, None)
             continue
         n, heads, width, address, step = _heads(x, where)
-        kind, on = x.dtype, x.get_device()
+        kind, on = x.dtype, _gpu_of(x, where)
         if dtype is None:
             if kind is not f32 and kind is not bf16:
                 raise DeltaKVError(-1, where, "rows are float32 or bfloat16")
@@ -593,14 +611,14 @@ def token_logprobs(total_rows: int, logits, dtype: int, vocab: int, row_stride: 
     where = "token_logprobs"
     rows, n_top = int(total_rows), int(n_top)
     kinds, int32, _ = _dtypes()
-    shape, dev = logits.shape, logits.get_device()
+    shape, dev = logits.shape, _gpu_of(logits, where)
     if len(shape) == 2:
         step, one = logits.stride()
         fits = shape[0] >= rows and shape[1] >= vocab and (one == 1 or vocab == 1) and (rows <= 1 or step == row_stride)
     else:
         fits = logits.is_contiguous() and (rows == 0 or logits.numel() >= (rows - 1) * row_stride + vocab)
-    if not fits or dev < 0:
-        raise DeltaKVError(-1, where, "logits are [total_rows, vocab] on a GPU, row_stride elements from row to row")
+    if not fits:
+        raise DeltaKVError(-1, where, "logits are [total_rows, vocab], row_stride elements from row to row")
     if dtype in (F32, BF16) and logits.dtype is not kinds[dtype]:
         raise DeltaKVError(-1, where, "logits are of the type that dtype says")
     f32 = kinds[F32]
