@@ -10,7 +10,7 @@
  *     throws, aborts or prints;
  *   - a call that fails leaves the pool's state unchanged;
  *   - calls that launch GPU work (dk_kv_append, dk_delta_attend, dk_append_attend, their _sized
- *     forms, dk_delta_attend_noalloc, dk_scored_attend, dk_rotate_append, dk_rotate_rows,
+ *     forms, dk_delta_attend_noalloc, dk_scored_attend, dk_shared_attend, dk_rotate_append, dk_rotate_rows,
  *     dk_seq_gather, dk_verify_greedy, dk_token_logprobs) are
  *     asynchronous on the HIP stream passed as `stream` (a hipStream_t cast to void*,
  *     NULL = the default stream).  They never wait for the device and never allocate
@@ -284,6 +284,25 @@ int32_t dk_scored_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
                          void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
+ * shared_attend: dk_delta_attend for batches whose slots share cells (dk_seq_alias, the radix cache, dk_seq_reorder): keys that several
+ * entries see through the same cells are read and multiplied once for the rows of all of them.  Which these are is found from the
+ * slots' cells, whatever the order of the batch: prefixes of prefixes, any number of groups, entries that share nothing.  A range is
+ * shared where that is the faster way (entries of a hundred and more packed rows fill the matrix units by themselves, and prefixes of a
+ * few hundred positions cost more to join than to read again); the results' meaning does not depend on it.
+ * Arguments, modes and results as in dk_delta_attend, with these differences: scale may be any finite number; every softmax weight of a
+ * bf16 pool is rounded once to bf16 before it meets V, as in dk_scored_attend; q, out, k_new and v_new are 16-byte aligned (else
+ * DK_ERR_UNSUPPORTED); out and lse overlap neither one another nor the inputs (DK_ERR_INVALID); new tokens are never shared, not even
+ * by slots that alias them; the call needs no staging memory, never returns DK_ERR_BUSY, and can always be captured into a graph: its
+ * descriptors (some 50 bytes a sequence and 12 for each of its runs of cells) travel in the arguments of its launches, one more
+ * launch for every 3.75 KiB of them beyond the first 3.5.  The workspace is at least dk_shared_workspace_bytes() for the same batch, lengths,
+ * cells and mode (staged = 0 or 1).  Fewer than 2^31 / (query heads a KV head)^2 tokens and 2^29 positions (DK_ERR_UNSUPPORTED).
+ */
+int32_t dk_shared_workspace_bytes(dk_pool* pool, int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta, int32_t staged,
+                                  int64_t* bytes_out);
+int32_t dk_shared_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta, const void* q, const void* k_new,
+                         const void* v_new, float scale, void* out, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
  * Rotary positions, with norms of queries and keys in the same pass.  Of every head x of Q and K:
  *   y = x / sqrt(mean(x^2) + eps) * weight           if norm (weight NULL: ones)
  *   the first rotary_dim elements of y in pairs (a, b), pair i turned by the angle t = position * inv_freq[i]:
@@ -480,17 +499,19 @@ int32_t dk_seq_stats(dk_pool* pool, int32_t slot, int64_t* segments_out, int64_t
 int32_t dk_staging_wait(dk_pool* pool);
 
 /*
- * What the last attention call that was enqueued (dk_scored_attend among them), or the last dk_attend_workspace_bytes()
+ * What the last attention call that was enqueued (dk_scored_attend and dk_shared_attend among them), or the last dk_attend_workspace_bytes()
  * (which leaves no short sequences to the scalar kernel), of this pool planned: HOST int64 [DK_PLAN_FIELDS].  DK_ERR_INVALID
  * before the first of them.
  */
-enum { DK_ROUTE_SCALAR = 0, DK_ROUTE_TILE = 1, DK_ROUTE_GENERAL = 2, DK_ROUTE_F32 = 3, DK_ROUTE_SCORED = 4 };
+enum { DK_ROUTE_SCALAR = 0, DK_ROUTE_TILE = 1, DK_ROUTE_GENERAL = 2, DK_ROUTE_F32 = 3, DK_ROUTE_SCORED = 4, DK_ROUTE_SHARED = 5 };
 enum {
   DK_PLAN_ROUTE = 0,        /* scalar kernel; tile, general or fp32 kernel, each of the first two beside the streaming kernel;
-                               the kernels of dk_scored_attend */
-  DK_PLAN_ROW_ITEMS = 1,    /* work items of the tile, block or fp32 kernel; of dk_scored_attend's kernel for many rows */
-  DK_PLAN_STREAM_ITEMS = 2, /* work items of the streaming kernel; of dk_scored_attend's kernel for few rows */
-  DK_PLAN_MERGES = 3,       /* row tiles whose key range is split */
+                               the kernels of dk_scored_attend; those of dk_shared_attend */
+  DK_PLAN_ROW_ITEMS = 1,    /* work items of the tile, block or fp32 kernel; of dk_scored_attend's kernel for many rows;
+                               of dk_shared_attend, those of ranges that more than 64 packed rows see */
+  DK_PLAN_STREAM_ITEMS = 2, /* work items of the streaming kernel; of dk_scored_attend's kernel for few rows;
+                               of dk_shared_attend, all others */
+  DK_PLAN_MERGES = 3,       /* row tiles whose key range is split; dk_shared_attend: entries whose rows are joined from pieces */
   DK_PLAN_BYTES = 4,        /* workspace */
   DK_PLAN_FIELDS = 5
 };
@@ -529,7 +550,7 @@ int32_t dk_set_attend_variant(dk_pool* pool, int32_t variant);
 int32_t dk_set_tuning(dk_pool* pool, const char* name, double value);
 /*
  * Device time of the attention work (tile, streaming and merge kernels; not the descriptor upload) of recent
- * dk_delta_attend, dk_append_attend and dk_scored_attend calls on this pool, measured with HIP events recorded on the call's stream.
+ * dk_delta_attend, dk_append_attend, dk_scored_attend and dk_shared_attend calls on this pool, measured with HIP events recorded on the call's stream.
  * dk_set_attend_timing(pool, n): keep the last n calls (0 <= n <= 256; 0 switches recording off).
  * dk_attend_times: waits for the recorded work, then writes the durations in milliseconds, oldest
  * first, of the last min(cap, recorded) calls to ms_out (HOST float [cap]); *n_out receives the count.
@@ -542,7 +563,7 @@ int32_t dk_last_attend_ms(dk_pool* pool, float* ms_out);
 /*
  * Host time the launching calls of this pool have spent, by phase, in microseconds since the last reset
  * (a profiling probe: a few clock reads per call).  us_out HOST double [DK_HOST_PHASES] indexed by the
- * enum below, calls_out HOST int64 [2]: number of attention calls (dk_scored_attend among them, under delta_attend below) and
+ * enum below, calls_out HOST int64 [2]: number of attention calls (dk_scored_attend and dk_shared_attend among them, under delta_attend below) and
  * of appends (dk_rotate_append among them, under kv_append below).
  * Each pointer nullable; reset != 0 clears the sums.
  */

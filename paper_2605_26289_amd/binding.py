@@ -95,6 +95,9 @@ SIGNATURES = {
     "dk_scored_workspace_bytes": (C.c_int32, [C.c_void_p, C.c_int32, _ARRAY, _ARRAY, C.c_int32, C.c_void_p, _I64P]),
     "dk_scored_attend": (C.c_int32, [C.c_void_p, C.c_int32, _ARRAY, _ARRAY, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
                                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
+    "dk_shared_workspace_bytes": (C.c_int32, [C.c_void_p, C.c_int32, _ARRAY, _ARRAY, C.c_int32, _I64P]),
+    "dk_shared_attend": (C.c_int32, [C.c_void_p, C.c_int32, _ARRAY, _ARRAY, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
     "dk_rotate_append": (C.c_int32, [C.c_void_p, C.c_int32, _ARRAY, _ARRAY, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p,
                                      C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
     "dk_rotate_rows": (C.c_int32, [C.c_int32, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
@@ -389,7 +392,7 @@ def append_attend(pool, slots, cu_delta, q, k_new, v_new, out, scale: float, lse
                                      _ptr(lse), _ptr(workspace), ws_bytes, _stream(stream)), "append_attend", pool)
 
 
-ROUTES = ("scalar", "tile", "general", "f32", "scored")
+ROUTES = ("scalar", "tile", "general", "f32", "scored", "shared")
 
 
 def last_plan(pool) -> dict:
@@ -478,6 +481,32 @@ def scored_attend(pool, slots, cu_delta, q, out, scale: float, scores: Scores, k
             float(scale), scores.address, _buffer(out, kind[code], n * hq * d, dev, where, "out"),
             _buffer(lse, kind[F32], n * hq, dev, where, "lse"), *_room(workspace, dev, where), _stream_on(dev, stream, where))
     _launch(lib().dk_scored_attend, args, where, pool)
+
+
+def shared_workspace_bytes(pool, slots, cu_delta, staged) -> int:
+    s_arr, s_p = _array(slots)
+    c_arr, c_p = _array(cu_delta)
+    _tokens(s_arr, c_arr, "shared_workspace_bytes")
+    out = C.c_int64()
+    _check(lib().dk_shared_workspace_bytes(pool, len(s_arr), s_p, c_p, int(staged), C.byref(out)), "shared_workspace_bytes", pool)
+    return out.value
+
+
+def shared_attend(pool, slots, cu_delta, q, out, scale: float, k_new=None, v_new=None, lse=None, workspace=None, stream=None) -> None:
+    """Rows are contiguous and of the pool's type: q, out [tokens, query heads, head_dim], k_new, v_new [tokens, KV heads, head_dim]."""
+    where = "shared_attend"
+    s_arr, s_p = _array(slots)
+    c_arr, c_p = _array(cu_delta)
+    n = _tokens(s_arr, c_arr, where)
+    hq, hkv, d, code = pool.shape
+    kind, dev = _dtypes()[0], _gpu_of(q, where)
+    args = (pool, len(s_arr), s_p, c_p, _buffer(q, kind[code], n * hq * d, dev, where, "q"),
+            _buffer(k_new, kind[code], n * hkv * d, dev, where, "k_new"), _buffer(v_new, kind[code], n * hkv * d, dev, where, "v_new"),
+            float(scale), _buffer(out, kind[code], n * hq * d, dev, where, "out"), _buffer(lse, kind[F32], n * hq, dev, where, "lse"),
+            *_room(workspace, dev, where), _stream_on(dev, stream, where))
+    rc = lib().dk_shared_attend(*args)
+    if rc != OK:
+        _check(rc, where, pool)
 
 
 class Rotary:

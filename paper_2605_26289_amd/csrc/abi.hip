@@ -18,8 +18,10 @@
 #include "kernels.hpp"
 #include "plan.hpp"
 #include "plan_scored.hpp"
+#include "plan_shared.hpp"
 #include "pool.hpp"
 #include "radix.hpp"
+#include "shared_kernels.hpp"
 
 namespace {
 
@@ -84,8 +86,11 @@ struct dk_pool {
   int64_t last_plan[DK_PLAN_FIELDS] = {-1};  // see dk_last_plan
   dk::ScoredConfig scored_cfg;
   dk::ScoredPlan scored_plan;  // likewise, for dk_scored_attend
+  dk::SharedConfig shared_cfg;
+  dk::SharedPlan shared_plan;  // likewise, for dk_shared_attend
   std::vector<int64_t> append_cells, append_old_len;  // likewise, for the bookkeeping of appends
   std::vector<dk::Extent> append_runs;
+  std::vector<char> shared_blob;
 
   dk_pool(const dk_pool_desc& d, int32_t granule)
       : desc(d), meta(d.n_slots, d.n_session_slots, d.arena_cells, granule), granule_cells(granule) {}
@@ -136,6 +141,14 @@ struct dk_pool {
     last_plan[DK_PLAN_STREAM_ITEMS] = (int64_t)scored_plan.few.size();
     last_plan[DK_PLAN_MERGES] = (int64_t)scored_plan.merges.size();
     last_plan[DK_PLAN_BYTES] = (int64_t)scored_plan.total_bytes;
+  }
+
+  void keep_shared_plan() {
+    last_plan[DK_PLAN_ROUTE] = DK_ROUTE_SHARED;
+    last_plan[DK_PLAN_ROW_ITEMS] = shared_plan.row_items;
+    last_plan[DK_PLAN_STREAM_ITEMS] = shared_plan.items - shared_plan.row_items;
+    last_plan[DK_PLAN_MERGES] = (int64_t)shared_plan.merges.size() - 1;
+    last_plan[DK_PLAN_BYTES] = (int64_t)shared_plan.total_bytes;
   }
 
   int32_t hip_fail(hipError_t e) {
@@ -290,6 +303,10 @@ int32_t dk_pool_create(const dk_pool_desc* desc, dk_pool** pool_out) {
     p->scored_cfg.head_dim = desc->head_dim;
     p->scored_cfg.bf16 = desc->dtype == DK_BF16;
     p->scored_cfg.once_cells = p->cfg.once_cells;
+    p->shared_cfg.n_q_heads = desc->n_q_heads;
+    p->shared_cfg.n_kv_heads = desc->n_kv_heads;
+    p->shared_cfg.head_dim = desc->head_dim;
+    p->shared_cfg.bf16 = desc->dtype == DK_BF16;
     p->arrival_slice = take_slice();
     *pool_out = p;
     return DK_OK;
@@ -995,6 +1012,127 @@ int32_t dk_scored_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     if (e != hipSuccess) return pool->hip_fail(e);
     pool->ev_calls += timing;
     pool->keep_scored_plan();
+    pool->host_us[DK_HOST_LAUNCH] += clk.lap();
+    ++pool->host_calls[0];
+    return DK_OK;
+  });
+}
+
+}  // extern "C"
+
+extern "C" {
+
+int32_t dk_shared_workspace_bytes(dk_pool* pool, int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta, int32_t staged,
+                                  int64_t* bytes_out) {
+  if (!pool || !bytes_out || staged < 0 || staged > 1) return DK_ERR_INVALID;
+  return guarded([&]() -> int32_t {
+    std::lock_guard<std::mutex> launch(pool->launch_mu);
+    std::lock_guard<std::mutex> lk(pool->meta.mutex());
+    const int32_t rc = dk::build_shared_plan(pool->meta, pool->shared_cfg, n_seqs, slots, cu_delta, staged != 0, &pool->shared_plan);
+    if (rc == DK_OK) *bytes_out = (int64_t)pool->shared_plan.total_bytes;
+    return rc;
+  });
+}
+
+int32_t dk_shared_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta, const void* q, const void* k_new,
+                         const void* v_new, float scale, void* out, float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!pool || (k_new == nullptr) != (v_new == nullptr) || !(scale >= -FLT_MAX && scale <= FLT_MAX)) return DK_ERR_INVALID;
+  return guarded([&]() -> int32_t {
+    std::lock_guard<std::mutex> launch(pool->launch_mu);
+    PhaseClock clk;
+    hipStream_t st = (hipStream_t)stream;
+    const dk_pool_desc& d = pool->desc;
+    dk::SharedPlan& plan = pool->shared_plan;
+    {
+      std::lock_guard<std::mutex> lk(pool->meta.mutex());
+      const int32_t rc = dk::build_shared_plan(pool->meta, pool->shared_cfg, n_seqs, slots, cu_delta, k_new != nullptr, &plan);
+      if (rc != DK_OK) return rc;
+    }
+    if (plan.total_tokens == 0) return DK_OK;
+    if (!q || !out) return DK_ERR_INVALID;
+    // rows move in pieces of 16 bytes, a staged one is found by a 24-bit multiplication
+    if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)k_new | (uintptr_t)v_new) & 15) return DK_ERR_UNSUPPORTED;
+    if ((int64_t)d.n_kv_heads * d.head_dim * 4 >= (1 << 24)) return DK_ERR_UNSUPPORTED;
+    // (rows that are not finite have Q and V read again when their output has been written once)
+    const int64_t elem = d.dtype == DK_BF16 ? 2 : 4, q_row = (int64_t)d.n_q_heads * d.head_dim, k_row = (int64_t)d.n_kv_heads * d.head_dim;
+    const Span to = span_of(out, plan.total_tokens, q_row, q_row, elem), sums = span_of(lse, plan.total_tokens, d.n_q_heads, d.n_q_heads, 4);
+    for (const Span& from : {span_of(q, plan.total_tokens, q_row, q_row, elem), span_of(k_new, plan.total_tokens, k_row, k_row, elem),
+                             span_of(v_new, plan.total_tokens, k_row, k_row, elem)})
+      if (overlap(to, from) || overlap(sums, from)) return DK_ERR_INVALID;
+    if (overlap(to, sums)) return DK_ERR_INVALID;
+    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < (int64_t)plan.total_bytes) return DK_ERR_WORKSPACE;
+    pool->host_us[DK_HOST_PLAN] += clk.lap();
+    // The two kernels' descriptors travel in their arguments, or go to the workspace in those of launches of their own: either way the
+    // call can be captured, and needs no staging memory.
+    const bool in_args = plan.in_args();
+    dk::SharedBlob main_blob{}, merge_blob{};
+    std::vector<char>& bytes = pool->shared_blob;
+    char *h = (char*)&main_blob, *hm = (char*)&merge_blob;
+    if (!in_args) {
+      bytes.resize(plan.main_bytes + plan.merge_bytes);
+      h = bytes.data();
+      hm = h + plan.off_merge;
+    }
+    const auto put = [](char* at, const void* src, size_t n) { if (n) std::memcpy(at, src, n); };
+    put(h, plan.starts.data(), plan.starts.size() * sizeof(int32_t));
+    put(h + plan.off_nodes, plan.out_nodes.data(), plan.out_nodes.size() * sizeof(DkShNode));
+    put(h + plan.off_segs, plan.segs.data(), plan.segs.size() * sizeof(DkShSeg));
+    put(h + plan.off_tokens, plan.tokens.data(), plan.tokens.size() * sizeof(int32_t));
+    put(hm, plan.merges.data(), plan.merges.size() * sizeof(DkShMerge));
+    put(hm + plan.off_sources, plan.sources.data(), plan.sources.size() * sizeof(DkShSource));
+    pool->host_us[DK_HOST_STAGE] += clk.lap();
+    hipError_t e = hipSuccess;
+    if (!in_args) {
+      dk::SharedCarry piece;
+      for (size_t at = 0; at < bytes.size() && e == hipSuccess; at += sizeof(piece)) {
+        const size_t n = std::min(sizeof(piece), bytes.size() - at);
+        std::memcpy(&piece, bytes.data() + at, n);
+        e = dk::launch_shared_carry(piece, (char*)workspace + at, (int32_t)n, st);
+      }
+      if (e != hipSuccess) return pool->hip_fail(e);
+    }
+    pool->host_us[DK_HOST_UPLOAD] += clk.lap();
+    const uintptr_t desc = in_args ? 0 : (uintptr_t)workspace, merge_desc = in_args ? 0 : desc + plan.off_merge;
+    dk::SharedArgs a{};
+    a.starts = (const int32_t*)desc;
+    a.nodes = (const DkShNode*)(desc + plan.off_nodes);
+    a.segs = (const DkShSeg*)(desc + plan.off_segs);
+    a.tokens = (const int32_t*)(desc + plan.off_tokens);
+    a.q = q;
+    a.k_arena = d.k_arena;
+    a.v_arena = d.v_arena;
+    a.k_new = k_new;
+    a.v_new = v_new;
+    a.out = out;
+    a.lse = lse;
+    a.parts = (float*)((char*)workspace + plan.off_parts);
+    a.parts_ml = a.parts + (size_t)plan.part_rows * d.n_kv_heads * d.head_dim;
+    a.arena_cells = pool->meta_arena_cells;
+    const double c = (double)scale * 1.4426950408889634;
+    a.c = (float)std::min<double>(std::max<double>(c, -FLT_MAX), FLT_MAX);
+    a.f32 = d.dtype == DK_F32;
+    if (!a.f32) {  // (a scale of nothing makes all scores alike, and so does the smallest)
+      a.flip = a.c < 0.f ? 0x80008000u : 0u;
+      a.c = std::max(std::fabs(a.c), FLT_MIN);
+    }
+    a.n_nodes = (int32_t)plan.out_nodes.size() - 1;
+    a.n_q_heads = d.n_q_heads;
+    a.n_kv_heads = d.n_kv_heads;
+    a.group = d.n_q_heads / d.n_kv_heads;
+    a.gmagic = a.group > 1 ? (uint32_t)(((1ull << 32) + a.group - 1) / a.group) : 0u;
+    a.in_args = in_args;
+    const dk::SharedMergeArgs ma{(const DkShMerge*)merge_desc, (const DkShSource*)(merge_desc + plan.off_sources), (int32_t)plan.merges.size() - 1,
+                                 plan.spread, a.f32 ? plan.tile_rows : dk::SHARED_TILE};
+    const bool timing = !pool->ev0.empty();
+    const size_t ev_slot = timing ? (size_t)(pool->ev_calls % (int64_t)pool->ev0.size()) : 0;
+    if (timing) e = hipEventRecord(pool->ev0[ev_slot], st);
+    if (e == hipSuccess)
+      e = dk::launch_attend_shared(in_args ? &main_blob : nullptr, in_args ? &merge_blob : nullptr, a, ma, d.head_dim, plan.items, plan.merge_blocks,
+                                   plan.tile_rows, st);
+    if (e == hipSuccess && timing) e = hipEventRecord(pool->ev1[ev_slot], st);
+    if (e != hipSuccess) return pool->hip_fail(e);
+    pool->ev_calls += timing;
+    pool->keep_shared_plan();
     pool->host_us[DK_HOST_LAUNCH] += clk.lap();
     ++pool->host_calls[0];
     return DK_OK;

@@ -1,0 +1,322 @@
+#include "plan_shared.hpp"
+
+#include <algorithm>
+#include <cmath>
+
+namespace dk {
+
+namespace {
+
+// What the cuts go by, in microseconds.
+constexpr double FIXED_US = 5.0;      // a work item without its keys
+constexpr double ROWS_KEY_US = 0.9 / 64;  // a key of a tile of 128 rows, two workgroups to a compute unit
+constexpr double FEW_KEY_US = 0.7 / 64;   // a key of a tile of up to 64 rows, 128-wide heads
+constexpr double F32_KEY_US = 1.0 / 64;
+constexpr double PART_US = 1.0e-3;    // a partial row of one KV head, written and read, a compute unit's share
+
+double key_us(const SharedConfig& cfg, int64_t rows) {
+  if (!cfg.bf16) return F32_KEY_US * cfg.head_dim / 128;
+  if (rows <= SHARED_FEW) return FEW_KEY_US * cfg.head_dim / 128;
+  return ROWS_KEY_US * cfg.head_dim / 128;
+}
+int64_t tile_rows(const SharedConfig& cfg, const SharedPlan& p, int64_t rows) {
+  if (!cfg.bf16) return p.tile_rows;
+  return rows <= SHARED_FEW ? SHARED_FEW : SHARED_TILE;
+}
+double tiles_us(const SharedConfig& cfg, const SharedPlan& p, int64_t rows) {  // a key for all rows
+  const int64_t tile = tile_rows(cfg, p, rows);
+  return key_us(cfg, rows) * (double)((rows + tile - 1) / tile);
+}
+
+struct Builder {
+  const SharedConfig& cfg;
+  const int32_t* cu;
+  bool staged;
+  SharedPlan* p;
+  int64_t group;
+
+  int64_t rows_of(int32_t entry) const { return (int64_t)(cu[entry + 1] - cu[entry]) * group; }
+  int64_t ext_end(int32_t entry) const { return p->ext0[(size_t)entry + 1]; }
+
+  // Segments of positions [lo, hi) of an entry's cells.
+  void add_segs(int32_t entry, int64_t lo, int64_t hi) {
+    for (int64_t i = p->ext0[(size_t)entry]; i < ext_end(entry); ++i) {
+      const Extent& x = p->ext[(size_t)i];
+      const int64_t a = std::max(lo, x.pos), b = std::min(hi, x.pos + x.len);
+      if (a < b) p->node_segs.push_back({(int32_t)(x.cell + a - x.pos), (int32_t)a, (int32_t)(b - a)});
+    }
+  }
+
+  // Whether the members' rows together over `keys` positions cost less than each entry's alone.
+  bool worth_sharing(int32_t begin, int32_t end, int64_t keys) const {
+    double alone = 0.0;
+    int64_t rows = 0;
+    for (int32_t i = begin; i < end; ++i) {
+      const int64_t r = rows_of(p->members[(size_t)i].entry);
+      rows += r;
+      alone += tiles_us(cfg, *p, r);
+    }
+    const double pieces = std::max(1.0, (double)keys / 512.0);
+    return (double)keys * (alone - tiles_us(cfg, *p, rows)) > FIXED_US + PART_US * pieces * (double)rows;
+  }
+
+  void add_own(const SharedPlan::Member& m, int64_t start) {
+    const int32_t b = m.entry, delta = cu[b + 1] - cu[b];
+    const int64_t n = p->n[(size_t)b];
+    SharedPlan::Node x{};
+    x.entry = b;
+    x.link = m.link;
+    x.seg0 = (int32_t)p->node_segs.size();
+    add_segs(b, start, staged ? n : n + delta);
+    if (staged) p->node_segs.push_back({~cu[b], (int32_t)n, delta});
+    x.nsegs = (int32_t)p->node_segs.size() - x.seg0;
+    x.d = {cu[b], (int32_t)rows_of(b), (int32_t)start, (int32_t)(n + delta - start), 0, 0, -1, (int32_t)n};
+    p->nodes.push_back(x);
+  }
+
+  void add_shared(int32_t begin, int32_t end, int64_t start, int64_t pos) {
+    SharedPlan::Node x{};
+    x.entry = x.link = -1;
+    x.seg0 = (int32_t)p->node_segs.size();
+    add_segs(p->members[(size_t)begin].entry, start, pos);
+    x.nsegs = (int32_t)p->node_segs.size() - x.seg0;
+    const int32_t tok0 = (int32_t)p->tokens.size();
+    int64_t rows = 0;
+    for (int32_t i = begin; i < end; ++i) {
+      SharedPlan::Member& m = p->members[(size_t)i];
+      p->links.push_back({(int32_t)p->nodes.size(), (int32_t)rows, m.link});
+      m.link = (int32_t)p->links.size() - 1;
+      for (int32_t t = cu[m.entry]; t < cu[m.entry + 1]; ++t) p->tokens.push_back(t);
+      rows += rows_of(m.entry);
+    }
+    x.d = {tok0, (int32_t)rows, (int32_t)start, (int32_t)(pos - start), 0, 0, 0, SHARED_ALL};
+    p->nodes.push_back(x);
+  }
+
+  // The tree of shared prefixes, from the roots down: members that agree on a position's cell stay together.
+  void build() {
+    p->tasks.clear();
+    if (!p->members.empty()) p->tasks.push_back({0, (int32_t)p->members.size(), 0, 0});
+    while (!p->tasks.empty()) {
+      SharedPlan::Task t = p->tasks.back();
+      p->tasks.pop_back();
+      if (t.end - t.begin == 1) {
+        add_own(p->members[(size_t)t.begin], t.start);
+        continue;
+      }
+      while (true) {  // as far as all of them have the same cells
+        int64_t step = INT64_MAX, cell = -1;
+        for (int32_t i = t.begin; i < t.end && step > 0; ++i) {
+          SharedPlan::Member& m = p->members[(size_t)i];
+          if (p->n[(size_t)m.entry] <= t.pos) {
+            step = 0;
+            break;
+          }
+          while (p->ext[(size_t)m.ext].pos + p->ext[(size_t)m.ext].len <= t.pos) ++m.ext;
+          const Extent& x = p->ext[(size_t)m.ext];
+          const int64_t here = x.cell + t.pos - x.pos;
+          if (cell >= 0 && here != cell) step = 0;
+          cell = here;
+          step = std::min(step, std::min(x.pos + x.len, p->n[(size_t)m.entry]) - t.pos);
+        }
+        if (step <= 0) break;
+        t.pos += step;
+      }
+      if (t.pos > t.start && worth_sharing(t.begin, t.end, t.pos - t.start)) {
+        add_shared(t.begin, t.end, t.start, t.pos);
+        t.start = t.pos;
+      }
+      // those that end here part from all others, the rest by their next cell
+      for (int32_t i = t.begin; i < t.end; ++i) {
+        SharedPlan::Member& m = p->members[(size_t)i];
+        if (p->n[(size_t)m.entry] <= t.pos) {
+          m.key = -1 - i;
+          continue;
+        }
+        while (p->ext[(size_t)m.ext].pos + p->ext[(size_t)m.ext].len <= t.pos) ++m.ext;
+        m.key = p->ext[(size_t)m.ext].cell + t.pos - p->ext[(size_t)m.ext].pos;
+      }
+      std::sort(p->members.begin() + t.begin, p->members.begin() + t.end, [](const SharedPlan::Member& a, const SharedPlan::Member& b) {
+        return a.key != b.key ? a.key < b.key : a.entry < b.entry;
+      });
+      for (int32_t i = t.begin; i < t.end;) {
+        int32_t j = i + 1;
+        while (j < t.end && p->members[(size_t)j].key == p->members[(size_t)i].key) ++j;
+        p->tasks.push_back({i, j, t.start, t.pos});
+        i = j;
+      }
+    }
+  }
+
+  // Pieces of every node if a work item may take `us`: the longest item, all items' time, pieces' partial rows.
+  struct Cut {
+    double longest = 0, all = 0, parts = 0;
+    int64_t items = 0;
+  };
+  int64_t chunk_of(const SharedPlan::Node& x, double us) const {
+    const double keys = (us - FIXED_US) / x.per_key;
+    int64_t chunk = std::max<int64_t>(128, ((int64_t)std::min(keys, 1e9) + 63) / 64 * 64);
+    const int64_t pieces = ((int64_t)x.d.keys + chunk - 1) / chunk;
+    return ((int64_t)x.d.keys + pieces - 1) / pieces / 64 * 64 + ((((int64_t)x.d.keys + pieces - 1) / pieces) % 64 ? 64 : 0);
+  }
+  Cut cut(double us) const {
+    Cut c;
+    for (const SharedPlan::Node& x : p->nodes) {
+      const int64_t chunk = chunk_of(x, us), pieces = (x.d.keys + chunk - 1) / chunk;
+      const double item = FIXED_US + x.per_key * (double)std::min<int64_t>(chunk, x.d.keys);
+      c.longest = std::max(c.longest, item);
+      c.all += x.tiles * (pieces * FIXED_US + x.per_key * (double)x.d.keys);
+      c.items += x.tiles * pieces;
+      if (pieces > 1 || x.entry < 0 || x.link >= 0) c.parts += (double)(pieces * x.d.rows);
+    }
+    return c;
+  }
+
+  void choose_pieces() {
+    const double at_once = std::max(1.0, (cfg.bf16 ? 512.0 : 256.0) / cfg.n_kv_heads);
+    double most = 0;
+    for (const SharedPlan::Node& x : p->nodes) most = std::max(most, FIXED_US + x.per_key * x.d.keys);
+    double best_us = most, best = 1e300;
+    for (double us = most; us > FIXED_US * 1.2; us *= 0.8) {
+      const Cut c = cut(us);
+      const double run = (double)c.items <= at_once ? c.longest : std::max(c.longest, c.all / at_once + 0.5 * c.longest);
+      const double est = run + PART_US * c.parts / at_once * 2 + (c.parts > 0 ? 3.0 : 0.0);
+      if (est < best) {
+        best = est;
+        best_us = us;
+      }
+      if (c.items > 64 * at_once) break;
+    }
+    for (SharedPlan::Node& x : p->nodes) {
+      x.d.chunk = (int32_t)chunk_of(x, best_us);
+      x.pieces = (x.d.keys + x.d.chunk - 1) / x.d.chunk;
+    }
+  }
+};
+
+size_t section(size_t& at, size_t bytes) {
+  const size_t off = at;
+  at = (at + bytes + 15) / 16 * 16;
+  return off;
+}
+
+}  // namespace
+
+int32_t build_shared_plan(Pool& pool, const SharedConfig& cfg, int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta, bool staged,
+                          SharedPlan* p) {
+  int32_t rc = pool.check_batch(n_seqs, slots, cu_delta);
+  if (rc != OK) return rc;
+  p->ext.clear();
+  p->ext0.clear();
+  p->n.clear();
+  p->members.clear();
+  p->links.clear();
+  p->nodes.clear();
+  p->node_segs.clear();
+  p->starts.clear();
+  p->out_nodes.clear();
+  p->segs.clear();
+  p->tokens.clear();
+  p->merges.clear();
+  p->sources.clear();
+  p->total_tokens = n_seqs ? cu_delta[n_seqs] : 0;
+  p->part_rows = p->items = p->row_items = 0;
+  const int64_t group = cfg.n_q_heads / cfg.n_kv_heads;
+  // packed row numbers are divided by the group by a multiplication that is exact while row * (group - 1) < 2^32
+  if (p->total_tokens >= (int64_t(1) << 31) / (group * group)) return ERR_UNSUPPORTED;
+  p->tile_rows = p->total_tokens * group <= 16 ? 16 : 32;
+  for (int32_t b = 0; b < n_seqs; ++b) {
+    const int32_t delta = cu_delta[b + 1] - cu_delta[b];
+    int64_t len = 0;
+    rc = pool.extents_locked(slots[b], &p->one, &len);
+    if (rc != OK) return rc;
+    if (!staged && delta > len) return ERR_INVALID;
+    if (len + delta >= SHARED_ALL / 2) return ERR_UNSUPPORTED;
+    p->ext0.push_back((int32_t)p->ext.size());
+    p->n.push_back(staged ? len : len - delta);
+    if (delta == 0) continue;
+    p->members.push_back({b, (int32_t)p->ext.size(), -1, 0});
+    p->ext.insert(p->ext.end(), p->one.begin(), p->one.end());
+  }
+  p->ext0.push_back((int32_t)p->ext.size());
+  Builder build{cfg, cu_delta, staged, p, group};
+  build.build();
+  for (SharedPlan::Node& x : p->nodes) {
+    const int64_t tile = tile_rows(cfg, *p, x.d.rows);
+    x.tiles = (int32_t)((x.d.rows + tile - 1) / tile);
+    x.per_key = (float)key_us(cfg, x.d.rows);
+  }
+  build.choose_pieces();
+  // longest items first
+  p->order.resize(p->nodes.size());
+  for (size_t i = 0; i < p->nodes.size(); ++i) {
+    p->order[i] = (int32_t)i;
+    SharedPlan::Node& x = p->nodes[i];
+    x.fixed = x.per_key * (float)std::min(x.d.chunk, x.d.keys);
+    if (x.entry < 0 || x.link >= 0 || x.pieces > 1) {
+      x.d.part0 = (int32_t)p->part_rows;
+      p->part_rows += (int64_t)x.pieces * x.d.rows;
+      if (p->part_rows > INT32_MAX / 2) return ERR_UNSUPPORTED;
+    }
+  }
+  std::stable_sort(p->order.begin(), p->order.end(), [&](int32_t a, int32_t b) { return p->nodes[(size_t)a].fixed > p->nodes[(size_t)b].fixed; });
+  for (const int32_t i : p->order) {
+    SharedPlan::Node& x = p->nodes[(size_t)i];
+    x.d.seg0 = (int32_t)p->segs.size();
+    p->segs.insert(p->segs.end(), p->node_segs.begin() + x.seg0, p->node_segs.begin() + x.seg0 + x.nsegs);
+    p->starts.push_back((int32_t)p->items);
+    p->out_nodes.push_back(x.d);
+    p->items += (int64_t)x.tiles * x.pieces;
+    if (x.d.rows > SHARED_FEW) p->row_items += (int64_t)x.tiles * x.pieces;
+    if (p->items > INT32_MAX / 64 / cfg.n_kv_heads) return ERR_UNSUPPORTED;
+  }
+  p->starts.push_back((int32_t)p->items);
+  DkShNode last{};
+  last.seg0 = (int32_t)p->segs.size();
+  p->out_nodes.push_back(last);
+  // merges: the rows of entries that have more than one partial row
+  int64_t merge_rows = 0, most = 0;
+  for (const SharedPlan::Node& x : p->nodes) {
+    if (x.entry < 0 || x.d.part0 < 0) continue;
+    merge_rows += x.d.rows;
+    int64_t all = x.pieces;
+    DkShMerge m{0, x.d.tok0, x.d.rows, (int32_t)p->sources.size(), x.d.part0, x.pieces, x.d.chunk, x.d.n + 1 - x.d.lo};
+    for (int32_t l = x.link; l >= 0; l = p->links[(size_t)l].before) {
+      const SharedPlan::Link& k = p->links[(size_t)l];
+      const SharedPlan::Node& y = p->nodes[(size_t)k.node];
+      p->sources.push_back({y.d.part0 + k.row0, y.d.rows, y.pieces});
+      all += y.pieces;
+    }
+    most = std::max(most, all);
+    p->merges.push_back(m);
+  }
+  // Lane groups share the partial rows of a row where there are too few rows to fill the chip otherwise.
+  const int64_t groups = 1024 / cfg.head_dim;
+  p->spread = 1;
+  while (p->spread < groups && 2 * p->spread <= most && merge_rows * cfg.n_kv_heads * p->spread < 8192) p->spread *= 2;
+  const int64_t rows_a_block = groups / p->spread;
+  int64_t blocks = 0;
+  for (DkShMerge& m : p->merges) {
+    m.block0 = (int32_t)blocks;
+    blocks += (m.rows + rows_a_block - 1) / rows_a_block;
+  }
+  if (blocks > INT32_MAX / 256 / cfg.n_kv_heads) return ERR_UNSUPPORTED;
+  p->merge_blocks = (int32_t)blocks;
+  p->merges.push_back({(int32_t)blocks, 0, 0, (int32_t)p->sources.size(), 0, 0, 64, 0});
+  size_t at = 0;
+  section(at, p->starts.size() * sizeof(int32_t));
+  p->off_nodes = section(at, p->out_nodes.size() * sizeof(DkShNode));
+  p->off_segs = section(at, p->segs.size() * sizeof(DkShSeg));
+  p->off_tokens = section(at, p->tokens.size() * sizeof(int32_t));
+  p->main_bytes = at;
+  at = 0;
+  section(at, p->merges.size() * sizeof(DkShMerge));
+  p->off_sources = section(at, p->sources.size() * sizeof(DkShSource));
+  p->merge_bytes = at;
+  p->off_merge = p->main_bytes;
+  p->off_parts = (p->main_bytes + p->merge_bytes + 255) / 256 * 256;
+  p->total_bytes = p->off_parts + (size_t)p->part_rows * cfg.n_kv_heads * (cfg.head_dim + 2) * sizeof(float) + 256;
+  return OK;
+}
+
+}  // namespace dk

@@ -147,6 +147,19 @@ class DevicePool:
             dk.scored_attend(self.handle, slots, cu_delta, q, out, scale, scores, k_new, v_new, lse, ws)
         return out
 
+    def shared_attend(self, slots, cu_delta, q, scale: float, k_new=None, v_new=None, out=None, lse=None):
+        """attend() with cells that several slots share read once for all of them (dk_shared_attend)."""
+        if out is None:
+            out = torch.empty_like(q)
+        try:
+            dk.shared_attend(self.handle, slots, cu_delta, q, out, scale, k_new, v_new, lse, self.workspace)
+        except dk.DeltaKVError as e:
+            if e.name != "WORKSPACE":
+                raise
+            ws = self._grow_workspace(dk.shared_workspace_bytes(self.handle, slots, cu_delta, k_new is not None))
+            dk.shared_attend(self.handle, slots, cu_delta, q, out, scale, k_new, v_new, lse, ws)
+        return out
+
     def rotate_append(self, slots, cu_delta, q, k, v, rotary: dk.Rotary, out=None):
         """Normalises and rotates Q and K by position, K and V into the slots' next cells; returns Q (dk_rotate_append)."""
         if out is None:
