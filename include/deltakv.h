@@ -10,8 +10,8 @@
  *     throws, aborts or prints;
  *   - a call that fails leaves the pool's state unchanged;
  *   - calls that launch GPU work (dk_kv_append, dk_delta_attend, dk_append_attend, their _sized
- *     forms, dk_delta_attend_noalloc, dk_scored_attend, dk_shared_attend, dk_rotate_append, dk_rotate_rows,
- *     dk_seq_gather, dk_verify_greedy, dk_token_logprobs) are
+ *     forms, dk_delta_attend_noalloc, dk_scored_attend, dk_shared_attend, dk_seq_reorder, dk_rotate_append, dk_rotate_rows,
+ *     dk_seq_gather, dk_verify_greedy, dk_token_logprobs, dk_beam_select) are
  *     asynchronous on the HIP stream passed as `stream` (a hipStream_t cast to void*,
  *     NULL = the default stream).  They never wait for the device and never allocate
  *     device or pinned memory: descriptors travel through the caller's staging memory
@@ -141,6 +141,21 @@ int32_t dk_seq_trim(dk_pool* pool, int32_t slot, int64_t new_len);
  * (a new_len above the slot's length) leave every slot as it was.
  */
 int32_t dk_seq_trim_batch(dk_pool* pool, int32_t n_seqs, const int32_t* slots, const int64_t* new_len);
+
+/*
+ * seq_reorder: every slots[i] becomes what slots[parents[i]] was before the call (the beams of a beam search after a selection: those
+ * that go on more than once, those that go on no more).  parents are indexes into slots; any number of slots may name the same one.
+ *   slots    HOST [n]  distinct acquired slot ids
+ *   parents  HOST [n]  each in [0, n)
+ * One child of a parent takes its cells over as they are (itself if it is among them); every other child shares those that fill
+ * whole granules, as after dk_seq_alias, and gets cells of its own for the rest, into which fewer than granule_cells tokens' K
+ * and V are copied on `stream`.  So a search's sequences stay in few runs of cells however long it goes on, what it copies does not
+ * depend on their length, and dk_shared_attend finds what they share.  Afterwards all of them grow independently.
+ * DK_ERR_INVALID (a parent out of range), DK_ERR_NO_SLOT, DK_ERR_DUP_SLOT, and DK_ERR_NO_CELLS unless the arena has a free granule for
+ * every copy -- cells of states that no slot has any more are free after the call, not during it -- leave every slot as it was.
+ * Cells are chosen at call time: a captured call replays its copies, not the bookkeeping.
+ */
+int32_t dk_seq_reorder(dk_pool* pool, int32_t n, const int32_t* slots, const int32_t* parents, void* stream);
 
 /*
  * kv_append: write new tokens' K and V into the slots' next cells (the cache write of
@@ -405,6 +420,31 @@ int32_t dk_logprobs_workspace_bytes(int32_t total_rows, int64_t vocab, int32_t d
 int32_t dk_token_logprobs(int32_t total_rows, const void* logits, int32_t dtype, int64_t vocab, int64_t row_stride, float scale,
                           const int32_t* tokens, float* logprob_out, int32_t* rank_out, float* entropy_out, int32_t n_top,
                           int32_t* top_ids_out, float* top_logprobs_out, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * beam_select: the best continuations of each request's beams.  Group g is the logits rows cu_rows[g] .. cu_rows[g+1]-1, its beams; of
+ * every one of its rows r and every token t
+ *   score(r, t) = scores[r] + scale * x[r][t] - ln sum_u exp(scale * x[r][u])
+ * the n_out largest are written in order, equal ones by the lower row, in a row by the larger logit and the lower token.  row_out
+ * names rows of the batch, so with one slot per row it gives the parents of dk_seq_reorder once the caller has chosen among the
+ * continuations (n_out may be twice the beams, so that those that end can be set aside).
+ *   cu_rows_dev   DEVICE int32 [n_groups+1], non-decreasing from 0 to total_rows; at most 64 rows a group (further ones are not looked
+ *                 at; offsets outside 0 .. total_rows are held to it)
+ *   logits        as for dk_token_logprobs
+ *   scores        DEVICE float [total_rows]: cumulative log probabilities.  A row takes part if its score is finite (-infinity: a beam
+ *                 that has ended, or not begun), its logits hold no NaN and no +infinity, and some of them are finite; a token whose
+ *                 logit is -infinity is no continuation
+ *   row_out, token_out  DEVICE int32 [n_groups, n_out];  score_out  DEVICE float [n_groups, n_out].  Where a group has fewer
+ *                 continuations the rest are -1, -1 and -infinity
+ *   scale         the inverse of the temperature, 2^-20 .. 2^20;  n_out  1 .. 64;  vocab <= 2^20 (DK_ERR_UNSUPPORTED otherwise)
+ *   workspace     DEVICE, 256-byte aligned, >= dk_beam_workspace_bytes() for the same arguments
+ * Scores are made and compared in fp64 from sums in fp32, 1e-7 of a log probability.  total_rows < 2^24, less than 2^35 logits in all.
+ * Asynchronous on `stream`; stateless, needs no pool; allocates nothing.
+ */
+int32_t dk_beam_workspace_bytes(int32_t total_rows, int64_t vocab, int32_t dtype, int32_t n_out, int64_t* bytes_out);
+int32_t dk_beam_select(int32_t n_groups, int32_t total_rows, const int32_t* cu_rows_dev, const void* logits, int32_t dtype, int64_t vocab,
+                       int64_t row_stride, double scale, const float* scores, int32_t n_out, int32_t* row_out, int32_t* token_out,
+                       float* score_out, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
  * Radix prefix cache and the per-turn procedure of paper Alg. 1 (Sec. 3.3), HOST only.  The trie is keyed

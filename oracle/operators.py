@@ -3,6 +3,7 @@
   scored_attend    attention of new tokens with capped scores, a bias by distance, and a range of positions for every row
   rotate           norm of a head and its rotation by position
   token_logprobs   log probability and rank of a token, entropy, best alternatives of a logits row
+  beam_select      the best continuations of groups of rows
 
 Everything is float64, loop by loop, with no tiling, fusion or reordering.
 """
@@ -94,3 +95,24 @@ def token_logprobs(logits, tokens, scale: float = 1.0, n_top: int = 0):
         ids[r] = np.lexsort((np.arange(vocab), -key[r]))[:n_top]
         tlp[r] = ln_p[ids[r]]
     return lp, rank, ent, ids, tlp
+
+
+def beam_select(logits, scores, cu_rows, n_out: int, scale: float = 1.0):
+    """(rows, tokens, scores) [groups, n_out]: every continuation of a group's live rows in one list, best first; equal ones by row, then
+    logit, then token."""
+    x = np.asarray(logits, dtype=np.float64)
+    groups = len(cu_rows) - 1
+    rows, tokens = np.full((groups, n_out), -1, dtype=np.int64), np.full((groups, n_out), -1, dtype=np.int64)
+    best = np.full((groups, n_out), -np.inf)
+    for g in range(groups):
+        every = []
+        for r in range(cu_rows[g], cu_rows[g + 1]):
+            if not np.isfinite(scores[r]) or np.isnan(x[r]).any() or not np.isfinite(x[r].max()):
+                continue
+            y = scale * (x[r] - x[r].max())
+            ln_z = math.log(np.exp(y).sum())
+            every += [(float(scores[r]) + (y[t] - ln_z), -r, x[r][t], -t) for t in range(x.shape[1]) if x[r][t] > -np.inf]
+        every.sort(reverse=True)
+        for j, (s, r, _, t) in enumerate(every[:n_out]):
+            rows[g, j], tokens[g, j], best[g, j] = -r, -t, s
+    return rows, tokens, best

@@ -88,6 +88,18 @@ class OraclePool:
             raise OracleError("INVALID")
         self.seqs[dst] = list(self.seqs[donor][:p1])  # same cell objects, new list
 
+    def reorder(self, slots, parents) -> None:
+        """Every slot becomes what its parent's was; which cells are shared afterwards is the library's choice, contents are not."""
+        for s in slots:
+            self._check(s)
+        if len(set(slots)) != len(slots):
+            raise OracleError("DUP_SLOT")
+        if len(parents) != len(slots) or any(p < 0 or p >= len(slots) for p in parents):
+            raise OracleError("INVALID")
+        before = [list(self.seqs[s]) for s in slots]
+        for s, p in zip(slots, parents):
+            self.seqs[s] = list(before[p])
+
     def trim(self, slot: int, new_len: int) -> None:
         self._check(slot)
         if new_len < 0 or new_len > len(self.seqs[slot]):

@@ -69,6 +69,7 @@ SIGNATURES = {
     "dk_seq_alias": (C.c_int32, [C.c_void_p, C.c_int32, C.c_int32, C.c_int64, C.c_int64]),
     "dk_seq_trim": (C.c_int32, [C.c_void_p, C.c_int32, C.c_int64]),
     "dk_seq_trim_batch": (C.c_int32, [C.c_void_p, C.c_int32, _ARRAY, _ARRAY]),
+    "dk_seq_reorder": (C.c_int32, [C.c_void_p, C.c_int32, _ARRAY, _ARRAY, C.c_void_p]),
     "dk_kv_append": (C.c_int32, [C.c_void_p, C.c_int32, _ARRAY, _ARRAY, _ARRAY, C.c_void_p, C.c_void_p, C.c_void_p]),
     "dk_kv_reserve": (C.c_int32, [C.c_void_p, C.c_int32, _ARRAY, _ARRAY, _ARRAY, _ARRAY]),
     "dk_attend_workspace_bytes": (C.c_int32, [C.c_void_p, C.c_int32, _ARRAY, _ARRAY, C.c_int32, _I64P]),
@@ -108,6 +109,9 @@ SIGNATURES = {
     "dk_token_logprobs": (C.c_int32, [C.c_int32, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_float, C.c_void_p,
                                       C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
                                       C.c_int64, C.c_void_p]),
+    "dk_beam_workspace_bytes": (C.c_int32, [C.c_int32, C.c_int64, C.c_int32, C.c_int32, _I64P]),
+    "dk_beam_select": (C.c_int32, [C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_double,
+                                   C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
     "dk_radix_create": (C.c_int32, [C.c_void_p, C.c_int64, C.c_int32, C.POINTER(C.c_void_p)]),
     "dk_radix_destroy": (C.c_int32, [C.c_void_p]),
     "dk_radix_begin_turn": (C.c_int32, [C.c_void_p, C.c_int32, _I32P, C.c_int64, _I64P]),
@@ -351,6 +355,17 @@ def kv_append(pool, slots, cu_delta, k_new, v_new, n_accept=None, stream=None) -
     a_arr, a_p = _array(n_accept)
     _launch(lib().dk_kv_append, (pool, len(s_arr), s_p, c_p, a_p, _ptr(k_new), _ptr(v_new), _stream(stream)),
             "kv_append", pool)
+
+
+def seq_reorder(pool, slots, parents, stream=None) -> None:
+    """Slot i of the list becomes what the slot at index parents[i] was."""
+    s_arr, s_p = _array(slots)
+    p_arr, p_p = _array(parents)
+    if s_arr.shape != p_arr.shape or s_arr.ndim != 1:
+        raise DeltaKVError(-1, "seq_reorder", "one parent for every slot")
+    rc = lib().dk_seq_reorder(pool, len(s_arr), s_p, p_p, _stream(stream))
+    if rc != OK:
+        _check(rc, "seq_reorder", pool)
 
 
 def kv_reserve(pool, slots, cu_delta, n_accept=None) -> np.ndarray:
@@ -626,6 +641,21 @@ def rotary_freqs(rotary_dim: int, base: float, scaling: int = ROTARY_PLAIN, para
     return out[: rotary_dim // 2], amplitude.value
 
 
+def _logits(logits, dtype: int, rows: int, vocab: int, row_stride: int, where: str) -> int:
+    """The GPU of logits that are what a call says of them."""
+    shape, dev = logits.shape, _gpu_of(logits, where)
+    if len(shape) == 2:
+        step, one = logits.stride()
+        fits = shape[0] >= rows and shape[1] >= vocab and (one == 1 or vocab == 1) and (rows <= 1 or step == row_stride)
+    else:
+        fits = logits.is_contiguous() and (rows == 0 or logits.numel() >= (rows - 1) * row_stride + vocab)
+    if not fits:
+        raise DeltaKVError(-1, where, "logits are [total_rows, vocab], row_stride elements from row to row")
+    if dtype in (F32, BF16) and logits.dtype is not _dtypes()[0][dtype]:
+        raise DeltaKVError(-1, where, "logits are of the type that dtype says")
+    return dev
+
+
 def logprobs_workspace_bytes(total_rows: int, vocab: int, dtype: int, n_top: int = 0) -> int:
     out = C.c_int64()
     _check(lib().dk_logprobs_workspace_bytes(int(total_rows), int(vocab), int(dtype), int(n_top), C.byref(out)),
@@ -640,16 +670,7 @@ def token_logprobs(total_rows: int, logits, dtype: int, vocab: int, row_stride: 
     where = "token_logprobs"
     rows, n_top = int(total_rows), int(n_top)
     kinds, int32, _ = _dtypes()
-    shape, dev = logits.shape, _gpu_of(logits, where)
-    if len(shape) == 2:
-        step, one = logits.stride()
-        fits = shape[0] >= rows and shape[1] >= vocab and (one == 1 or vocab == 1) and (rows <= 1 or step == row_stride)
-    else:
-        fits = logits.is_contiguous() and (rows == 0 or logits.numel() >= (rows - 1) * row_stride + vocab)
-    if not fits:
-        raise DeltaKVError(-1, where, "logits are [total_rows, vocab], row_stride elements from row to row")
-    if dtype in (F32, BF16) and logits.dtype is not kinds[dtype]:
-        raise DeltaKVError(-1, where, "logits are of the type that dtype says")
+    dev = _logits(logits, dtype, rows, vocab, row_stride, where)
     f32 = kinds[F32]
     _check(lib().dk_token_logprobs(rows, logits.data_ptr(), int(dtype), int(vocab), int(row_stride), float(scale),
                                    _buffer(tokens, int32, rows, dev, where, "tokens"), _buffer(logprob_out, f32, rows, dev, where, "logprob_out"),
@@ -658,6 +679,27 @@ def token_logprobs(total_rows: int, logits, dtype: int, vocab: int, row_stride: 
                                    _buffer(top_ids_out, int32, rows * n_top, dev, where, "top_ids_out"),
                                    _buffer(top_logprobs_out, f32, rows * n_top, dev, where, "top_logprobs_out"),
                                    *_room(workspace, dev, where), _stream_on(dev, stream, where)), where)
+
+
+def beam_workspace_bytes(total_rows: int, vocab: int, dtype: int, n_out: int) -> int:
+    out = C.c_int64()
+    _check(lib().dk_beam_workspace_bytes(int(total_rows), int(vocab), int(dtype), int(n_out), C.byref(out)), "beam_workspace_bytes")
+    return out.value
+
+
+def beam_select(n_groups: int, total_rows: int, cu_rows_dev, logits, dtype: int, vocab: int, row_stride: int, scores, n_out: int, row_out,
+                token_out, score_out, workspace, scale: float = 1.0, stream=None) -> None:
+    """All tensors are device tensors, contiguous but for logits, whose rows are row_stride elements apart; nothing is synchronised."""
+    where = "beam_select"
+    groups, rows, n = int(n_groups), int(total_rows), int(n_out)
+    (f32, _), int32, _ = _dtypes()
+    dev = _logits(logits, dtype, rows, vocab, row_stride, where)
+    _check(lib().dk_beam_select(groups, rows, _buffer(cu_rows_dev, int32, groups + 1, dev, where, "cu_rows_dev"), logits.data_ptr(), int(dtype),
+                                int(vocab), int(row_stride), float(scale), _buffer(scores, f32, rows, dev, where, "scores"), n,
+                                _buffer(row_out, int32, groups * n, dev, where, "row_out"),
+                                _buffer(token_out, int32, groups * n, dev, where, "token_out"),
+                                _buffer(score_out, f32, groups * n, dev, where, "score_out"), *_room(workspace, dev, where),
+                                _stream_on(dev, stream, where)), where)
 
 
 # -- host-only: radix prefix cache, prompt lookup, scheduler helpers ---------------------------------------

@@ -13,7 +13,7 @@ LIB = os.path.join(HERE, "libdeltakv.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 
 SOURCES = ["pool.cpp", "plan.cpp", "plan_scored.cpp", "plan_shared.cpp", "radix.cpp", "pld.cpp", "sched.cpp", "rotary_freqs.cpp", "abi.hip", "kernels_basic.hip", "attend_stream.hip", "attend_tile.hip", "attend_block.hip", "attend_f32.hip", "attend_scored.hip",
-           "attend_shared.hip", "verify.hip", "logprobs.hip", "rotary.hip"]
+           "attend_shared.hip", "verify.hip", "logprobs.hip", "beam.hip", "rotary.hip"]
 
 HIP_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",

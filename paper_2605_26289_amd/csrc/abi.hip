@@ -91,6 +91,7 @@ struct dk_pool {
   std::vector<int64_t> append_cells, append_old_len;  // likewise, for the bookkeeping of appends
   std::vector<dk::Extent> append_runs;
   std::vector<char> shared_blob;
+  dk::Pool::Reorder reordered;
 
   dk_pool(const dk_pool_desc& d, int32_t granule)
       : desc(d), meta(d.n_slots, d.n_session_slots, d.arena_cells, granule), granule_cells(granule) {}
@@ -482,6 +483,35 @@ int32_t dk_kv_reserve(dk_pool* pool, int32_t n_seqs, const int32_t* slots, const
     int32_t rc = pool->meta.append(n_seqs, slots, cu_delta, n_accept, &dst, nullptr);
     if (rc != DK_OK) return rc;
     for (int64_t t = 0; t < total; ++t) cells_out[t] = dst[t];
+    return DK_OK;
+  });
+}
+
+int32_t dk_seq_reorder(dk_pool* pool, int32_t n, const int32_t* slots, const int32_t* parents, void* stream) {
+  if (!pool) return DK_ERR_INVALID;
+  return guarded([&]() -> int32_t {
+    std::lock_guard<std::mutex> launch(pool->launch_mu);
+    // a launch's grid: two rows of workgroups for every copy's KV head
+    if (pool->desc.n_kv_heads > (1 << 23) / dk::KV_MAX_MOVES) return DK_ERR_UNSUPPORTED;
+    dk::Pool::Reorder& r = pool->reordered;
+    const int32_t rc = pool->meta.reorder(n, slots, parents, &r);
+    if (rc != DK_OK) return rc;
+    hipError_t e = hipSuccess;
+    dk::KvMoves moves;
+    for (size_t at = 0; at < r.moves.size() && e == hipSuccess; at += dk::KV_MAX_MOVES) {
+      const int32_t count = (int32_t)std::min<size_t>(dk::KV_MAX_MOVES, r.moves.size() - at);
+      for (int32_t i = 0; i < count; ++i) {
+        const dk::Pool::Move& m = r.moves[at + (size_t)i];
+        moves.move[i] = {(int32_t)m.from, (int32_t)m.to, (int32_t)m.len};
+      }
+      e = dk::launch_kv_moves(pool->view(), pool->desc.k_arena, pool->desc.v_arena, moves, count, (hipStream_t)stream);
+    }
+    if (e != hipSuccess) {
+      // (copies already enqueued wrote cells that no slot owns: harmless)
+      pool->meta.undo_reorder(n, slots, &r);
+      return pool->hip_fail(e);
+    }
+    pool->meta.settle_reorder(&r);
     return DK_OK;
   });
 }
@@ -1418,6 +1448,33 @@ int32_t dk_token_logprobs(int32_t total_rows, const void* logits, int32_t dtype,
   const dk::LogprobArgs a{logits, dtype, total_rows, vocab, row_stride, scale, n_top, tokens, logprob_out, rank_out, entropy_out,
                           top_ids_out, top_logprobs_out};
   const hipError_t e = dk::launch_token_logprobs(a, workspace, (hipStream_t)stream);
+  return e == hipSuccess ? DK_OK : DK_ERR_HIP;
+}
+
+int32_t dk_beam_workspace_bytes(int32_t total_rows, int64_t vocab, int32_t dtype, int32_t n_out, int64_t* bytes_out) {
+  if (!bytes_out || total_rows < 0 || vocab <= 0 || n_out <= 0) return DK_ERR_INVALID;
+  if ((dtype != DK_F32 && dtype != DK_BF16) || n_out > dk::BEAM_MAX_OUT || vocab > dk::BEAM_MAX_VOCAB) return DK_ERR_UNSUPPORTED;
+  if (total_rows >= (1 << 24) || (int64_t)total_rows * vocab >= (int64_t(1) << 35)) return DK_ERR_UNSUPPORTED;
+  *bytes_out = dk::beam_workspace_bytes(total_rows, vocab, dtype, n_out);
+  return DK_OK;
+}
+
+int32_t dk_beam_select(int32_t n_groups, int32_t total_rows, const int32_t* cu_rows_dev, const void* logits, int32_t dtype, int64_t vocab,
+                       int64_t row_stride, double scale, const float* scores, int32_t n_out, int32_t* row_out, int32_t* token_out,
+                       float* score_out, void* workspace, int64_t workspace_bytes, void* stream) {
+  int64_t need = 0;
+  const int32_t rc = dk_beam_workspace_bytes(total_rows, vocab, dtype, n_out, &need);
+  if (rc != DK_OK) return rc;
+  if (n_groups < 0 || row_stride < vocab || !(scale > 0.0) || !(scale <= DBL_MAX)) return DK_ERR_INVALID;
+  if (scale < 0x1p-20 || scale > 0x1p20 || n_groups >= (1 << 24)) return DK_ERR_UNSUPPORTED;  // products with a logit stay within the type
+  if (n_groups == 0) return DK_OK;
+  if (!cu_rows_dev || !row_out || !token_out || !score_out || (total_rows > 0 && (!logits || !scores))) return DK_ERR_INVALID;
+  const int64_t elem = dtype == DK_BF16 ? 2 : 4;
+  // rows are read with 16-byte loads
+  if (((uintptr_t)logits & 15) || (row_stride * elem) % 16) return DK_ERR_UNSUPPORTED;
+  if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return DK_ERR_WORKSPACE;
+  const dk::BeamArgs a{logits, dtype, n_groups, total_rows, vocab, row_stride, scale, cu_rows_dev, scores, n_out, row_out, token_out, score_out};
+  const hipError_t e = dk::launch_beam_select(a, workspace, (hipStream_t)stream);
   return e == hipSuccess ? DK_OK : DK_ERR_HIP;
 }
 

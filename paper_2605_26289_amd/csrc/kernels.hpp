@@ -44,6 +44,17 @@ static_assert(kv_runs_in_one_launch({nullptr, nullptr, 0, 8, 8, 128, 1}, 3355442
 hipError_t launch_kv_scatter_runs(const ArenaView& a, void* k_arena, void* v_arena, const KvRuns& runs, int32_t n_runs,
                                   int32_t n_tok, const void* k_new, const void* v_new, hipStream_t stream);
 
+// Copies inside the arena: `len` cells from `from` on to those from `to` on, K and V of all heads; no copy writes a cell that another one
+// reads.  At most this many travel in the arguments of a launch.
+struct KvMove {
+  int32_t from, to, len;
+};
+constexpr int32_t KV_MAX_MOVES = 320;
+struct KvMoves {
+  KvMove move[KV_MAX_MOVES];
+};
+hipError_t launch_kv_moves(const ArenaView& a, void* k_arena, void* v_arena, const KvMoves& moves, int32_t n_moves, hipStream_t stream);
+
 // Descriptors of at most INLINE_BLOB_BYTES are passed to the kernels inside their arguments instead of being
 // uploaded first: a short turn then costs no host-to-device copy (and no staging buffer).
 struct InlineBlob {
@@ -162,6 +173,24 @@ struct LogprobArgs {
 };
 int64_t logprobs_workspace_bytes(int32_t rows, int64_t vocab, int32_t dtype, int32_t n_top);
 hipError_t launch_token_logprobs(const LogprobArgs& a, void* workspace, hipStream_t stream);
+
+// The best continuations of groups of logits rows.
+constexpr int32_t BEAM_MAX_OUT = 64, BEAM_MAX_ROWS = 64;  // of a group
+constexpr int64_t BEAM_MAX_VOCAB = 1 << 20;
+struct BeamArgs {
+  const void* logits;
+  int32_t dtype, n_groups, rows;
+  int64_t vocab, row_stride;
+  double scale;
+  const int32_t* cu_rows;
+  const float* scores;
+  int32_t n_out;
+  int32_t* row_out;
+  int32_t* token_out;
+  float* score_out;
+};
+int64_t beam_workspace_bytes(int32_t rows, int64_t vocab, int32_t dtype, int32_t n_out);
+hipError_t launch_beam_select(const BeamArgs& a, void* workspace, hipStream_t stream);
 
 // Norms and rotation of Q and K.  Appends carry the runs of consecutive cells and positions that their tokens go to in the
 // kernel arguments, at most this many of them: run r is tokens tok[r] .. tok[r + 1] - 1, from cell[r] and pos[r] on.

@@ -132,6 +132,45 @@ hipError_t launch_kv_scatter_runs(const ArenaView& a, void* k_arena, void* v_are
   return hipGetLastError();
 }
 
+// Reordered states: what a child's state has beyond whole granules of its parent's, copied into cells of its own.  The cells of one KV
+// head are one run of bytes on either side, so a workgroup takes a piece of the run of one (move, head, K or V), four 16-byte loads a
+// lane on their way before the first store.  Bound by the launch: a granule's rest is at most 64 KiB a head.
+constexpr int KV_MOVE_LOADS = 4;
+static_assert(sizeof(KvMoves) + 96 <= 4096, "kernel arguments are limited to 4 KiB");
+__global__ __launch_bounds__(256) void kv_move_kernel(KvMoves moves, uint4* __restrict__ k_arena, uint4* __restrict__ v_arena,
+                                                      int32_t n_kv_heads, int32_t row_vec, int64_t arena_cells) {
+  // (`moves` starts the kernel-argument segment and is read through it, as above)
+  typedef const __attribute__((address_space(4))) KvMoves* const_moves_ptr;
+  const_moves_ptr table = (const_moves_ptr)__builtin_amdgcn_kernarg_segment_ptr();
+  (void)moves;
+  const int32_t job = (int32_t)(blockIdx.x >> 1), m = job / n_kv_heads, g = job - m * n_kv_heads;
+  const int64_t vecs = (int64_t)table->move[m].len * row_vec, at = (int64_t)g * arena_cells;
+  uint4* arena = blockIdx.x & 1 ? v_arena : k_arena;
+  const uint4* from = arena + (at + table->move[m].from) * row_vec;
+  uint4* to = arena + (at + table->move[m].to) * row_vec;
+  for (int64_t base = (int64_t)blockIdx.y * (256 * KV_MOVE_LOADS) + threadIdx.x; base < vecs; base += (int64_t)gridDim.y * (256 * KV_MOVE_LOADS)) {
+    uint4 x[KV_MOVE_LOADS];
+#pragma unroll
+    for (int i = 0; i < KV_MOVE_LOADS; ++i)
+      if (base + 256 * i < vecs) x[i] = from[base + 256 * i];
+#pragma unroll
+    for (int i = 0; i < KV_MOVE_LOADS; ++i)
+      if (base + 256 * i < vecs) to[base + 256 * i] = x[i];
+  }
+}
+
+hipError_t launch_kv_moves(const ArenaView& a, void* k_arena, void* v_arena, const KvMoves& moves, int32_t n_moves, hipStream_t stream) {
+  if (n_moves <= 0) return hipSuccess;
+  if (n_moves > KV_MAX_MOVES || (int64_t)n_moves * a.n_kv_heads > (1 << 23)) return hipErrorInvalidValue;  // (fewer than 2^32 threads)
+  int64_t longest = 0;
+  for (int32_t i = 0; i < n_moves; ++i) longest = moves.move[i].len > longest ? moves.move[i].len : longest;
+  const int32_t rv = row_vecs(a);
+  const int64_t pieces = (longest * rv + 256 * KV_MOVE_LOADS - 1) / (256 * KV_MOVE_LOADS);
+  const dim3 grid((unsigned)(2 * n_moves * a.n_kv_heads), (unsigned)(pieces < 64 ? pieces : 64));
+  kv_move_kernel<<<grid, 256, 0, stream>>>(moves, (uint4*)k_arena, (uint4*)v_arena, a.n_kv_heads, rv, a.arena_cells);
+  return hipGetLastError();
+}
+
 hipError_t launch_kv_scatter(const ArenaView& a, void* k_arena, void* v_arena, const int32_t* cell_of_dev,
                              int64_t tok_base, int32_t n_tok, const void* k_new, const void* v_new,
                              hipStream_t stream) {

@@ -22,51 +22,12 @@
 
 #include <type_traits>
 
-#include "kernels.hpp"
+#include "logprob_parts.hpp"
 
 namespace dk {
 
 namespace {
 
-constexpr int LP_THREADS = 256;
-constexpr int LP_WAVES = LP_THREADS / 64;
-constexpr int LP_UNROLL = 8, LP_UNROLL_FEW = 2;  // 16-byte loads of a lane
-constexpr int LP_CAP = 256;                      // candidates of a wavefront
-constexpr int LP_MAX_CHUNKS = 2048;              // of a row: 2^24 logits of 4 bytes, LP_UNROLL loads a lane
-static_assert(LP_MAX_CHUNKS * (LP_THREADS * LP_UNROLL * 4) >= LOGPROBS_MAX_VOCAB, "and so are 2^24 / 4 in shorter chunks, see cut_rows");
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-
-// What a chunk says of its row.
-struct Part {
-  float m, s0, s1;  // largest logit; sum 2^y and sum 2^y y against it
-  int32_t above;
-};
-
-__device__ __forceinline__ float logit_key(float x) { return x != x ? INFINITY : x; }
-__device__ __forceinline__ float logit_at(const float* p, int64_t i) { return p[i]; }
-__device__ __forceinline__ float logit_at(const uint16_t* p, int64_t i) { return __uint_as_float((uint32_t)p[i] << 16); }
-
-__device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) x = fmaxf(x, __shfl_xor(x, off));
-  return x;
-}
-__device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off);
-  return x;
-}
-// Whole numbers in the order of the floats (no NaN; both zeros alike).
-__device__ __forceinline__ uint32_t ordered(float x) {
-  const uint32_t b = __float_as_uint(x + 0.f);
-  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-}
-__device__ __forceinline__ float from_ordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
-// A logit and its id as one whole number: the larger comes first, of equals the one with the lower id.  0: none.
-typedef uint64_t Pick;
-__device__ __forceinline__ Pick pick_of(float x, int32_t id) { return (uint64_t)ordered(x) << 32 | (uint32_t)~id; }
-__device__ __forceinline__ float pick_value(Pick p) { return from_ordered((uint32_t)(p >> 32)); }
-__device__ __forceinline__ int32_t pick_id(Pick p) { return (int32_t)~(uint32_t)p; }
 // The n-th and the k-th largest of the lanes' values, or a little less: the first BITS bits of each, and the smallest value that
 // begins with them.
 template <int BITS>
@@ -300,7 +261,7 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_chunk_kernel(Logpro
         // equal the first n, in the order of the ids: lane by lane, 16 bytes by 16 bytes.
         count = 0;
         mark([&](float v) { return v > t; });
-        if (collect() && count <= LP_CAP - 8 - LOGPROBS_MAX_TOP) {
+        if (collect() && count <= LP_CAP - 8 - a.n_top) {
           int ties = 0;
 #pragma unroll
           for (int u = 0; u < UNROLL; ++u) {
@@ -432,18 +393,6 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_finish_kernel(Logpr
   }
 }
 
-// Chunks of a row.  Calls of few rows take short chunks, so that more compute units read and the lists of each are shorter.
-struct Cut {
-  int32_t unroll, n_chunks;
-};
-Cut cut_rows(int32_t rows, int64_t vocab, int32_t dtype) {
-  const int64_t per = (int64_t)LP_THREADS * 16 / (dtype == 1 ? 2 : 4);
-  const int64_t wide = (vocab + per * LP_UNROLL - 1) / (per * LP_UNROLL);
-  if (rows * wide >= 256) return {LP_UNROLL, (int32_t)wide};
-  return {LP_UNROLL_FEW, (int32_t)((vocab + per * LP_UNROLL_FEW - 1) / (per * LP_UNROLL_FEW))};
-}
-int64_t parts_bytes(int32_t rows, const Cut& cut) { return ((int64_t)rows * cut.n_chunks * (int64_t)sizeof(Part) + 255) / 256 * 256; }
-
 template <typename T, int UNROLL>
 void launch_chunks(const LogprobArgs& a, const Cut& cut, Part* parts, Pick* tops, hipStream_t stream) {
   const bool once = (int64_t)a.rows * a.vocab * (int64_t)sizeof(T) >= (int64_t)64 << 20;  // (as in verify.hip)
@@ -462,6 +411,14 @@ void launch_chunks(const LogprobArgs& a, const Cut& cut, Part* parts, Pick* tops
 
 }  // namespace
 
+hipError_t launch_logprob_chunks(const LogprobArgs& a, const Cut& cut, Part* parts, Pick* tops, hipStream_t stream) {
+  if ((int64_t)a.rows * cut.n_chunks >= (int64_t(1) << 32) / LP_THREADS || cut.n_chunks > LP_MAX_CHUNKS) return hipErrorInvalidValue;
+  const bool wide = cut.unroll == LP_UNROLL;
+  if (a.dtype == 1) wide ? launch_chunks<uint16_t, LP_UNROLL>(a, cut, parts, tops, stream) : launch_chunks<uint16_t, LP_UNROLL_FEW>(a, cut, parts, tops, stream);
+  else wide ? launch_chunks<float, LP_UNROLL>(a, cut, parts, tops, stream) : launch_chunks<float, LP_UNROLL_FEW>(a, cut, parts, tops, stream);
+  return hipGetLastError();
+}
+
 int64_t logprobs_workspace_bytes(int32_t rows, int64_t vocab, int32_t dtype, int32_t n_top) {
   const Cut cut = cut_rows(rows, vocab, dtype);
   return parts_bytes(rows, cut) + (int64_t)rows * cut.n_chunks * n_top * (int64_t)sizeof(Pick) + 256;
@@ -470,13 +427,9 @@ int64_t logprobs_workspace_bytes(int32_t rows, int64_t vocab, int32_t dtype, int
 hipError_t launch_token_logprobs(const LogprobArgs& a, void* workspace, hipStream_t stream) {
   if (a.rows <= 0) return hipSuccess;
   const Cut cut = cut_rows(a.rows, a.vocab, a.dtype);
-  if ((int64_t)a.rows * cut.n_chunks >= (int64_t(1) << 32) / LP_THREADS || cut.n_chunks > LP_MAX_CHUNKS) return hipErrorInvalidValue;
   Part* parts = (Part*)workspace;
   Pick* tops = (Pick*)((char*)workspace + parts_bytes(a.rows, cut));
-  const bool wide = cut.unroll == LP_UNROLL;
-  if (a.dtype == 1) wide ? launch_chunks<uint16_t, LP_UNROLL>(a, cut, parts, tops, stream) : launch_chunks<uint16_t, LP_UNROLL_FEW>(a, cut, parts, tops, stream);
-  else wide ? launch_chunks<float, LP_UNROLL>(a, cut, parts, tops, stream) : launch_chunks<float, LP_UNROLL_FEW>(a, cut, parts, tops, stream);
-  hipError_t e = hipGetLastError();
+  const hipError_t e = launch_logprob_chunks(a, cut, parts, tops, stream);
   if (e != hipSuccess) return e;
   if (a.n_top > 0) token_logprobs_finish_kernel<true><<<dim3((unsigned)a.rows), a.n_top > 22 ? LP_THREADS : 64, 0, stream>>>(a, cut.n_chunks, parts, tops);
   else token_logprobs_finish_kernel<false><<<dim3((unsigned)a.rows), 64, 0, stream>>>(a, cut.n_chunks, parts, tops);

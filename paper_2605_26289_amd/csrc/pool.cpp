@@ -376,4 +376,78 @@ int32_t Pool::append(int32_t n_seqs, const int32_t* slots, const int32_t* cu_del
   return OK;
 }
 
+int32_t Pool::reorder(int32_t n, const int32_t* slots, const int32_t* parents, Reorder* r) {
+  if (n < 0 || (n > 0 && (!slots || !parents))) return ERR_INVALID;
+  std::lock_guard<std::mutex> lk(mu_);
+  r->before.clear();
+  r->moves.clear();
+  std::vector<char> seen(slots_.size(), 0);
+  for (int32_t i = 0; i < n; ++i) {
+    if (!valid(slots[i])) return ERR_NO_SLOT;
+    if (seen[slots[i]]) return ERR_DUP_SLOT;
+    seen[slots[i]] = 1;
+  }
+  for (int32_t i = 0; i < n; ++i)
+    if (parents[i] < 0 || parents[i] >= n) return ERR_INVALID;
+  r->keeper.assign((size_t)n, -1);
+  for (int32_t i = n - 1; i >= 0; --i) r->keeper[(size_t)parents[i]] = i;
+  for (int32_t i = 0; i < n; ++i)
+    if (parents[i] == i) r->keeper[(size_t)i] = i;
+  // How many of a state's own tokens fill whole granules (or the room borrowed from the node in front): a child aliases that far.
+  const auto whole = [this](const Node& h) {
+    if (h.len < h.borrow_cap) return int64_t(0);
+    return h.borrow_cap + (h.len - h.borrow_cap) / gr_ * gr_;
+  };
+  int64_t need = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const Slot& s = slots_[slots[parents[i]]];
+    if (r->keeper[(size_t)parents[i]] != i && s.head && s.head->len > whole(*s.head)) ++need;
+  }
+  if (need > alloc_.free_count()) return ERR_NO_CELLS;
+  r->before.reserve((size_t)n);
+  r->moves.reserve((size_t)need);
+  std::vector<std::shared_ptr<Node>> heads((size_t)n);
+  for (int32_t i = 0; i < n; ++i) r->before.push_back(slots_[slots[i]]);
+  for (int32_t i = 0; i < n; ++i) {  // (all that can throw happens before the first slot changes)
+    const std::shared_ptr<Node>& h = r->before[(size_t)parents[i]].head;
+    if (r->keeper[(size_t)parents[i]] == i || !h) {
+      heads[(size_t)i] = h;
+      continue;
+    }
+    const int64_t keep = whole(*h), rest = h->len - keep, base = h->base + keep;
+    std::shared_ptr<Node> a;
+    if (base > 0) {
+      a = h;
+      while (a->base >= base) a = a->parent;
+      a->frozen = std::max(a->frozen, base);
+    }
+    heads[(size_t)i] = std::make_shared<Node>(&alloc_, gr_, a, base);
+    if (rest > 0) {
+      heads[(size_t)i]->grow(rest);
+      r->moves.push_back({h->cell_of(keep), heads[(size_t)i]->cell_of(0), rest});
+    }
+  }
+  for (int32_t i = 0; i < n; ++i) {
+    Slot& s = slots_[slots[i]];
+    set_head(s, std::move(heads[(size_t)i]));
+    s.len = r->before[(size_t)parents[i]].len;
+  }
+  return OK;
+}
+
+void Pool::undo_reorder(int32_t n, const int32_t* slots, Reorder* r) {
+  std::lock_guard<std::mutex> lk(mu_);
+  for (int32_t i = 0; i < n && i < (int32_t)r->before.size(); ++i) {
+    Slot& s = slots_[slots[i]];
+    set_head(s, r->before[(size_t)i].head);
+    s.len = r->before[(size_t)i].len;
+  }
+  r->before.clear();
+}
+
+void Pool::settle_reorder(Reorder* r) {
+  std::lock_guard<std::mutex> lk(mu_);
+  r->before.clear();
+}
+
 }  // namespace dk

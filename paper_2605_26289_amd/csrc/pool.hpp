@@ -121,6 +121,23 @@ class Pool {
   int32_t append(int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta, const int32_t* n_accept,
                  std::vector<int64_t>* dst_cell, std::vector<int64_t>* old_len = nullptr, std::vector<Extent>* runs = nullptr);
 
+  // Every slots[i] becomes what slots[parents[i]] was (distinct slots; parents are indexes into them), all or nothing.  One child of a
+  // parent takes its chain over as it is, itself if it is among them, else the first; every other one aliases what fills whole granules
+  // and gets cells of its own for the rest, fewer than a granule's, which `moves` says where to copy from.  `before` keeps what the
+  // slots were, so that undo_reorder() can put it back; settle_reorder() lets go of it (states that no slot has any more give their cells
+  // back there, so it is not left to the next call).
+  struct Move {
+    int64_t from, to, len;  // cells
+  };
+  struct Reorder {
+    std::vector<Slot> before;
+    std::vector<Move> moves;
+    std::vector<int32_t> keeper;
+  };
+  int32_t reorder(int32_t n, const int32_t* slots, const int32_t* parents, Reorder* r);
+  void undo_reorder(int32_t n, const int32_t* slots, Reorder* r);
+  void settle_reorder(Reorder* r);
+
   // Logical view of a slot as merged extents, positions ascending.
   int32_t extents(int32_t slot, std::vector<Extent>* out, int64_t* len_out);
   int32_t check_batch(int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta);

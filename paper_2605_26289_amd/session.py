@@ -93,6 +93,10 @@ class DevicePool:
     def append(self, slots: Sequence[int], cu_delta: Sequence[int], k_new, v_new, n_accept=None) -> None:
         dk.kv_append(self.handle, slots, cu_delta, k_new, v_new, n_accept)
 
+    def reorder(self, slots: Sequence[int], parents: Sequence[int]) -> None:
+        """Every slot becomes what the slot at its parent's index was (dk_seq_reorder)."""
+        dk.seq_reorder(self.handle, slots, parents)
+
     def ensure_workspace(self, slots, cu_delta, staged) -> torch.Tensor:
         return self._grow_workspace(dk.attend_workspace_bytes(self.handle, slots, cu_delta, staged))
 
