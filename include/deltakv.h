@@ -148,9 +148,9 @@ int32_t dk_seq_trim_batch(dk_pool* pool, int32_t n_seqs, const int32_t* slots, c
  *   slots    HOST [n]  distinct acquired slot ids
  *   parents  HOST [n]  each in [0, n)
  * One child of a parent takes its cells over as they are (itself if it is among them); every other child shares those that fill
- * whole granules, as after dk_seq_alias, and gets cells of its own for the rest, into which fewer than granule_cells tokens' K
- * and V are copied on `stream`.  So a search's sequences stay in few runs of cells however long it goes on, what it copies does not
- * depend on their length, and dk_shared_attend finds what they share.  Afterwards all of them grow independently.
+ * whole quarters of granules (whole ones where granule_cells is below 256 or no multiple of 4), as after dk_seq_alias, and takes a
+ * granule of its own for the rest, into which those tokens' K and V are copied on `stream`.  So a search's sequences stay in few
+ * runs of cells however long it goes on, what is copied does not depend on their length, and dk_shared_attend finds what they share.  Afterwards all of them grow independently.
  * DK_ERR_INVALID (a parent out of range), DK_ERR_NO_SLOT, DK_ERR_DUP_SLOT, and DK_ERR_NO_CELLS unless the arena has a free granule for
  * every copy -- cells of states that no slot has any more are free after the call, not during it -- leave every slot as it was.
  * Cells are chosen at call time: a captured call replays its copies, not the bookkeeping.

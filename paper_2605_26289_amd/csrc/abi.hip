@@ -491,21 +491,29 @@ int32_t dk_seq_reorder(dk_pool* pool, int32_t n, const int32_t* slots, const int
   if (!pool) return DK_ERR_INVALID;
   return guarded([&]() -> int32_t {
     std::lock_guard<std::mutex> launch(pool->launch_mu);
-    // a launch's grid: two rows of workgroups for every copy's KV head
-    if (pool->desc.n_kv_heads > (1 << 23) / dk::KV_MAX_MOVES) return DK_ERR_UNSUPPORTED;
     dk::Pool::Reorder& r = pool->reordered;
     const int32_t rc = pool->meta.reorder(n, slots, parents, &r);
     if (rc != DK_OK) return rc;
     hipError_t e = hipSuccess;
     dk::KvMoves moves;
-    for (size_t at = 0; at < r.moves.size() && e == hipSuccess; at += dk::KV_MAX_MOVES) {
-      const int32_t count = (int32_t)std::min<size_t>(dk::KV_MAX_MOVES, r.moves.size() - at);
-      for (int32_t i = 0; i < count; ++i) {
-        const dk::Pool::Move& m = r.moves[at + (size_t)i];
-        moves.move[i] = {(int32_t)m.from, (int32_t)m.to, (int32_t)m.len};
-      }
-      e = dk::launch_kv_moves(pool->view(), pool->desc.k_arena, pool->desc.v_arena, moves, count, (hipStream_t)stream);
+    int32_t count = 0;
+    const auto flush = [&]() {
+      if (count > 0 && e == hipSuccess)
+        e = dk::launch_kv_moves(pool->view(), pool->desc.k_arena, pool->desc.v_arena, moves, count, (hipStream_t)stream);
+      count = 0;
+    };
+    const int64_t longest = dk::kv_move_longest(pool->view());
+    if (longest <= 0 && !r.moves.empty()) {  // (a cell of 32 GiB)
+      pool->meta.undo_reorder(n, slots, &r);
+      return DK_ERR_UNSUPPORTED;
     }
+    for (const dk::Pool::Move& m : r.moves) {
+      for (int64_t at = 0; at < m.len; at += longest) {
+        if (count == dk::KV_MAX_MOVES) flush();
+        moves.move[count++] = {(int32_t)(m.from + at), (int32_t)(m.to + at), (int32_t)std::min(longest, m.len - at)};
+      }
+    }
+    flush();
     if (e != hipSuccess) {
       // (copies already enqueued wrote cells that no slot owns: harmless)
       pool->meta.undo_reorder(n, slots, &r);

@@ -25,6 +25,8 @@ constexpr int BEAM_MAX_LISTS = BEAM_MAX_ROWS * (int)((BEAM_MAX_VOCAB + LP_THREAD
 static_assert(BEAM_MAX_LISTS >= 1024, "calls of few rows have fewer than 4 x 256 chunks");
 constexpr int BEAM_MAX_HEADS = BEAM_MAX_LISTS + 2 * BEAM_MAX_OUT;
 constexpr int BEAM_CAP = 1024;  // continuations that reach T
+constexpr int BEAM_OWN = 8;      // entries that a thread asks for before all else
+constexpr int BEAM_ROW_SUMS = 16;
 
 // Whole numbers in the order of the doubles (no NaN).  0: none.
 __device__ __forceinline__ uint64_t ordered64(double x) {
@@ -48,9 +50,10 @@ __device__ __forceinline__ uint64_t rest_of(int row, Pick p) {
 
 __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, int32_t n_chunks, const Part* __restrict__ parts,
                                                                    const Pick* __restrict__ tops) {
+  __shared__ float2 sums[BEAM_MAX_ROWS * BEAM_ROW_SUMS];  // largest logit and sum of the rows' chunks, where they fit
   __shared__ uint32_t heads[BEAM_MAX_HEADS];
   __shared__ Found found[BEAM_CAP];
-  __shared__ double base[BEAM_MAX_ROWS];  // of a row that takes part: its score less scale x (its largest logit) and the log of its sum
+  __shared__ double base[BEAM_MAX_ROWS];  // of a row that takes part: its score less the log of its sum
   __shared__ float most[BEAM_MAX_ROWS];   // its largest logit; NaN: it takes no part
   __shared__ int32_t came;
   __shared__ Found bound;
@@ -58,29 +61,44 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
   const int n = a.n_out;
   const int r0 = min(max(a.cu_rows[g], 0), a.rows);
   const int rows = min(min(max(a.cu_rows[g + 1], r0), a.rows) - r0, BEAM_MAX_ROWS);
-  const int lists = rows * n_chunks;
+  const int lists = rows * n_chunks, entries = lists * n;
   const Part* gp = parts + (int64_t)r0 * n_chunks;
   const Pick* gt = tops + (int64_t)r0 * n_chunks * n;
 
-  // the rows' sums, a wavefront each
-  for (int r = wave; r < rows; r += BEAM_WAVES) {
-    const float score = a.scores[r0 + r];
-    const Part own = lane < n_chunks ? gp[r * n_chunks + lane] : Part{-INFINITY, 0.f, 0.f, 0};
-    float m = own.m;
-    for (int k = lane + 64; k < n_chunks; k += 64) m = fmaxf(m, gp[r * n_chunks + k].m);
-    m = wave_max(m);
-    const double c = a.scale * 1.4426950408889634;
-    double s = own.m == -INFINITY ? (double)own.s0 : (double)own.s0 * exp2(((double)own.m - (double)m) * c);  // (a NaN's chunk has a sum that is one)
-    for (int k = lane + 64; k < n_chunks; k += 64) {
-      const Part p = gp[r * n_chunks + k];
-      s += p.m == -INFINITY ? (double)p.s0 : (double)p.s0 * exp2(((double)p.m - (double)m) * c);
-    }
+  // All that is read is asked for at once, as far as it fits the registers: the kernel is a chain of round trips.
+  Pick own[BEAM_OWN];
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off);
-    if (lane == 0) {
+  for (int j = 0; j < BEAM_OWN; ++j) own[j] = tid + j * BEAM_THREADS < entries ? gt[tid + j * BEAM_THREADS] : 0;
+  const float own_score = tid < rows ? a.scores[r0 + tid] : 0.f;
+  const bool fits = n_chunks <= BEAM_ROW_SUMS;
+  if (fits) {
+    for (int i = tid; i < lists; i += BEAM_THREADS) sums[i] = make_float2(gp[i].m, gp[i].s0);
+  }
+  if (tid < rows) most[tid] = own_score;
+  __syncthreads();
+
+  // the rows' sums, `per` lanes to a row
+  int per = 1;
+  while (per < 64 && per < n_chunks) per *= 2;
+  const double c = a.scale * 1.4426950408889634;
+  for (int at = 0; at < rows; at += BEAM_THREADS / per) {
+    const int r = at + tid / per, sub = tid % per;
+    const bool there = r < rows;
+    const auto part = [&](int k) { return fits ? sums[r * n_chunks + k] : make_float2(gp[r * n_chunks + k].m, gp[r * n_chunks + k].s0); };
+    float m = -INFINITY;
+    for (int k = sub; there && k < n_chunks; k += per) m = fmaxf(m, part(k).x);
+    for (int off = per / 2; off >= 1; off /= 2) m = fmaxf(m, __shfl_xor(m, off));
+    double s = 0.0;
+    for (int k = sub; there && k < n_chunks; k += per) {
+      const float2 p = part(k);  // (of a chunk of nothing but -infinity the sum is 0, of one with a NaN it is one)
+      s += p.x == -INFINITY ? (double)p.y : (double)p.y * exp2(((double)p.x - (double)m) * c);
+    }
+    for (int off = per / 2; off >= 1; off /= 2) s += __shfl_xor(s, off);
+    if (there && sub == 0) {
+      const float score = most[r];
       const bool live = __builtin_fabsf(score) < INFINITY && __builtin_fabsf(m) < INFINITY && s > 0.0 && s < (double)INFINITY;
-      most[r] = live ? m : __uint_as_float(0x7fc00000u);
       base[r] = live ? (double)score - log(s) : 0.0;
+      most[r] = live ? m : __uint_as_float(0x7fc00000u);
     }
   }
   __syncthreads();
@@ -93,43 +111,66 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
 
   const int k = lists > 0 ? min(n, (2 * n + lists - 1) / lists) : 0;
   const int n_heads = lists * k;
-  for (int i = tid; i < n_heads; i += BEAM_THREADS) {
-    const int list = i / k, e = i - list * k;
-    heads[i] = (uint32_t)(score_of(list / n_chunks, gt[(int64_t)list * n + e]) >> 32);
+  uint64_t own_key[BEAM_OWN];
+  int own_list[BEAM_OWN];
+#pragma unroll
+  for (int j = 0; j < BEAM_OWN; ++j) {
+    const int i = tid + j * BEAM_THREADS;
+    own_key[j] = 0;
+    own_list[j] = 0;
+    if (j * BEAM_THREADS >= entries || i >= entries) continue;
+    own_list[j] = i / n;
+    own_key[j] = score_of(own_list[j] / n_chunks, own[j]);
+    const int e = i - own_list[j] * n;
+    if (e < k) heads[own_list[j] * k + e] = (uint32_t)(own_key[j] >> 32);
   }
+  for (int i = tid; i < n_heads && entries > BEAM_OWN * BEAM_THREADS; i += BEAM_THREADS) {
+    const int list = i / k, e = i - list * k;
+    if (list * n + e >= BEAM_OWN * BEAM_THREADS) heads[i] = (uint32_t)(score_of(list / n_chunks, gt[list * n + e]) >> 32);
+  }
+  if (tid == 0) came = 0;
   __syncthreads();
-  // every wavefront finds T by itself, bit by bit
+  // Every wavefront finds T by itself, bit by bit; its last bits (2^-10 of a score and less) do not matter.
   uint32_t t = 0;
   if (n_heads > n) {
-    constexpr int KEEP = 8;
+    constexpr int KEEP = 4;
     uint32_t mine[KEEP];
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) mine[i] = lane + 64 * i < n_heads ? heads[lane + 64 * i] : 0u;
-    for (int bit = 31; bit >= 0; --bit) {
+    for (int bit = 31; bit >= 10; --bit) {
       const uint32_t u = t | 1u << bit;
-      int count = 0;
+      int count = __builtin_popcountll(__builtin_amdgcn_ballot_w64(mine[0] >= u));
+      if (n_heads > 64) {
 #pragma unroll
-      for (int i = 0; i < KEEP; ++i) count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(mine[i] >= u));
-      for (int i = 64 * KEEP; i < n_heads; i += 64) count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i + lane < n_heads && heads[i + lane] >= u));
+        for (int i = 1; i < KEEP; ++i) count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(mine[i] >= u));
+        for (int i = 64 * KEEP; i < n_heads; i += 64) count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i + lane < n_heads && heads[i + lane] >= u));
+      }
       if (count >= n) t = u;
     }
   }
   Found least = {(uint64_t)t << 32, 0};
   if (least.score == 0) least.score = 1;  // (0 is none)
+  // what reaches T goes to LDS, a wavefront's at a time
+  const auto collect = [&](uint64_t key, int row, Pick p) {
+    const Found f = {key, rest_of(row, p)};
+    const bool take = key != 0 && !least.before(f);
+    const uint64_t b = __builtin_amdgcn_ballot_w64(take);
+    if (b == 0) return;
+    int at = 0;
+    if (lane == __builtin_ctzll(b)) at = atomicAdd(&came, __builtin_popcountll(b));
+    at = __shfl(at, __builtin_ctzll(b)) + __builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)b, 0));
+    if (take && at < BEAM_CAP) found[at] = f;
+  };
   int total = 0;
   while (true) {
-    if (tid == 0) came = 0;
-    __syncthreads();
-    // the lists whose first entry reaches T, an entry to a thread
-    for (int i = tid; i < lists * n; i += BEAM_THREADS) {
-      const int list = i / n;
-      if (heads[list * k] < (uint32_t)(least.score >> 32)) continue;
-      const int row = list / n_chunks;
-      const Pick q = gt[i];
-      const Found f = {score_of(row, q), rest_of(row, q)};
-      if (f.score == 0 || least.before(f)) continue;
-      const int at = atomicAdd(&came, 1);
-      if (at < BEAM_CAP) found[at] = f;
+#pragma unroll
+    for (int j = 0; j < BEAM_OWN; ++j)
+      if (j * BEAM_THREADS < entries) collect(own_key[j], own_list[j] / n_chunks, own[j]);
+    for (int at = BEAM_OWN * BEAM_THREADS; at < entries; at += BEAM_THREADS) {
+      const int i = at + tid, list = min(i, entries - 1) / n;
+      const bool look = i < entries && heads[list * k] >= (uint32_t)(least.score >> 32);
+      const Pick p = look ? gt[i] : 0;
+      collect(look ? score_of(list / n_chunks, p) : 0, list / n_chunks, p);
     }
     __syncthreads();
     total = came;
@@ -143,6 +184,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
     }
     __syncthreads();
     least = bound;
+    if (tid == 0) came = 0;
     __syncthreads();
   }
   const int64_t out0 = (int64_t)g * n;

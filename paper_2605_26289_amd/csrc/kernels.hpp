@@ -45,7 +45,7 @@ hipError_t launch_kv_scatter_runs(const ArenaView& a, void* k_arena, void* v_are
                                   int32_t n_tok, const void* k_new, const void* v_new, hipStream_t stream);
 
 // Copies inside the arena: `len` cells from `from` on to those from `to` on, K and V of all heads; no copy writes a cell that another one
-// reads.  At most this many travel in the arguments of a launch.
+// reads.  At most this many travel in the arguments of a launch, each of 1 to kv_move_longest() cells.
 struct KvMove {
   int32_t from, to, len;
 };
@@ -53,6 +53,7 @@ constexpr int32_t KV_MAX_MOVES = 320;
 struct KvMoves {
   KvMove move[KV_MAX_MOVES];
 };
+int32_t kv_move_longest(const ArenaView& a);
 hipError_t launch_kv_moves(const ArenaView& a, void* k_arena, void* v_arena, const KvMoves& moves, int32_t n_moves, hipStream_t stream);
 
 // Descriptors of at most INLINE_BLOB_BYTES are passed to the kernels inside their arguments instead of being

@@ -132,42 +132,56 @@ hipError_t launch_kv_scatter_runs(const ArenaView& a, void* k_arena, void* v_are
   return hipGetLastError();
 }
 
-// Reordered states: what a child's state has beyond whole granules of its parent's, copied into cells of its own.  The cells of one KV
-// head are one run of bytes on either side, so a workgroup takes a piece of the run of one (move, head, K or V), four 16-byte loads a
-// lane on their way before the first store.  Bound by the launch: a granule's rest is at most 64 KiB a head.
-constexpr int KV_MOVE_LOADS = 4;
+// Reordered states: what a child's state has of its own, copied into its cells.  Workgroup (2 m + v, y): 32 KiB of K (v 0) or V of move m,
+// its heads one behind the other, eight 16-byte loads of a lane on their way before the first store.  Bound by latency: arguments and
+// the move come from host memory in one round trip, which a division by an argument in front of the move made two.
+constexpr int KV_MOVE_LOADS = 8, KV_MOVE_VECS = 256 * KV_MOVE_LOADS;
 static_assert(sizeof(KvMoves) + 96 <= 4096, "kernel arguments are limited to 4 KiB");
 __global__ __launch_bounds__(256) void kv_move_kernel(KvMoves moves, uint4* __restrict__ k_arena, uint4* __restrict__ v_arena,
-                                                      int32_t n_kv_heads, int32_t row_vec, int64_t arena_cells) {
+                                                      int32_t n_kv_heads, int32_t row_vec, int64_t arena_cells, int32_t blocks_y) {
   // (`moves` starts the kernel-argument segment and is read through it, as above)
   typedef const __attribute__((address_space(4))) KvMoves* const_moves_ptr;
   const_moves_ptr table = (const_moves_ptr)__builtin_amdgcn_kernarg_segment_ptr();
   (void)moves;
-  const int32_t job = (int32_t)(blockIdx.x >> 1), m = job / n_kv_heads, g = job - m * n_kv_heads;
-  const int64_t vecs = (int64_t)table->move[m].len * row_vec, at = (int64_t)g * arena_cells;
+  const int m = (int)(blockIdx.x >> 1);
+  const int32_t from = table->move[m].from, to = table->move[m].to, vecs = table->move[m].len * row_vec;
+  const int32_t total = vecs * n_kv_heads;  // (below 2^31, see launch_kv_moves)
+  const uint32_t magic = 0xffffffffu / (uint32_t)vecs + 1;  // a head number by it is at most one too high (vecs > 1: rows are 128 bytes or more)
   uint4* arena = blockIdx.x & 1 ? v_arena : k_arena;
-  const uint4* from = arena + (at + table->move[m].from) * row_vec;
-  uint4* to = arena + (at + table->move[m].to) * row_vec;
-  for (int64_t base = (int64_t)blockIdx.y * (256 * KV_MOVE_LOADS) + threadIdx.x; base < vecs; base += (int64_t)gridDim.y * (256 * KV_MOVE_LOADS)) {
+  for (int64_t base = (int64_t)blockIdx.y * KV_MOVE_VECS; base < total; base += (int64_t)blocks_y * KV_MOVE_VECS) {
     uint4 x[KV_MOVE_LOADS];
+    int64_t at[KV_MOVE_LOADS];
+#pragma unroll
+    for (int i = 0; i < KV_MOVE_LOADS; ++i) {  // (lanes past the end read the last one again)
+      const int32_t idx = (int32_t)min(base + 256 * i + threadIdx.x, (int64_t)total - 1);
+      int32_t g = (int32_t)__umulhi((uint32_t)idx, magic);
+      g -= g * vecs > idx ? 1 : 0;
+      at[i] = (int64_t)g * arena_cells * row_vec + (idx - g * vecs);
+      x[i] = arena[at[i] + (int64_t)from * row_vec];
+    }
 #pragma unroll
     for (int i = 0; i < KV_MOVE_LOADS; ++i)
-      if (base + 256 * i < vecs) x[i] = from[base + 256 * i];
-#pragma unroll
-    for (int i = 0; i < KV_MOVE_LOADS; ++i)
-      if (base + 256 * i < vecs) to[base + 256 * i] = x[i];
+      if (base + 256 * i + threadIdx.x < total) arena[at[i] + (int64_t)to * row_vec] = x[i];
   }
+}
+
+int32_t kv_move_longest(const ArenaView& a) {
+  const int64_t cells = ((int64_t(1) << 31) - 1) / ((int64_t)row_vecs(a) * a.n_kv_heads);
+  return (int32_t)(cells < (1 << 24) ? cells : 1 << 24);
 }
 
 hipError_t launch_kv_moves(const ArenaView& a, void* k_arena, void* v_arena, const KvMoves& moves, int32_t n_moves, hipStream_t stream) {
   if (n_moves <= 0) return hipSuccess;
-  if (n_moves > KV_MAX_MOVES || (int64_t)n_moves * a.n_kv_heads > (1 << 23)) return hipErrorInvalidValue;  // (fewer than 2^32 threads)
+  if (n_moves > KV_MAX_MOVES) return hipErrorInvalidValue;
   int64_t longest = 0;
-  for (int32_t i = 0; i < n_moves; ++i) longest = moves.move[i].len > longest ? moves.move[i].len : longest;
+  for (int32_t i = 0; i < n_moves; ++i) {
+    if (moves.move[i].len <= 0 || moves.move[i].len > kv_move_longest(a)) return hipErrorInvalidValue;
+    longest = moves.move[i].len > longest ? moves.move[i].len : longest;
+  }
   const int32_t rv = row_vecs(a);
-  const int64_t pieces = (longest * rv + 256 * KV_MOVE_LOADS - 1) / (256 * KV_MOVE_LOADS);
-  const dim3 grid((unsigned)(2 * n_moves * a.n_kv_heads), (unsigned)(pieces < 64 ? pieces : 64));
-  kv_move_kernel<<<grid, 256, 0, stream>>>(moves, (uint4*)k_arena, (uint4*)v_arena, a.n_kv_heads, rv, a.arena_cells);
+  const int64_t pieces = (longest * rv * a.n_kv_heads + KV_MOVE_VECS - 1) / KV_MOVE_VECS;
+  const dim3 grid((unsigned)(2 * n_moves), (unsigned)(pieces < 1024 ? pieces : 1024));
+  kv_move_kernel<<<grid, 256, 0, stream>>>(moves, (uint4*)k_arena, (uint4*)v_arena, a.n_kv_heads, rv, a.arena_cells, (int32_t)grid.y);
   return hipGetLastError();
 }
 

@@ -36,15 +36,14 @@ struct Builder {
   int64_t group;
 
   int64_t rows_of(int32_t entry) const { return (int64_t)(cu[entry + 1] - cu[entry]) * group; }
-  int64_t ext_end(int32_t entry) const { return p->ext0[(size_t)entry + 1]; }
-
   // Segments of positions [lo, hi) of an entry's cells.
   void add_segs(int32_t entry, int64_t lo, int64_t hi) {
-    for (int64_t i = p->ext0[(size_t)entry]; i < ext_end(entry); ++i) {
-      const Extent& x = p->ext[(size_t)i];
-      const int64_t a = std::max(lo, x.pos), b = std::min(hi, x.pos + x.len);
-      if (a < b) p->node_segs.push_back({(int32_t)(x.cell + a - x.pos), (int32_t)a, (int32_t)(b - a)});
+    p->ext.clear();
+    for (int32_t i = p->part0[(size_t)entry]; i < p->part0[(size_t)entry + 1]; ++i) {
+      const Pool::Part& x = p->parts[(size_t)i];
+      if (std::max(lo, x.lo) < std::min(hi, x.hi)) Pool::add_extents(*x.node, std::max(lo, x.lo), std::min(hi, x.hi), &p->ext);
     }
+    for (const Extent& x : p->ext) p->node_segs.push_back({(int32_t)x.cell, (int32_t)x.pos, (int32_t)x.len});
   }
 
   // Whether the members' rows together over `keys` positions cost less than each entry's alone.
@@ -93,7 +92,7 @@ struct Builder {
     p->nodes.push_back(x);
   }
 
-  // The tree of shared prefixes, from the roots down: members that agree on a position's cell stay together.
+  // The tree of shared prefixes, from the roots down: members that have a position in the same node of the pool stay together.
   void build() {
     p->tasks.clear();
     if (!p->members.empty()) p->tasks.push_back({0, (int32_t)p->members.size(), 0, 0});
@@ -105,19 +104,19 @@ struct Builder {
         continue;
       }
       while (true) {  // as far as all of them have the same cells
-        int64_t step = INT64_MAX, cell = -1;
+        int64_t step = INT64_MAX;
+        const Node* same = nullptr;
         for (int32_t i = t.begin; i < t.end && step > 0; ++i) {
           SharedPlan::Member& m = p->members[(size_t)i];
           if (p->n[(size_t)m.entry] <= t.pos) {
             step = 0;
             break;
           }
-          while (p->ext[(size_t)m.ext].pos + p->ext[(size_t)m.ext].len <= t.pos) ++m.ext;
-          const Extent& x = p->ext[(size_t)m.ext];
-          const int64_t here = x.cell + t.pos - x.pos;
-          if (cell >= 0 && here != cell) step = 0;
-          cell = here;
-          step = std::min(step, std::min(x.pos + x.len, p->n[(size_t)m.entry]) - t.pos);
+          while (p->parts[(size_t)m.part].hi <= t.pos) ++m.part;
+          const Pool::Part& x = p->parts[(size_t)m.part];
+          if (same && x.node != same) step = 0;
+          same = x.node;
+          step = std::min(step, std::min(x.hi, p->n[(size_t)m.entry]) - t.pos);
         }
         if (step <= 0) break;
         t.pos += step;
@@ -126,15 +125,15 @@ struct Builder {
         add_shared(t.begin, t.end, t.start, t.pos);
         t.start = t.pos;
       }
-      // those that end here part from all others, the rest by their next cell
+      // those that end here part from all others, the rest by the node they go on in
       for (int32_t i = t.begin; i < t.end; ++i) {
         SharedPlan::Member& m = p->members[(size_t)i];
         if (p->n[(size_t)m.entry] <= t.pos) {
           m.key = -1 - i;
           continue;
         }
-        while (p->ext[(size_t)m.ext].pos + p->ext[(size_t)m.ext].len <= t.pos) ++m.ext;
-        m.key = p->ext[(size_t)m.ext].cell + t.pos - p->ext[(size_t)m.ext].pos;
+        while (p->parts[(size_t)m.part].hi <= t.pos) ++m.part;
+        m.key = p->parts[(size_t)m.part].node->cell_of(0);
       }
       std::sort(p->members.begin() + t.begin, p->members.begin() + t.end, [](const SharedPlan::Member& a, const SharedPlan::Member& b) {
         return a.key != b.key ? a.key < b.key : a.entry < b.entry;
@@ -148,44 +147,55 @@ struct Builder {
     }
   }
 
-  // Pieces of every node if a work item may take `us`: the longest item, all items' time, pieces' partial rows.
-  struct Cut {
-    double longest = 0, all = 0, parts = 0;
-    int64_t items = 0;
-  };
   int64_t chunk_of(const SharedPlan::Node& x, double us) const {
-    const double keys = (us - FIXED_US) / x.per_key;
-    int64_t chunk = std::max<int64_t>(128, ((int64_t)std::min(keys, 1e9) + 63) / 64 * 64);
-    const int64_t pieces = ((int64_t)x.d.keys + chunk - 1) / chunk;
-    return ((int64_t)x.d.keys + pieces - 1) / pieces / 64 * 64 + ((((int64_t)x.d.keys + pieces - 1) / pieces) % 64 ? 64 : 0);
-  }
-  Cut cut(double us) const {
-    Cut c;
-    for (const SharedPlan::Node& x : p->nodes) {
-      const int64_t chunk = chunk_of(x, us), pieces = (x.d.keys + chunk - 1) / chunk;
-      const double item = FIXED_US + x.per_key * (double)std::min<int64_t>(chunk, x.d.keys);
-      c.longest = std::max(c.longest, item);
-      c.all += x.tiles * (pieces * FIXED_US + x.per_key * (double)x.d.keys);
-      c.items += x.tiles * pieces;
-      if (pieces > 1 || x.entry < 0 || x.link >= 0) c.parts += (double)(pieces * x.d.rows);
-    }
-    return c;
+    const double keys = std::min((us - FIXED_US) / x.per_key, 1e9);
+    const int64_t most = std::max<int64_t>(128, ((int64_t)keys + 63) / 64 * 64);
+    if (x.d.keys <= most) return (x.d.keys + 63) / 64 * 64;
+    const int64_t pieces = (x.d.keys + most - 1) / most;
+    return ((x.d.keys + pieces - 1) / pieces + 63) / 64 * 64;
   }
 
+  // The longest time that a work item may take, so that all are done soonest: as long as the longest where they all run at once, else
+  // the mean of the places' loads and half of the longest; and the partial rows' way to memory and back.
   void choose_pieces() {
     const double at_once = std::max(1.0, (cfg.bf16 ? 512.0 : 256.0) / cfg.n_kv_heads);
-    double most = 0;
-    for (const SharedPlan::Node& x : p->nodes) most = std::max(most, FIXED_US + x.per_key * x.d.keys);
-    double best_us = most, best = 1e300;
-    for (double us = most; us > FIXED_US * 1.2; us *= 0.8) {
-      const Cut c = cut(us);
-      const double run = (double)c.items <= at_once ? c.longest : std::max(c.longest, c.all / at_once + 0.5 * c.longest);
-      const double est = run + PART_US * c.parts / at_once * 2 + (c.parts > 0 ? 3.0 : 0.0);
+    std::vector<SharedPlan::Load>& loads = p->loads;  // longest first: only those before the first that fits are cut
+    loads.clear();
+    for (const SharedPlan::Node& x : p->nodes)
+      loads.push_back({FIXED_US + x.per_key * x.d.keys, x.per_key, (double)x.tiles, (double)x.d.rows, x.entry < 0 || x.link >= 0 ? 1.0 : 0.0});
+    std::sort(loads.begin(), loads.end(), [](const SharedPlan::Load& a, const SharedPlan::Load& b) { return a.us > b.us; });
+    double all = 0, items = 0, parts = 0;  // of those that are not cut
+    for (const SharedPlan::Load& x : loads) {
+      all += x.tiles * x.us;
+      items += x.tiles;
+      parts += x.part * x.rows;
+    }
+    const double least = FIXED_US * 1.2;
+    double best_us = loads[0].us, best = 1e300;
+    size_t n_cut = 0;
+    for (double us = loads[0].us; us > least; us *= 0.8) {
+      for (; n_cut < loads.size() && loads[n_cut].us > us; ++n_cut) {
+        const SharedPlan::Load& x = loads[n_cut];
+        all -= x.tiles * x.us;
+        items -= x.tiles;
+        parts -= x.part * x.rows;
+      }
+      double longest = n_cut < loads.size() ? loads[n_cut].us : 0, cut_all = 0, cut_items = 0, cut_parts = 0;
+      for (size_t i = 0; i < n_cut; ++i) {
+        const SharedPlan::Load& x = loads[i];
+        const double keys_us = x.us - FIXED_US, most = std::max(us - FIXED_US, 128 * x.per_key), pieces = std::ceil(keys_us / most);
+        longest = std::max(longest, FIXED_US + keys_us / pieces);
+        cut_all += x.tiles * (pieces * FIXED_US + keys_us);
+        cut_items += x.tiles * pieces;
+        cut_parts += pieces * x.rows;
+      }
+      const double run = items + cut_items <= at_once ? longest : std::max(longest, (all + cut_all) / at_once + 0.5 * longest);
+      const double est = run + PART_US * (parts + cut_parts) / at_once * 2 + (parts + cut_parts > 0 ? 3.0 : 0.0);
       if (est < best) {
         best = est;
         best_us = us;
       }
-      if (c.items > 64 * at_once) break;
+      if (items + cut_items > 16 * at_once) break;
     }
     for (SharedPlan::Node& x : p->nodes) {
       x.d.chunk = (int32_t)chunk_of(x, best_us);
@@ -206,8 +216,8 @@ int32_t build_shared_plan(Pool& pool, const SharedConfig& cfg, int32_t n_seqs, c
                           SharedPlan* p) {
   int32_t rc = pool.check_batch(n_seqs, slots, cu_delta);
   if (rc != OK) return rc;
-  p->ext.clear();
-  p->ext0.clear();
+  p->parts.clear();
+  p->part0.clear();
   p->n.clear();
   p->members.clear();
   p->links.clear();
@@ -228,17 +238,16 @@ int32_t build_shared_plan(Pool& pool, const SharedConfig& cfg, int32_t n_seqs, c
   for (int32_t b = 0; b < n_seqs; ++b) {
     const int32_t delta = cu_delta[b + 1] - cu_delta[b];
     int64_t len = 0;
-    rc = pool.extents_locked(slots[b], &p->one, &len);
+    p->part0.push_back((int32_t)p->parts.size());
+    rc = pool.chain_locked(slots[b], &p->parts, &len);
     if (rc != OK) return rc;
     if (!staged && delta > len) return ERR_INVALID;
     if (len + delta >= SHARED_ALL / 2) return ERR_UNSUPPORTED;
-    p->ext0.push_back((int32_t)p->ext.size());
     p->n.push_back(staged ? len : len - delta);
     if (delta == 0) continue;
-    p->members.push_back({b, (int32_t)p->ext.size(), -1, 0});
-    p->ext.insert(p->ext.end(), p->one.begin(), p->one.end());
+    p->members.push_back({b, p->part0.back(), -1, 0});
   }
-  p->ext0.push_back((int32_t)p->ext.size());
+  p->part0.push_back((int32_t)p->parts.size());
   Builder build{cfg, cu_delta, staged, p, group};
   build.build();
   for (SharedPlan::Node& x : p->nodes) {
@@ -246,7 +255,7 @@ int32_t build_shared_plan(Pool& pool, const SharedConfig& cfg, int32_t n_seqs, c
     x.tiles = (int32_t)((x.d.rows + tile - 1) / tile);
     x.per_key = (float)key_us(cfg, x.d.rows);
   }
-  build.choose_pieces();
+  if (!p->nodes.empty()) build.choose_pieces();
   // longest items first
   p->order.resize(p->nodes.size());
   for (size_t i = 0; i < p->nodes.size(); ++i) {

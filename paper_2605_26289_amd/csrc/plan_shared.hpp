@@ -21,9 +21,9 @@ struct SharedPlan {
   };
   struct Member {  // an entry on its way down the tree of shared prefixes
     int32_t entry;
-    int32_t ext;    // the run of cells that the position under consideration is in
+    int32_t part;   // the part of its chain that the position under consideration is in
     int32_t link;   // its innermost shared node so far
-    int64_t key;    // cell at which it parts from others
+    int64_t key;    // first cell of the node in which it parts from others
   };
   struct Task {  // members [begin, end) whose cells are the same below `pos`; positions from `start` on are in no node yet
     int32_t begin, end;
@@ -36,8 +36,13 @@ struct SharedPlan {
     float per_key, fixed;  // cost of a work item
     int32_t entry, link;   // of one entry: which, and its innermost shared node; shared: -1
   };
-  std::vector<Extent> one, ext;
-  std::vector<int32_t> ext0;       // first run of every entry in `ext`
+  struct Load {  // of a node that is not cut: time of an item, of a key; row tiles, rows; 1: it leaves partial rows however it is cut
+    double us, per_key, tiles, rows, part;
+  };
+  std::vector<Load> loads;
+  std::vector<Extent> ext;
+  std::vector<Pool::Part> parts;   // the entries' chains
+  std::vector<int32_t> part0;      // first part of every entry
   std::vector<int64_t> n;          // cached tokens of every entry before the call
   std::vector<Member> members, spare;
   std::vector<Task> tasks;

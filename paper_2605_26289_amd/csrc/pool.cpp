@@ -6,7 +6,7 @@
 namespace dk {
 
 // ---------------------------------------------------------------- GranuleAllocator
-GranuleAllocator::GranuleAllocator(int64_t n) : free_(n), total_(n) {
+GranuleAllocator::GranuleAllocator(int64_t n) : tails_((size_t)std::max<int64_t>(n, 0), 0), free_(n), total_(n) {
   if (n > 0) runs_[0] = n;
 }
 
@@ -36,8 +36,15 @@ int64_t GranuleAllocator::take_fresh() {
   int64_t g = best->first;
   // If the run directly follows a cell range some sequence may still grow into, start in
   // the middle of the run so that both can keep extending contiguously.
-  if (g > 0 && tails_.count(g - 1) && best->second >= 2) g += best->second / 2;
+  if (g > 0 && tails_[(size_t)g - 1] && best->second >= 2) g += best->second / 2;
   remove_from_run(best, g);
+  return g;
+}
+
+int64_t GranuleAllocator::take_first() {
+  if (runs_.empty()) return -1;
+  const int64_t g = runs_.begin()->first;
+  remove_from_run(runs_.begin(), g);
   return g;
 }
 
@@ -73,7 +80,7 @@ int64_t Node::granules_needed(int64_t extra) const {
   return std::max<int64_t>(0, want - (int64_t)granules.size());
 }
 
-void Node::grow(int64_t extra) {
+void Node::grow(int64_t extra, bool anywhere) {
   const int64_t add = granules_needed(extra);
   for (int64_t i = 0; i < add; ++i) {
     int64_t g = -1;
@@ -84,7 +91,7 @@ void Node::grow(int64_t extra) {
       const int64_t after = (borrow_cell + borrow_cap) / gr;
       if (alloc->take(after)) g = after;
     }
-    if (g < 0) g = alloc->take_fresh();
+    if (g < 0) g = anywhere ? alloc->take_first() : alloc->take_fresh();
     granules.push_back(g);
     alloc->mark_tail(g);
   }
@@ -238,36 +245,60 @@ int32_t Pool::trim_locked(int32_t slot, int64_t new_len) {
   return OK;
 }
 
+void Pool::add_extents(const Node& n, int64_t lo, int64_t hi, std::vector<Extent>* out) {
+  const auto add = [&](int64_t cell, int64_t pos, int64_t take) {
+    if (!out->empty() && out->back().cell + out->back().len == cell && out->back().pos + out->back().len == pos) {
+      out->back().len += take;
+    } else {
+      out->push_back({cell, pos, take});
+    }
+  };
+  const int64_t lent = n.base + n.borrow_cap;
+  if (lo < std::min(hi, lent)) {  // first cells in the rest of the parent's last granule
+    add(n.borrow_cell + lo - n.base, lo, std::min(hi, lent) - lo);
+    lo = std::min(hi, lent);
+  }
+  while (lo < hi) {
+    const int64_t o = lo - lent, take = std::min(hi - lo, n.gr - o % n.gr);
+    add(n.granules[(size_t)(o / n.gr)] * n.gr + o % n.gr, lo, take);
+    lo += take;
+  }
+}
+
 void Pool::resolve(const std::shared_ptr<Node>& head, int64_t len, std::vector<Extent>* out) {
   out->clear();
-  std::vector<std::pair<const Node*, int64_t>> parts;  // node, exclusive upper position it contributes
-  int64_t limit = len;
+  // from the newest node on; few chains are longer than the array
+  constexpr int FEW = 16;
+  Part few[FEW];
+  std::vector<Part> many;
+  int64_t limit = len, count = 0;
   for (const Node* n = head.get(); n && limit > 0; n = n->parent.get()) {
     const int64_t hi = std::min(limit, n->end());
-    if (hi > n->base) parts.emplace_back(n, hi);
+    if (hi > n->base) {
+      if (count < FEW) few[count] = {n, n->base, hi};
+      else many.push_back({n, n->base, hi});
+      ++count;
+    }
     limit = std::min(limit, n->base);
   }
-  for (auto it = parts.rbegin(); it != parts.rend(); ++it) {
-    const Node* n = it->first;
-    int64_t own = it->second - n->base;  // tokens of this node that are visible
-    const auto add = [&](int64_t cell, int64_t pos, int64_t take) {
-      if (!out->empty() && out->back().cell + out->back().len == cell && out->back().pos + out->back().len == pos) {
-        out->back().len += take;
-      } else {
-        out->push_back({cell, pos, take});
-      }
-    };
-    if (n->borrow_cap > 0 && own > 0) {  // first cells in the rest of the parent's last granule
-      const int64_t take = std::min(own, n->borrow_cap);
-      add(n->borrow_cell, n->base, take);
-      own -= take;
-    }
-    for (size_t gi = 0; own > 0; ++gi) {
-      const int64_t take = std::min(own, n->gr);
-      add(n->granules[gi] * n->gr, n->base + n->borrow_cap + (int64_t)gi * n->gr, take);
-      own -= take;
-    }
+  for (int64_t i = count - 1; i >= 0; --i) {
+    const Part& p = i < FEW ? few[i] : many[(size_t)(i - FEW)];
+    add_extents(*p.node, p.lo, p.hi, out);
   }
+}
+
+int32_t Pool::chain_locked(int32_t slot, std::vector<Part>* out, int64_t* len_out) {
+  if (!valid(slot)) return ERR_NO_SLOT;
+  const size_t first = out->size();
+  int64_t limit = slots_[slot].len;
+  if (len_out) *len_out = limit;
+  for (const Node* n = slots_[slot].head.get(); n && limit > 0; n = n->parent.get()) {
+    const int64_t hi = std::min(limit, n->end());
+    if (hi > n->base) out->push_back({n, n->base, hi});
+    limit = std::min(limit, n->base);
+  }
+  std::reverse(out->begin() + (std::ptrdiff_t)first, out->end());
+  return OK;
 }
 
 int32_t Pool::extents_locked(int32_t slot, std::vector<Extent>* out, int64_t* len_out) {
@@ -393,10 +424,13 @@ int32_t Pool::reorder(int32_t n, const int32_t* slots, const int32_t* parents, R
   for (int32_t i = n - 1; i >= 0; --i) r->keeper[(size_t)parents[i]] = i;
   for (int32_t i = 0; i < n; ++i)
     if (parents[i] == i) r->keeper[(size_t)i] = i;
-  // How many of a state's own tokens fill whole granules (or the room borrowed from the node in front): a child aliases that far.
-  const auto whole = [this](const Node& h) {
+  // How many of a state's own tokens a child aliases: whole quarters of granules (and the room borrowed from the node in front).  Of
+  // whole granules, a state of 100 to 600 tokens leaves 128 to be copied on average, of quarters 32; each node in front of it takes
+  // up to four times the cells it fills for that, but beams have most of those in common.
+  const int64_t unit = gr_ >= 256 && gr_ % 4 == 0 ? gr_ / 4 : gr_;
+  const auto whole = [unit](const Node& h) {
     if (h.len < h.borrow_cap) return int64_t(0);
-    return h.borrow_cap + (h.len - h.borrow_cap) / gr_ * gr_;
+    return h.borrow_cap + (h.len - h.borrow_cap) / unit * unit;
   };
   int64_t need = 0;
   for (int32_t i = 0; i < n; ++i) {
@@ -423,7 +457,7 @@ int32_t Pool::reorder(int32_t n, const int32_t* slots, const int32_t* parents, R
     }
     heads[(size_t)i] = std::make_shared<Node>(&alloc_, gr_, a, base);
     if (rest > 0) {
-      heads[(size_t)i]->grow(rest);
+      heads[(size_t)i]->grow(rest, true);
       r->moves.push_back({h->cell_of(keep), heads[(size_t)i]->cell_of(0), rest});
     }
   }

@@ -13,7 +13,6 @@
 #include <map>
 #include <memory>
 #include <mutex>
-#include <set>
 #include <vector>
 
 namespace dk {
@@ -37,14 +36,17 @@ class GranuleAllocator {
   bool take(int64_t g);
   // Takes a granule that starts a fresh extent; -1 if none is free.
   int64_t take_fresh();
+  // Takes the free granule with the lowest number; -1 if none is free.  For states of less than a granule, which fill gaps: looking
+  // through the runs for the longest costs a microsecond and more where there are many.
+  int64_t take_first();
   void give_back(int64_t g);
-  void mark_tail(int64_t g) { tails_.insert(g); }
-  void unmark_tail(int64_t g) { tails_.erase(g); }
+  void mark_tail(int64_t g) { tails_[(size_t)g] = 1; }
+  void unmark_tail(int64_t g) { tails_[(size_t)g] = 0; }
 
  private:
   void remove_from_run(std::map<int64_t, int64_t>::iterator it, int64_t g);
   std::map<int64_t, int64_t> runs_;  // start -> length, maximal and disjoint
-  std::set<int64_t> tails_;          // last granule of each live node (places where a sequence may grow)
+  std::vector<char> tails_;          // 1: last granule of a live node (a place where a sequence may grow)
   int64_t free_;
   int64_t total_;
 };
@@ -62,7 +64,7 @@ struct Node {
 
   int64_t end() const { return base + len; }
   int64_t granules_needed(int64_t extra) const;  // granules an append of `extra` tokens must add
-  void grow(int64_t extra);                      // caller has checked the allocator holds enough
+  void grow(int64_t extra, bool anywhere = false);  // caller has checked the allocator holds enough; anywhere: a first granule fills a gap
   void shrink_to(int64_t new_len);               // own length, frees whole unused granules
   int64_t cell_of(int64_t own_offset) const {
     if (own_offset < borrow_cap) return borrow_cell + own_offset;
@@ -122,8 +124,8 @@ class Pool {
                  std::vector<int64_t>* dst_cell, std::vector<int64_t>* old_len = nullptr, std::vector<Extent>* runs = nullptr);
 
   // Every slots[i] becomes what slots[parents[i]] was (distinct slots; parents are indexes into them), all or nothing.  One child of a
-  // parent takes its chain over as it is, itself if it is among them, else the first; every other one aliases what fills whole granules
-  // and gets cells of its own for the rest, fewer than a granule's, which `moves` says where to copy from.  `before` keeps what the
+  // parent takes its chain over as it is, itself if it is among them, else the first; every other one aliases what fills whole
+  // quarters of granules (granules below 256 cells: whole ones) and gets cells of its own for the rest, which `moves` says where to copy from.  `before` keeps what the
   // slots were, so that undo_reorder() can put it back; settle_reorder() lets go of it (states that no slot has any more give their cells
   // back there, so it is not left to the next call).
   struct Move {
@@ -145,6 +147,16 @@ class Pool {
   int64_t granule_cells() const { return gr_; }
   int64_t arena_cells() const { return alloc_.total() * gr_; }
   std::mutex& mutex() { return mu_; }
+
+  // For callers that hold mutex().  A slot's chain as the nodes that its positions are in, ascending, added to `out`; two slots have the
+  // same cells exactly where they have the same node.
+  struct Part {
+    const Node* node;
+    int64_t lo, hi;
+  };
+  int32_t chain_locked(int32_t slot, std::vector<Part>* out, int64_t* len_out);
+  // Cells of positions [lo, hi) of a node, added to `out`, joined with its last extent where they follow it.
+  static void add_extents(const Node& n, int64_t lo, int64_t hi, std::vector<Extent>* out);
 
   // unlocked variants for callers that hold mutex()
   int32_t extents_locked(int32_t slot, std::vector<Extent>* out, int64_t* len_out);

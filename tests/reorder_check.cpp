@@ -26,7 +26,7 @@ int main(int argc, char** argv) {
     g_seed = seed;
     std::mt19937 rng(seed);
     const auto below = [&](int n) { return (int)(rng() % (unsigned)std::max(1, n)); };
-    const int granule = 1 + below(16), cells = granule * (seed % 4 == 0 ? 40 : 400), kSlots = 12;
+    const int granule = seed % 10 == 9 ? 256 : 1 + below(16), cells = granule * (seed % 4 == 0 ? 40 : 400), kSlots = 12;
     Pool pool(kSlots, 0, cells, granule);
     std::vector<int> memory((size_t)cells, -1);
     std::vector<std::vector<int>> model(kSlots);
@@ -98,7 +98,7 @@ int main(int argc, char** argv) {
           CHECK(held1 == held0);
         } else {
           for (const Pool::Move& m : re.moves) {
-            CHECK(m.len > 0 && m.len < granule);
+            CHECK(m.len > 0 && m.len < (granule == 256 ? 256 : granule));
             for (int64_t i = 0; i < m.len; ++i) {
               CHECK(m.to + i < m.from || m.to + i >= m.from + m.len);
               memory[(size_t)(m.to + i)] = memory[(size_t)(m.from + i)];
@@ -128,7 +128,7 @@ int main(int argc, char** argv) {
       CHECK(pool.acquire(0, 0, &s) == OK && pool.alias(prompt, s, 0, granule + 1) == OK);
       beams.push_back(s);
     }
-    const int steps = std::min(60, 6 * granule);
+    const int unit = granule == 256 ? 64 : granule, steps = granule == 256 ? 600 : std::min(60, 6 * granule);
     for (int step = 0; step < steps; ++step) {
       std::vector<int32_t> parents, cu = {0};
       for (int b = 0; b < 4; ++b) {
@@ -141,7 +141,7 @@ int main(int argc, char** argv) {
       for (int b = 0; b < 4; ++b) {
         int64_t segs = 0, depth = 0, len = 0;
         CHECK(pool.seq_stats(beams[(size_t)b], &segs, &depth) == OK && pool.length(beams[(size_t)b], &len) == OK);
-        CHECK(len == granule + 2 + step && depth <= 3 + (step + 1) / granule && segs <= 4 + (step + 1) / granule);
+        CHECK(len == granule + 2 + step && depth <= 3 + (step + 1) / unit && segs <= 4 + (step + 1) / unit);
       }
     }
   }
