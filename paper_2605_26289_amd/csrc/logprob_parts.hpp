@@ -1,5 +1,4 @@
-// What the chunks of logits rows leave behind for the kernels that fold them: log probabilities (logprobs.hip) and beam selection
-// (beam.hip).
+// What the kernels that go through logits rows chunk by chunk share: log probabilities (logprobs.hip) and beam selection (beam.hip).
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -46,6 +45,22 @@ typedef uint64_t Pick;
 __device__ __forceinline__ Pick pick_of(float x, int32_t id) { return (uint64_t)ordered(x) << 32 | (uint32_t)~id; }
 __device__ __forceinline__ float pick_value(Pick p) { return from_ordered((uint32_t)(p >> 32)); }
 __device__ __forceinline__ int32_t pick_id(Pick p) { return (int32_t)~(uint32_t)p; }
+// The n-th and the k-th largest of the lanes' values, or a little less: the first BITS bits of each, and the smallest value that
+// begins with them.
+template <int BITS>
+__device__ __forceinline__ float2 nth_and_kth_largest(float x, int n, int k) {
+  const uint32_t key = ordered(x);
+  uint32_t tn = 0, tk = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 32 - BITS; --bit) {
+    const uint32_t un = tn | (1u << bit), uk = tk | (1u << bit);
+    if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(key >= un)) >= n) tn = un;
+    if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(key >= uk)) >= k) tk = uk;
+  }
+  // (below are no values, -infinity is the first)
+  return make_float2(from_ordered(max(tn, 0x007fffffu)), from_ordered(max(tk, 0x007fffffu)));
+}
+
 // Chunks of a row.  Calls of few rows take short chunks, so that more compute units read and the lists of each are shorter.
 struct Cut {
   int32_t unroll, n_chunks;
@@ -57,9 +72,5 @@ inline Cut cut_rows(int32_t rows, int64_t vocab, int32_t dtype) {
   return {LP_UNROLL_FEW, (int32_t)((vocab + per * LP_UNROLL_FEW - 1) / (per * LP_UNROLL_FEW))};
 }
 inline int64_t parts_bytes(int32_t rows, const Cut& cut) { return ((int64_t)rows * cut.n_chunks * (int64_t)sizeof(Part) + 255) / 256 * 256; }
-
-// One workgroup per (row, chunk): parts [rows][chunks]; with n_top, tops [rows][chunks][n_top], each list in order, none behind its end.
-// n_top up to 64.
-hipError_t launch_logprob_chunks(const LogprobArgs& a, const Cut& cut, Part* parts, Pick* tops, hipStream_t stream);
 
 }  // namespace dk

@@ -28,22 +28,6 @@ namespace dk {
 
 namespace {
 
-// The n-th and the k-th largest of the lanes' values, or a little less: the first BITS bits of each, and the smallest value that
-// begins with them.
-template <int BITS>
-__device__ __forceinline__ float2 nth_and_kth_largest(float x, int n, int k) {
-  const uint32_t key = ordered(x);
-  uint32_t tn = 0, tk = 0;
-#pragma unroll
-  for (int bit = 31; bit >= 32 - BITS; --bit) {
-    const uint32_t un = tn | (1u << bit), uk = tk | (1u << bit);
-    if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(key >= un)) >= n) tn = un;
-    if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(key >= uk)) >= k) tk = uk;
-  }
-  // (below are no values, -infinity is the first)
-  return make_float2(from_ordered(max(tn, 0x007fffffu)), from_ordered(max(tk, 0x007fffffu)));
-}
-
 // The wavefront's n first logits in order, one after the other and from memory: where more logits lie above T than there is room for.
 template <typename T, int UNROLL>
 __device__ __forceinline__ int pick_rounds(const T* p, int32_t base, int32_t vocab, int n, Pick* out) {
@@ -261,7 +245,7 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_chunk_kernel(Logpro
         // equal the first n, in the order of the ids: lane by lane, 16 bytes by 16 bytes.
         count = 0;
         mark([&](float v) { return v > t; });
-        if (collect() && count <= LP_CAP - 8 - a.n_top) {
+        if (collect() && count <= LP_CAP - 8 - LOGPROBS_MAX_TOP) {
           int ties = 0;
 #pragma unroll
           for (int u = 0; u < UNROLL; ++u) {
@@ -411,14 +395,6 @@ void launch_chunks(const LogprobArgs& a, const Cut& cut, Part* parts, Pick* tops
 
 }  // namespace
 
-hipError_t launch_logprob_chunks(const LogprobArgs& a, const Cut& cut, Part* parts, Pick* tops, hipStream_t stream) {
-  if ((int64_t)a.rows * cut.n_chunks >= (int64_t(1) << 32) / LP_THREADS || cut.n_chunks > LP_MAX_CHUNKS) return hipErrorInvalidValue;
-  const bool wide = cut.unroll == LP_UNROLL;
-  if (a.dtype == 1) wide ? launch_chunks<uint16_t, LP_UNROLL>(a, cut, parts, tops, stream) : launch_chunks<uint16_t, LP_UNROLL_FEW>(a, cut, parts, tops, stream);
-  else wide ? launch_chunks<float, LP_UNROLL>(a, cut, parts, tops, stream) : launch_chunks<float, LP_UNROLL_FEW>(a, cut, parts, tops, stream);
-  return hipGetLastError();
-}
-
 int64_t logprobs_workspace_bytes(int32_t rows, int64_t vocab, int32_t dtype, int32_t n_top) {
   const Cut cut = cut_rows(rows, vocab, dtype);
   return parts_bytes(rows, cut) + (int64_t)rows * cut.n_chunks * n_top * (int64_t)sizeof(Pick) + 256;
@@ -427,9 +403,13 @@ int64_t logprobs_workspace_bytes(int32_t rows, int64_t vocab, int32_t dtype, int
 hipError_t launch_token_logprobs(const LogprobArgs& a, void* workspace, hipStream_t stream) {
   if (a.rows <= 0) return hipSuccess;
   const Cut cut = cut_rows(a.rows, a.vocab, a.dtype);
+  if ((int64_t)a.rows * cut.n_chunks >= (int64_t(1) << 32) / LP_THREADS || cut.n_chunks > LP_MAX_CHUNKS) return hipErrorInvalidValue;
   Part* parts = (Part*)workspace;
   Pick* tops = (Pick*)((char*)workspace + parts_bytes(a.rows, cut));
-  const hipError_t e = launch_logprob_chunks(a, cut, parts, tops, stream);
+  const bool wide = cut.unroll == LP_UNROLL;
+  if (a.dtype == 1) wide ? launch_chunks<uint16_t, LP_UNROLL>(a, cut, parts, tops, stream) : launch_chunks<uint16_t, LP_UNROLL_FEW>(a, cut, parts, tops, stream);
+  else wide ? launch_chunks<float, LP_UNROLL>(a, cut, parts, tops, stream) : launch_chunks<float, LP_UNROLL_FEW>(a, cut, parts, tops, stream);
+  hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (a.n_top > 0) token_logprobs_finish_kernel<true><<<dim3((unsigned)a.rows), a.n_top > 22 ? LP_THREADS : 64, 0, stream>>>(a, cut.n_chunks, parts, tops);
   else token_logprobs_finish_kernel<false><<<dim3((unsigned)a.rows), 64, 0, stream>>>(a, cut.n_chunks, parts, tops);
