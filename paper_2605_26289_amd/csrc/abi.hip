@@ -1116,7 +1116,8 @@ int32_t dk_shared_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     put(h + plan.off_nodes, plan.out_nodes.data(), plan.out_nodes.size() * sizeof(DkShNode));
     put(h + plan.off_segs, plan.segs.data(), plan.segs.size() * sizeof(DkShSeg));
     put(h + plan.off_tokens, plan.tokens.data(), plan.tokens.size() * sizeof(int32_t));
-    put(hm, plan.merges.data(), plan.merges.size() * sizeof(DkShMerge));
+    put(hm, plan.blocks.data(), plan.blocks.size() * sizeof(int32_t));
+    put(hm + plan.off_merges, plan.merges.data(), plan.merges.size() * sizeof(DkShMerge));
     put(hm + plan.off_sources, plan.sources.data(), plan.sources.size() * sizeof(DkShSource));
     pool->host_us[DK_HOST_STAGE] += clk.lap();
     hipError_t e = hipSuccess;
@@ -1159,7 +1160,7 @@ int32_t dk_shared_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     a.group = d.n_q_heads / d.n_kv_heads;
     a.gmagic = a.group > 1 ? (uint32_t)(((1ull << 32) + a.group - 1) / a.group) : 0u;
     a.in_args = in_args;
-    const dk::SharedMergeArgs ma{(const DkShMerge*)merge_desc, (const DkShSource*)(merge_desc + plan.off_sources), (int32_t)plan.merges.size() - 1,
+    const dk::SharedMergeArgs ma{(const int32_t*)merge_desc, (const DkShMerge*)(merge_desc + plan.off_merges), (const DkShSource*)(merge_desc + plan.off_sources), (int32_t)plan.merges.size() - 1,
                                  plan.spread, a.f32 ? plan.tile_rows : dk::SHARED_TILE};
     const bool timing = !pool->ev0.empty();
     const size_t ev_slot = timing ? (size_t)(pool->ev_calls % (int64_t)pool->ev0.size()) : 0;

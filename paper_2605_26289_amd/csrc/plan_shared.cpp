@@ -7,18 +7,20 @@ namespace dk {
 
 namespace {
 
-// What the cuts go by, in microseconds.
-constexpr double FIXED_US = 5.0;      // a work item without its keys
-constexpr double ROWS_KEY_US = 0.9 / 64;  // a key of a tile of 128 rows, two workgroups to a compute unit
-constexpr double FEW_KEY_US = 0.7 / 64;   // a key of a tile of up to 64 rows, 128-wide heads
-constexpr double F32_KEY_US = 1.0 / 64;
-constexpr double PART_US = 1.0e-3;    // a partial row of one KV head, written and read, a compute unit's share
+// What the cuts go by: microseconds of a workgroup's place, of which the chip has 512 (fp32: 256).  Measured by clocks in the kernels.
+constexpr double FIXED_US = 6.0;          // a work item without its keys
+constexpr double ROWS_KEY_US = 2.3 / 64;  // a key of a tile of 128 rows of 128
+constexpr double FEW_KEY_US = 1.9 / 64;   // a key of a tile of up to 64 rows
+constexpr double F32_KEY_US = 3.1 / 64;   // a key of 32 rows of 128 in fp32
+constexpr double PART_US = 0.08;          // a partial row of 128, written and read
 
+double places(const SharedConfig& cfg) { return std::max(1.0, (cfg.bf16 ? 512.0 : 256.0) / cfg.n_kv_heads); }  // of a KV head
 double key_us(const SharedConfig& cfg, int64_t rows) {
-  if (!cfg.bf16) return F32_KEY_US * cfg.head_dim / 128;
-  if (rows <= SHARED_FEW) return FEW_KEY_US * cfg.head_dim / 128;
-  return ROWS_KEY_US * cfg.head_dim / 128;
+  const double width = 0.2 + 0.8 * cfg.head_dim / 128;
+  if (!cfg.bf16) return F32_KEY_US * width;
+  return (rows <= SHARED_FEW ? FEW_KEY_US : ROWS_KEY_US) * width;
 }
+double part_us(const SharedConfig& cfg) { return PART_US * cfg.head_dim / 128; }
 int64_t tile_rows(const SharedConfig& cfg, const SharedPlan& p, int64_t rows) {
   if (!cfg.bf16) return p.tile_rows;
   return rows <= SHARED_FEW ? SHARED_FEW : SHARED_TILE;
@@ -55,8 +57,9 @@ struct Builder {
       rows += r;
       alone += tiles_us(cfg, *p, r);
     }
-    const double pieces = std::max(1.0, (double)keys / 512.0);
-    return (double)keys * (alone - tiles_us(cfg, *p, rows)) > FIXED_US + PART_US * pieces * (double)rows;
+    const double together = tiles_us(cfg, *p, rows), tiles = together / key_us(cfg, rows);
+    const double pieces = std::max(1.0, std::min((double)keys / 512.0, places(cfg) / tiles));
+    return (double)keys * (alone - together) > FIXED_US + part_us(cfg) * pieces * (double)rows;
   }
 
   void add_own(const SharedPlan::Member& m, int64_t start) {
@@ -158,7 +161,7 @@ struct Builder {
   // The longest time that a work item may take, so that all are done soonest: as long as the longest where they all run at once, else
   // the mean of the places' loads and half of the longest; and the partial rows' way to memory and back.
   void choose_pieces() {
-    const double at_once = std::max(1.0, (cfg.bf16 ? 512.0 : 256.0) / cfg.n_kv_heads);
+    const double at_once = places(cfg);
     std::vector<SharedPlan::Load>& loads = p->loads;  // longest first: only those before the first that fits are cut
     loads.clear();
     for (const SharedPlan::Node& x : p->nodes)
@@ -190,7 +193,7 @@ struct Builder {
         cut_parts += pieces * x.rows;
       }
       const double run = items + cut_items <= at_once ? longest : std::max(longest, (all + cut_all) / at_once + 0.5 * longest);
-      const double est = run + PART_US * (parts + cut_parts) / at_once * 2 + (parts + cut_parts > 0 ? 3.0 : 0.0);
+      const double est = run + part_us(cfg) * (parts + cut_parts) / at_once + (parts + cut_parts > 0 ? 3.0 : 0.0);
       if (est < best) {
         best = est;
         best_us = us;
@@ -227,6 +230,7 @@ int32_t build_shared_plan(Pool& pool, const SharedConfig& cfg, int32_t n_seqs, c
   p->out_nodes.clear();
   p->segs.clear();
   p->tokens.clear();
+  p->blocks.clear();
   p->merges.clear();
   p->sources.clear();
   p->total_tokens = n_seqs ? cu_delta[n_seqs] : 0;
@@ -289,7 +293,7 @@ int32_t build_shared_plan(Pool& pool, const SharedConfig& cfg, int32_t n_seqs, c
     if (x.entry < 0 || x.d.part0 < 0) continue;
     merge_rows += x.d.rows;
     int64_t all = x.pieces;
-    DkShMerge m{0, x.d.tok0, x.d.rows, (int32_t)p->sources.size(), x.d.part0, x.pieces, x.d.chunk, x.d.n + 1 - x.d.lo};
+    DkShMerge m{x.d.tok0, x.d.rows, (int32_t)p->sources.size(), x.d.part0, x.pieces, x.d.chunk, x.d.n + 1 - x.d.lo};
     for (int32_t l = x.link; l >= 0; l = p->links[(size_t)l].before) {
       const SharedPlan::Link& k = p->links[(size_t)l];
       const SharedPlan::Node& y = p->nodes[(size_t)k.node];
@@ -305,13 +309,14 @@ int32_t build_shared_plan(Pool& pool, const SharedConfig& cfg, int32_t n_seqs, c
   while (p->spread < groups && 2 * p->spread <= most && merge_rows * cfg.n_kv_heads * p->spread < 8192) p->spread *= 2;
   const int64_t rows_a_block = groups / p->spread;
   int64_t blocks = 0;
-  for (DkShMerge& m : p->merges) {
-    m.block0 = (int32_t)blocks;
+  for (const DkShMerge& m : p->merges) {
+    p->blocks.push_back((int32_t)blocks);
     blocks += (m.rows + rows_a_block - 1) / rows_a_block;
   }
   if (blocks > INT32_MAX / 256 / cfg.n_kv_heads) return ERR_UNSUPPORTED;
   p->merge_blocks = (int32_t)blocks;
-  p->merges.push_back({(int32_t)blocks, 0, 0, (int32_t)p->sources.size(), 0, 0, 64, 0});
+  p->blocks.push_back((int32_t)blocks);
+  p->merges.push_back({0, 0, (int32_t)p->sources.size(), 0, 0, 64, 0});
   size_t at = 0;
   section(at, p->starts.size() * sizeof(int32_t));
   p->off_nodes = section(at, p->out_nodes.size() * sizeof(DkShNode));
@@ -319,7 +324,8 @@ int32_t build_shared_plan(Pool& pool, const SharedConfig& cfg, int32_t n_seqs, c
   p->off_tokens = section(at, p->tokens.size() * sizeof(int32_t));
   p->main_bytes = at;
   at = 0;
-  section(at, p->merges.size() * sizeof(DkShMerge));
+  section(at, p->blocks.size() * sizeof(int32_t));
+  p->off_merges = section(at, p->merges.size() * sizeof(DkShMerge));
   p->off_sources = section(at, p->sources.size() * sizeof(DkShSource));
   p->merge_bytes = at;
   p->off_merge = p->main_bytes;

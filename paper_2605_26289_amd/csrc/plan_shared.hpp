@@ -55,6 +55,7 @@ struct SharedPlan {
   std::vector<DkShNode> out_nodes;
   std::vector<DkShSeg> segs;
   std::vector<int32_t> tokens;
+  std::vector<int32_t> blocks;     // first workgroup (of a KV head) of every merge, and behind the last
   std::vector<DkShMerge> merges;   // one more than there are
   std::vector<DkShSource> sources;
   int64_t total_tokens = 0, part_rows = 0, items = 0, row_items = 0;
@@ -63,7 +64,7 @@ struct SharedPlan {
   int32_t merge_blocks = 0;
   // main kernel's descriptors, the merge's, partial rows
   size_t off_nodes = 0, off_segs = 0, off_tokens = 0, main_bytes = 0;
-  size_t off_sources = 0, merge_bytes = 0;
+  size_t off_merges = 0, off_sources = 0, merge_bytes = 0;
   size_t off_merge = 0, off_parts = 0, total_bytes = 0;
   bool in_args() const { return main_bytes <= (size_t)SHARED_BLOB_BYTES && merge_bytes <= (size_t)SHARED_BLOB_BYTES; }
 };

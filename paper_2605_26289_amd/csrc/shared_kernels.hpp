@@ -37,6 +37,7 @@ struct SharedArgs {
   int32_t in_args, f32;
 };
 struct SharedMergeArgs {
+  const int32_t* blocks;
   const DkShMerge* merges;
   const DkShSource* sources;
   int32_t n_merges, spread, tile_rows;

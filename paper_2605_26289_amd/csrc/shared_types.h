@@ -26,8 +26,8 @@ struct DkShSeg {
 };
 
 // Rows of one entry whose sums are in several partial rows: the pieces of its own range and those of the prefixes in front of it.
+// (Where its workgroups begin is in an array of its own.)
 struct DkShMerge {
-  int32_t block0;  // first workgroup (of a KV head)
   int32_t tok0, rows;
   int32_t src0;    // its prefixes: DkShSource up to the next record's first
   int32_t part0, pieces, chunk, sees;  // of its own range; sees: how many of its positions the first token sees

@@ -47,7 +47,7 @@ static void check(Pool& pool, const Shape& sh, const std::vector<int32_t>& slots
   // sections fit one behind the other
   CHECK(p.starts.size() * 4 <= p.off_nodes && p.off_nodes + p.out_nodes.size() * sizeof(DkShNode) <= p.off_segs);
   CHECK(p.off_segs + p.segs.size() * sizeof(DkShSeg) <= p.off_tokens && p.off_tokens + p.tokens.size() * 4 <= p.main_bytes);
-  CHECK(p.merges.size() * sizeof(DkShMerge) <= p.off_sources && p.off_sources + p.sources.size() * sizeof(DkShSource) <= p.merge_bytes);
+  CHECK(p.blocks.size() == p.merges.size() && p.blocks.size() * 4 <= p.off_merges && p.off_merges + p.merges.size() * sizeof(DkShMerge) <= p.off_sources && p.off_sources + p.sources.size() * sizeof(DkShSource) <= p.merge_bytes);
   CHECK(p.off_merge == p.main_bytes && p.off_merge + p.merge_bytes <= p.off_parts);
   CHECK(p.off_parts + (size_t)p.part_rows * sh.hkv * (sh.d + 2) * 4 <= p.total_bytes);
 
@@ -147,7 +147,7 @@ static void check(Pool& pool, const Shape& sh, const std::vector<int32_t>& slots
   for (size_t i = 0; i + 1 < p.merges.size(); ++i) {
     const DkShMerge& m = p.merges[i];
     const DkShMerge& next = p.merges[i + 1];
-    CHECK(next.block0 - m.block0 == (m.rows + rows_a_block - 1) / rows_a_block);
+    CHECK(p.blocks[i + 1] - p.blocks[i] == (m.rows + rows_a_block - 1) / rows_a_block);
     for (int r = 0; r < m.rows; ++r) {
       const int64_t row = (int64_t)m.tok0 * group + r;
       CHECK(!merged[(size_t)row] && !direct[(size_t)row]);
@@ -161,7 +161,7 @@ static void check(Pool& pool, const Shape& sh, const std::vector<int32_t>& slots
           CHECK(owner[(size_t)(p.sources[(size_t)s].part0 + (int64_t)k * p.sources[(size_t)s].step + r)] == row);
     }
   }
-  CHECK(p.merges.back().block0 == p.merge_blocks && taken == written);
+  CHECK(p.blocks.back() == p.merge_blocks && taken == written);
   for (int64_t row = 0; row < rows; ++row) CHECK(merged[(size_t)row] + direct[(size_t)row] == 1);
 }
 
