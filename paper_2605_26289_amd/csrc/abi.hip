@@ -148,7 +148,7 @@ struct dk_pool {
     last_plan[DK_PLAN_ROUTE] = DK_ROUTE_SHARED;
     last_plan[DK_PLAN_ROW_ITEMS] = shared_plan.row_items;
     last_plan[DK_PLAN_STREAM_ITEMS] = shared_plan.items - shared_plan.row_items;
-    last_plan[DK_PLAN_MERGES] = (int64_t)shared_plan.merges.size() - 1;
+    last_plan[DK_PLAN_MERGES] = shared_plan.n_merges;
     last_plan[DK_PLAN_BYTES] = (int64_t)shared_plan.total_bytes;
   }
 
@@ -1101,37 +1101,32 @@ int32_t dk_shared_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < (int64_t)plan.total_bytes) return DK_ERR_WORKSPACE;
     pool->host_us[DK_HOST_PLAN] += clk.lap();
     // The two kernels' descriptors travel in their arguments, or go to the workspace in those of launches of their own: either way the
-    // call can be captured, and needs no staging memory.
-    const bool in_args = plan.in_args();
+    // call can be captured, and needs no staging memory.  (Each such launch costs about 2.5 us of the host and of the device.)
+    const bool in_args = plan.in_args(), merge_in_args = plan.merge_in_args();
     dk::SharedBlob main_blob{}, merge_blob{};
     std::vector<char>& bytes = pool->shared_blob;
-    char *h = (char*)&main_blob, *hm = (char*)&merge_blob;
-    if (!in_args) {
-      bytes.resize(plan.main_bytes + plan.merge_bytes);
-      h = bytes.data();
-      hm = h + plan.off_merge;
-    }
+    bytes.resize((in_args ? 0 : plan.main_bytes) + (merge_in_args ? 0 : plan.merge_bytes));
+    char *h = in_args ? (char*)&main_blob : bytes.data(), *hm = merge_in_args ? (char*)&merge_blob : bytes.data() + plan.off_merge;
     const auto put = [](char* at, const void* src, size_t n) { if (n) std::memcpy(at, src, n); };
     put(h, plan.starts.data(), plan.starts.size() * sizeof(int32_t));
     put(h + plan.off_nodes, plan.out_nodes.data(), plan.out_nodes.size() * sizeof(DkShNode));
     put(h + plan.off_segs, plan.segs.data(), plan.segs.size() * sizeof(DkShSeg));
     put(h + plan.off_tokens, plan.tokens.data(), plan.tokens.size() * sizeof(int32_t));
     put(hm, plan.blocks.data(), plan.blocks.size() * sizeof(int32_t));
-    put(hm + plan.off_merges, plan.merges.data(), plan.merges.size() * sizeof(DkShMerge));
+    put(hm + plan.off_src0, plan.src0.data(), plan.src0.size() * sizeof(int32_t));
     put(hm + plan.off_sources, plan.sources.data(), plan.sources.size() * sizeof(DkShSource));
+    if (in_args && plan.n_merges > 0) put(hm + plan.merge_bytes, plan.out_nodes.data(), plan.node_bytes());
     pool->host_us[DK_HOST_STAGE] += clk.lap();
     hipError_t e = hipSuccess;
-    if (!in_args) {
-      dk::SharedCarry piece;
-      for (size_t at = 0; at < bytes.size() && e == hipSuccess; at += sizeof(piece)) {
-        const size_t n = std::min(sizeof(piece), bytes.size() - at);
-        std::memcpy(&piece, bytes.data() + at, n);
-        e = dk::launch_shared_carry(piece, (char*)workspace + at, (int32_t)n, st);
-      }
-      if (e != hipSuccess) return pool->hip_fail(e);
+    dk::SharedCarry piece;
+    for (size_t at = 0; at < bytes.size() && e == hipSuccess; at += sizeof(piece)) {
+      const size_t n = std::min(sizeof(piece), bytes.size() - at);
+      std::memcpy(&piece, bytes.data() + at, n);
+      e = dk::launch_shared_carry(piece, (char*)workspace + at, (int32_t)n, st);
     }
+    if (e != hipSuccess) return pool->hip_fail(e);
     pool->host_us[DK_HOST_UPLOAD] += clk.lap();
-    const uintptr_t desc = in_args ? 0 : (uintptr_t)workspace, merge_desc = in_args ? 0 : desc + plan.off_merge;
+    const uintptr_t desc = in_args ? 0 : (uintptr_t)workspace, merge_desc = merge_in_args ? 0 : (uintptr_t)workspace + plan.off_merge;
     dk::SharedArgs a{};
     a.starts = (const int32_t*)desc;
     a.nodes = (const DkShNode*)(desc + plan.off_nodes);
@@ -1160,13 +1155,14 @@ int32_t dk_shared_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
     a.group = d.n_q_heads / d.n_kv_heads;
     a.gmagic = a.group > 1 ? (uint32_t)(((1ull << 32) + a.group - 1) / a.group) : 0u;
     a.in_args = in_args;
-    const dk::SharedMergeArgs ma{(const int32_t*)merge_desc, (const DkShMerge*)(merge_desc + plan.off_merges), (const DkShSource*)(merge_desc + plan.off_sources), (int32_t)plan.merges.size() - 1,
-                                 plan.spread, a.f32 ? plan.tile_rows : dk::SHARED_TILE};
+    const dk::SharedMergeArgs ma{(const int32_t*)merge_desc, (const int32_t*)(merge_desc + plan.off_src0),
+                                 (const DkShSource*)(merge_desc + plan.off_sources), in_args ? (const DkShNode*)plan.merge_bytes : a.nodes,
+                                 plan.spread, a.f32 ? plan.tile_rows : dk::SHARED_TILE, merge_in_args, in_args};
     const bool timing = !pool->ev0.empty();
     const size_t ev_slot = timing ? (size_t)(pool->ev_calls % (int64_t)pool->ev0.size()) : 0;
     if (timing) e = hipEventRecord(pool->ev0[ev_slot], st);
     if (e == hipSuccess)
-      e = dk::launch_attend_shared(in_args ? &main_blob : nullptr, in_args ? &merge_blob : nullptr, a, ma, d.head_dim, plan.items, plan.merge_blocks,
+      e = dk::launch_attend_shared(in_args ? &main_blob : nullptr, merge_in_args ? &merge_blob : nullptr, a, ma, d.head_dim, plan.items, plan.merge_blocks,
                                    plan.tile_rows, st);
     if (e == hipSuccess && timing) e = hipEventRecord(pool->ev1[ev_slot], st);
     if (e != hipSuccess) return pool->hip_fail(e);

@@ -544,7 +544,8 @@ __device__ __forceinline__ void few_rows(const SharedArgs& a, const ScoreParams&
 
 }  // namespace
 
-// bf16.  Workgroup w: work item w / n_kv_heads, KV head w % n_kv_heads; two workgroups to a compute unit.
+// bf16.  Workgroup w: work item w / n_kv_heads, KV head w % n_kv_heads, so that with eight KV heads each XCD reads the keys of one (runs of
+// 4 to 64 items of one order on an XCD, the tiles of the same keys side by side, took as long or longer); two workgroups to a compute unit.
 template <int HD>
 __global__ __launch_bounds__(256, 2) void shared_attend_kernel(SharedBlob blob, SharedArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -570,20 +571,20 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedBlob blob, Shar
   __shared__ float2 xml[GROUPS];
   (void)blob;
   const int g = blockIdx.x % a.n_kv_heads, block = blockIdx.x / a.n_kv_heads;
-  const DkShMerge* records = shared_desc(a, ma.merges);
-  const DkShSource* sources = shared_desc(a, ma.sources);
-  const int at = last_not_above(shared_desc(a, ma.blocks), ma.n_merges, block, threadIdx.x & 63);
-  const DkShMerge mg = load_desc(records, at);
-  const int src_end = load_desc(records, at + 1).src0;
+  const int32_t *blocks = scored_desc(ma.blocks, ma.in_args != 0), *src0 = scored_desc(ma.src0, ma.in_args != 0);
+  const DkShSource* sources = scored_desc(ma.sources, ma.in_args != 0);
+  const int at = last_not_above(blocks, a.n_nodes, block, threadIdx.x & 63);
+  const DkShNode nd = load_desc(scored_desc(ma.nodes, ma.nodes_in_args != 0), at);
+  const int src_begin = load_desc(src0, at), src_end = load_desc(src0, at + 1);
   const int lane = threadIdx.x % LANES, grp = threadIdx.x / LANES;
   const int first = grp % ma.spread;
-  const int row = (block - load_desc(shared_desc(a, ma.blocks), at)) * (GROUPS / ma.spread) + grp / ma.spread;
-  const bool there = row < mg.rows;
-  const int r = min(row, mg.rows - 1);
+  const int row = (block - load_desc(blocks, at)) * (GROUPS / ma.spread) + grp / ma.spread;
+  const bool there = row < nd.rows;
+  const int r = min(row, nd.rows - 1);
   const int tok = shared_token(a, r);
   // of its own range, the pieces that some row of its tile sees
-  const int tile_last = shared_token(a, min(mg.rows, (r / ma.tile_rows + 1) * ma.tile_rows) - 1);
-  const int own = min(mg.pieces, (mg.sees + tile_last + mg.chunk - 1) / mg.chunk);
+  const int tile_last = shared_token(a, min(nd.rows, (r / ma.tile_rows + 1) * ma.tile_rows) - 1);
+  const int own = (min(nd.keys, nd.n + 1 - nd.lo + tile_last) + nd.chunk - 1) / nd.chunk;
 
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   float l = 0.f, m = -INFINITY;
@@ -614,11 +615,11 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedBlob blob, Shar
     const int done = pieces > skip ? (pieces - skip + ma.spread - 1) / ma.spread : 0;
     skip = skip + done * ma.spread - pieces;
   };
-  for (int s = mg.src0; s < src_end; ++s) {
+  for (int s = src_begin; s < src_end; ++s) {
     const DkShSource src = load_desc(sources, s);
     range(src.part0, src.step, src.pieces);
   }
-  range(mg.part0, mg.rows, own);
+  range(nd.part0, nd.rows, own);
   if (ma.spread > 1) {
     xo[threadIdx.x] = acc;
     if (lane == 0) xml[grp] = make_float2(m, l);
@@ -627,7 +628,7 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedBlob blob, Shar
       for (int k = 1; k < ma.spread; ++k) add(xml[grp + k].x, xml[grp + k].y, xo[threadIdx.x + k * LANES]);
   }
   if (first != 0 || !there) return;
-  const int64_t orow = (int64_t)(mg.tok0 + tok) * a.n_q_heads + g * a.group + r - tok * a.group;
+  const int64_t orow = (int64_t)(nd.tok0 + tok) * a.n_q_heads + g * a.group + r - tok * a.group;
   const float inv = 1.f / l;
   if constexpr (F32) {
     *(f32x4*)((float*)a.out + orow * HD + lane * 4) = acc * inv;
@@ -787,7 +788,7 @@ __global__ __launch_bounds__(64 * SF_WAVES, 2) void shared_attend_f32_kernel(Sha
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) s[rb][k & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i][k], qf[rb][i][k], s[rb][k & 1], 0, 0, 0);
     have = cur.next(a, g, SF_KT, t);
-    if (have) load_k();
+    load_k();  // (the same keys again where there are no more: a load that may not have been made is waited for at once)
     __builtin_amdgcn_sched_barrier(0);
     bool grow = false;
     float mx[RB];
@@ -927,7 +928,7 @@ hipError_t launch_attend_shared(const SharedBlob* main, const SharedBlob* merge,
   if (head_dim != 64 && head_dim != 128) return hipErrorInvalidValue;
   const unsigned grid = (unsigned)items * (unsigned)a.n_kv_heads;
   hipError_t e = head_dim == 64 ? launch_items<64>(main ? *main : none, a, tile_rows, grid, stream) : launch_items<128>(main ? *main : none, a, tile_rows, grid, stream);
-  if (e != hipSuccess || ma.n_merges == 0) return e;
+  if (e != hipSuccess || merge_blocks == 0) return e;
   const unsigned blocks = (unsigned)merge_blocks * (unsigned)a.n_kv_heads;
   const SharedBlob& blob = merge ? *merge : none;
   if (head_dim == 64) {

@@ -151,11 +151,12 @@ struct Builder {
   }
 
   int64_t chunk_of(const SharedPlan::Node& x, double us) const {
+    const int64_t step = cfg.bf16 ? 64 : 128;  // keys that all wavefronts of an item take at a time
     const double keys = std::min((us - FIXED_US) / x.per_key, 1e9);
-    const int64_t most = std::max<int64_t>(128, ((int64_t)keys + 63) / 64 * 64);
+    const int64_t most = std::max<int64_t>(128, ((int64_t)keys + step - 1) / step * step);
     if (x.d.keys <= most) return (x.d.keys + 63) / 64 * 64;
     const int64_t pieces = (x.d.keys + most - 1) / most;
-    return ((x.d.keys + pieces - 1) / pieces + 63) / 64 * 64;
+    return ((x.d.keys + pieces - 1) / pieces + step - 1) / step * step;
   }
 
   // The longest time that a work item may take, so that all are done soonest: as long as the longest where they all run at once, else
@@ -231,7 +232,7 @@ int32_t build_shared_plan(Pool& pool, const SharedConfig& cfg, int32_t n_seqs, c
   p->segs.clear();
   p->tokens.clear();
   p->blocks.clear();
-  p->merges.clear();
+  p->src0.clear();
   p->sources.clear();
   p->total_tokens = n_seqs ? cu_delta[n_seqs] : 0;
   p->part_rows = p->items = p->row_items = 0;
@@ -289,11 +290,14 @@ int32_t build_shared_plan(Pool& pool, const SharedConfig& cfg, int32_t n_seqs, c
   p->out_nodes.push_back(last);
   // merges: the rows of entries that have more than one partial row
   int64_t merge_rows = 0, most = 0;
-  for (const SharedPlan::Node& x : p->nodes) {
+  p->n_merges = 0;
+  for (const int32_t i : p->order) {
+    const SharedPlan::Node& x = p->nodes[(size_t)i];
+    p->src0.push_back((int32_t)p->sources.size());
     if (x.entry < 0 || x.d.part0 < 0) continue;
+    ++p->n_merges;
     merge_rows += x.d.rows;
     int64_t all = x.pieces;
-    DkShMerge m{x.d.tok0, x.d.rows, (int32_t)p->sources.size(), x.d.part0, x.pieces, x.d.chunk, x.d.n + 1 - x.d.lo};
     for (int32_t l = x.link; l >= 0; l = p->links[(size_t)l].before) {
       const SharedPlan::Link& k = p->links[(size_t)l];
       const SharedPlan::Node& y = p->nodes[(size_t)k.node];
@@ -301,22 +305,22 @@ int32_t build_shared_plan(Pool& pool, const SharedConfig& cfg, int32_t n_seqs, c
       all += y.pieces;
     }
     most = std::max(most, all);
-    p->merges.push_back(m);
   }
+  p->src0.push_back((int32_t)p->sources.size());
   // Lane groups share the partial rows of a row where there are too few rows to fill the chip otherwise.
   const int64_t groups = 1024 / cfg.head_dim;
   p->spread = 1;
   while (p->spread < groups && 2 * p->spread <= most && merge_rows * cfg.n_kv_heads * p->spread < 8192) p->spread *= 2;
   const int64_t rows_a_block = groups / p->spread;
   int64_t blocks = 0;
-  for (const DkShMerge& m : p->merges) {
-    p->blocks.push_back((int32_t)blocks);
-    blocks += (m.rows + rows_a_block - 1) / rows_a_block;
+  for (const int32_t i : p->order) {
+    const SharedPlan::Node& x = p->nodes[(size_t)i];
+    p->blocks.push_back((int32_t)std::min<int64_t>(blocks, INT32_MAX));
+    if (x.entry >= 0 && x.d.part0 >= 0) blocks += (x.d.rows + rows_a_block - 1) / rows_a_block;
   }
   if (blocks > INT32_MAX / 256 / cfg.n_kv_heads) return ERR_UNSUPPORTED;
   p->merge_blocks = (int32_t)blocks;
   p->blocks.push_back((int32_t)blocks);
-  p->merges.push_back({0, 0, (int32_t)p->sources.size(), 0, 0, 64, 0});
   size_t at = 0;
   section(at, p->starts.size() * sizeof(int32_t));
   p->off_nodes = section(at, p->out_nodes.size() * sizeof(DkShNode));
@@ -325,7 +329,7 @@ int32_t build_shared_plan(Pool& pool, const SharedConfig& cfg, int32_t n_seqs, c
   p->main_bytes = at;
   at = 0;
   section(at, p->blocks.size() * sizeof(int32_t));
-  p->off_merges = section(at, p->merges.size() * sizeof(DkShMerge));
+  p->off_src0 = section(at, p->src0.size() * sizeof(int32_t));
   p->off_sources = section(at, p->sources.size() * sizeof(DkShSource));
   p->merge_bytes = at;
   p->off_merge = p->main_bytes;

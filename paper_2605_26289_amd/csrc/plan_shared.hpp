@@ -55,18 +55,21 @@ struct SharedPlan {
   std::vector<DkShNode> out_nodes;
   std::vector<DkShSeg> segs;
   std::vector<int32_t> tokens;
-  std::vector<int32_t> blocks;     // first workgroup (of a KV head) of every merge, and behind the last
-  std::vector<DkShMerge> merges;   // one more than there are
+  // The merge: rows of entries that have more than one partial row.  By node, and behind the last: its first workgroup (of a KV head;
+  // others than such entries' have none) and the first of its sources, the prefixes in front of it.
+  std::vector<int32_t> blocks, src0;
   std::vector<DkShSource> sources;
   int64_t total_tokens = 0, part_rows = 0, items = 0, row_items = 0;
   int32_t tile_rows = 0;           // fp32: rows of an item
   int32_t spread = 1;              // lane groups that share the partial rows of a row in the merge
-  int32_t merge_blocks = 0;
-  // main kernel's descriptors, the merge's, partial rows
+  int32_t merge_blocks = 0, n_merges = 0;
+  // main kernel's descriptors, the merge's, its copy of the nodes where they travel in arguments, partial rows
   size_t off_nodes = 0, off_segs = 0, off_tokens = 0, main_bytes = 0;
-  size_t off_merges = 0, off_sources = 0, merge_bytes = 0;
+  size_t off_src0 = 0, off_sources = 0, merge_bytes = 0;
   size_t off_merge = 0, off_parts = 0, total_bytes = 0;
-  bool in_args() const { return main_bytes <= (size_t)SHARED_BLOB_BYTES && merge_bytes <= (size_t)SHARED_BLOB_BYTES; }
+  size_t node_bytes() const { return out_nodes.size() * sizeof(DkShNode); }
+  bool in_args() const { return main_bytes <= (size_t)SHARED_BLOB_BYTES && (n_merges == 0 || merge_bytes + node_bytes() <= (size_t)SHARED_BLOB_BYTES); }
+  bool merge_in_args() const { return merge_bytes <= (size_t)SHARED_BLOB_BYTES; }
 };
 
 // Caller holds pool.mutex().

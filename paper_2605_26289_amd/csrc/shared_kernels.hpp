@@ -36,17 +36,21 @@ struct SharedArgs {
   uint32_t gmagic;  // ceil(2^32 / group), 0 for group 1
   int32_t in_args, f32;
 };
+// By node: its first workgroup (of a KV head; only nodes of one entry that leaves partial rows have any) and its first source, and behind
+// the last.  The nodes are the attention kernel's where those are in the workspace, else a copy.
 struct SharedMergeArgs {
   const int32_t* blocks;
-  const DkShMerge* merges;
+  const int32_t* src0;
   const DkShSource* sources;
-  int32_t n_merges, spread, tile_rows;
+  const DkShNode* nodes;
+  int32_t spread, tile_rows, in_args, nodes_in_args;
 };
 static_assert(sizeof(SharedBlob) + sizeof(SharedArgs) + sizeof(SharedMergeArgs) + 64 <= 4096, "kernel arguments are limited to 4 KiB");
 static_assert(sizeof(SharedCarry) + 64 <= 4096, "likewise");
 
 hipError_t launch_shared_carry(const SharedCarry& piece, void* to, int32_t bytes, hipStream_t stream);
 // main, merge: the descriptors of the two kernels, where they travel in the arguments.  tile_rows: fp32, rows of an item.
+// merge_blocks: of a KV head.
 hipError_t launch_attend_shared(const SharedBlob* main, const SharedBlob* merge, const SharedArgs& a, const SharedMergeArgs& ma, int32_t head_dim,
                                 int64_t items, int32_t merge_blocks, int32_t tile_rows, hipStream_t stream);
 

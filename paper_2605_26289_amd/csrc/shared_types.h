@@ -25,13 +25,7 @@ struct DkShSeg {
   int32_t start, pos, len;
 };
 
-// Rows of one entry whose sums are in several partial rows: the pieces of its own range and those of the prefixes in front of it.
-// (Where its workgroups begin is in an array of its own.)
-struct DkShMerge {
-  int32_t tok0, rows;
-  int32_t src0;    // its prefixes: DkShSource up to the next record's first
-  int32_t part0, pieces, chunk, sees;  // of its own range; sees: how many of its positions the first token sees
-};
+// One of the prefixes in front of an entry's own range, for the merge of its rows.
 struct DkShSource {
   int32_t part0;  // of the entry's first row, in the first piece
   int32_t step;   // partial rows from piece to piece

@@ -40,14 +40,16 @@ static void check(Pool& pool, const Shape& sh, const std::vector<int32_t>& slots
   const int n_nodes = (int)p.out_nodes.size() - 1;
   CHECK((int)p.starts.size() == n_nodes + 1 && p.starts[n_nodes] == p.items);
   if (p.total_tokens == 0) {
-    CHECK(n_nodes == 0 && p.merges.size() == 1);
+    CHECK(n_nodes == 0 && p.n_merges == 0);
     return;
   }
   (p.in_args() ? g_inline : g_carried)++;
+  CHECK(!p.in_args() || p.merge_in_args());
   // sections fit one behind the other
   CHECK(p.starts.size() * 4 <= p.off_nodes && p.off_nodes + p.out_nodes.size() * sizeof(DkShNode) <= p.off_segs);
   CHECK(p.off_segs + p.segs.size() * sizeof(DkShSeg) <= p.off_tokens && p.off_tokens + p.tokens.size() * 4 <= p.main_bytes);
-  CHECK(p.blocks.size() == p.merges.size() && p.blocks.size() * 4 <= p.off_merges && p.off_merges + p.merges.size() * sizeof(DkShMerge) <= p.off_sources && p.off_sources + p.sources.size() * sizeof(DkShSource) <= p.merge_bytes);
+  CHECK((int)p.blocks.size() == n_nodes + 1 && (int)p.src0.size() == n_nodes + 1);
+  CHECK(p.blocks.size() * 4 <= p.off_src0 && p.off_src0 + p.src0.size() * 4 <= p.off_sources && p.off_sources + p.sources.size() * sizeof(DkShSource) <= p.merge_bytes);
   CHECK(p.off_merge == p.main_bytes && p.off_merge + p.merge_bytes <= p.off_parts);
   CHECK(p.off_parts + (size_t)p.part_rows * sh.hkv * (sh.d + 2) * 4 <= p.total_bytes);
 
@@ -144,24 +146,30 @@ static void check(Pool& pool, const Shape& sh, const std::vector<int32_t>& slots
   const int tile_rows = sh.bf16 ? SHARED_TILE : p.tile_rows;
   const int rows_a_block = 1024 / sh.d / p.spread;
   CHECK(p.spread >= 1 && rows_a_block >= 1 && (p.spread & (p.spread - 1)) == 0);
-  for (size_t i = 0; i + 1 < p.merges.size(); ++i) {
-    const DkShMerge& m = p.merges[i];
-    const DkShMerge& next = p.merges[i + 1];
-    CHECK(p.blocks[i + 1] - p.blocks[i] == (m.rows + rows_a_block - 1) / rows_a_block);
+  int n_merges = 0;
+  for (int i = 0; i < n_nodes; ++i) {
+    const DkShNode& m = p.out_nodes[(size_t)i];
+    const int n_blocks = p.blocks[(size_t)i + 1] - p.blocks[(size_t)i];
+    if (m.n == SHARED_ALL || m.part0 < 0) {
+      CHECK(n_blocks == 0 && p.src0[(size_t)i] == p.src0[(size_t)i + 1]);
+      continue;
+    }
+    ++n_merges;
+    CHECK(n_blocks == (m.rows + rows_a_block - 1) / rows_a_block);
     for (int r = 0; r < m.rows; ++r) {
       const int64_t row = (int64_t)m.tok0 * group + r;
       CHECK(!merged[(size_t)row] && !direct[(size_t)row]);
       merged[(size_t)row] = 1;
       const int tile_last = (std::min(m.rows, (r / tile_rows + 1) * tile_rows) - 1) / group;
-      const int own = (int)std::min<int64_t>(m.pieces, ((int64_t)m.sees + tile_last + m.chunk - 1) / m.chunk);
+      const int own = (int)((std::min<int64_t>(m.keys, (int64_t)m.n + 1 - m.lo + tile_last) + m.chunk - 1) / m.chunk);
       CHECK(own >= 1);
       for (int k = 0; k < own; ++k, ++taken) CHECK(owner[(size_t)(m.part0 + (int64_t)k * m.rows + r)] == row);
-      for (int s = m.src0; s < next.src0; ++s)
+      for (int s = p.src0[(size_t)i]; s < p.src0[(size_t)i + 1]; ++s)
         for (int k = 0; k < p.sources[(size_t)s].pieces; ++k, ++taken)
           CHECK(owner[(size_t)(p.sources[(size_t)s].part0 + (int64_t)k * p.sources[(size_t)s].step + r)] == row);
     }
   }
-  CHECK(p.blocks.back() == p.merge_blocks && taken == written);
+  CHECK(p.blocks.back() == p.merge_blocks && taken == written && n_merges == p.n_merges);
   for (int64_t row = 0; row < rows; ++row) CHECK(merged[(size_t)row] + direct[(size_t)row] == 1);
 }
 
