@@ -10,7 +10,8 @@ namespace {
 // What the cuts go by: microseconds of a workgroup's place, of which the chip has 512 (fp32: 256).  Measured by clocks in the kernels.
 constexpr double FIXED_US = 6.0;          // a work item without its keys
 constexpr double ROWS_KEY_US = 2.3 / 64;  // a key of a tile of 128 rows of 128
-constexpr double FEW_KEY_US = 1.9 / 64;   // a key of a tile of up to 64 rows
+constexpr double FEW_KEY_US = 1.9 / 64;   // a key of a tile of up to 32 rows
+constexpr double FEW2_KEY_US = 2.6 / 64;  // a key of one of up to 64
 constexpr double F32_KEY_US = 3.1 / 64;   // a key of 32 rows of 128 in fp32
 constexpr double PART_US = 0.08;          // a partial row of 128, written and read
 
@@ -18,7 +19,7 @@ double places(const SharedConfig& cfg) { return std::max(1.0, (cfg.bf16 ? 512.0 
 double key_us(const SharedConfig& cfg, int64_t rows) {
   const double width = 0.2 + 0.8 * cfg.head_dim / 128;
   if (!cfg.bf16) return F32_KEY_US * width;
-  return (rows <= SHARED_FEW ? FEW_KEY_US : ROWS_KEY_US) * width;
+  return (rows <= 32 ? FEW_KEY_US : rows <= SHARED_FEW ? FEW2_KEY_US : ROWS_KEY_US) * width;
 }
 double part_us(const SharedConfig& cfg) { return PART_US * cfg.head_dim / 128; }
 int64_t tile_rows(const SharedConfig& cfg, const SharedPlan& p, int64_t rows) {
@@ -150,17 +151,36 @@ struct Builder {
     }
   }
 
+  // Pieces of what takes keys_us, items of at most `us` (and of 128 keys and more).
+  static int64_t pieces_of(double keys_us, double per_key, double us) {
+    const double most = std::max(us - FIXED_US, 128 * per_key);
+    return keys_us <= most ? 1 : (int64_t)(keys_us / most * 0.999) + 1;
+  }
   int64_t chunk_of(const SharedPlan::Node& x, double us) const {
     const int64_t step = cfg.bf16 ? 64 : 128;  // keys that all wavefronts of an item take at a time
-    const double keys = std::min((us - FIXED_US) / x.per_key, 1e9);
-    const int64_t most = std::max<int64_t>(128, ((int64_t)keys + step - 1) / step * step);
-    if (x.d.keys <= most) return (x.d.keys + 63) / 64 * 64;
-    const int64_t pieces = (x.d.keys + most - 1) / most;
-    return ((x.d.keys + pieces - 1) / pieces + step - 1) / step * step;
+    const int64_t pieces = pieces_of(x.per_key * x.d.keys, x.per_key, us);
+    return pieces == 1 ? (x.d.keys + 63) / 64 * 64 : ((x.d.keys + pieces - 1) / pieces + step - 1) / step * step;
   }
 
-  // The longest time that a work item may take, so that all are done soonest: as long as the longest where they all run at once, else
-  // the mean of the places' loads and half of the longest; and the partial rows' way to memory and back.
+  // `n` items of the same length go where places are free first; `levels`: when how many places are free, soonest first.
+  void put_items(double n, double us) {
+    std::vector<SharedPlan::Level>& at = p->levels;
+    while (n > 0) {
+      const double k = std::min(n, at[0].places), end = 0.5 * (double)((int64_t)(2 * (at[0].us + us)) + 1);  // (half microseconds: few levels)
+      n -= k;
+      at[0].places -= k;
+      size_t i = at[0].places > 0 ? 0 : 1;
+      const size_t gone = i;
+      while (i < at.size() && at[i].us < end) ++i;
+      if (i < at.size() && at[i].us == end) at[i].places += k;
+      else at.insert(at.begin() + (std::ptrdiff_t)i, {end, k});
+      if (gone) at.erase(at.begin());
+    }
+  }
+
+  // The longest time that a work item may take, so that all are done soonest: as long as the longest where they all run at once; else
+  // until the last of those that are cut are done, longest first, or the mean of the places' loads and half of the longest of the others;
+  // and the partial rows' way to memory and back.
   void choose_pieces() {
     const double at_once = places(cfg);
     std::vector<SharedPlan::Load>& loads = p->loads;  // longest first: only those before the first that fits are cut
@@ -177,24 +197,39 @@ struct Builder {
     const double least = FIXED_US * 1.2;
     double best_us = loads[0].us, best = 1e300;
     size_t n_cut = 0;
-    for (double us = loads[0].us; us > least; us *= 0.8) {
+    for (double us = loads[0].us; us > least; us *= 0.9) {
       for (; n_cut < loads.size() && loads[n_cut].us > us; ++n_cut) {
         const SharedPlan::Load& x = loads[n_cut];
         all -= x.tiles * x.us;
         items -= x.tiles;
         parts -= x.part * x.rows;
       }
-      double longest = n_cut < loads.size() ? loads[n_cut].us : 0, cut_all = 0, cut_items = 0, cut_parts = 0;
+      const double uncut = n_cut < loads.size() ? loads[n_cut].us : 0;
+      double longest = uncut, cut_all = 0, cut_items = 0, cut_parts = 0;
       for (size_t i = 0; i < n_cut; ++i) {
         const SharedPlan::Load& x = loads[i];
-        const double keys_us = x.us - FIXED_US, most = std::max(us - FIXED_US, 128 * x.per_key), pieces = std::ceil(keys_us / most);
+        const double keys_us = x.us - FIXED_US, pieces = (double)pieces_of(keys_us, x.per_key, us);
         longest = std::max(longest, FIXED_US + keys_us / pieces);
         cut_all += x.tiles * (pieces * FIXED_US + keys_us);
         cut_items += x.tiles * pieces;
         cut_parts += pieces * x.rows;
       }
-      const double run = items + cut_items <= at_once ? longest : std::max(longest, (all + cut_all) / at_once + 0.5 * longest);
-      const double est = run + part_us(cfg) * (parts + cut_parts) / at_once + (parts + cut_parts > 0 ? 3.0 : 0.0);
+      const double joined = part_us(cfg) * (parts + cut_parts) / at_once + (parts + cut_parts > 0 ? 3.0 : 0.0);
+      const double mean = (all + cut_all) / at_once;
+      if (mean + joined >= best) break;  // shorter items only add to both
+      double run = longest;
+      if (items + cut_items > 16 * at_once) {
+        run = mean + 0.5 * longest;
+      } else if (items + cut_items > at_once) {
+        p->levels.assign(1, {0, at_once});
+        for (size_t i = 0; i < n_cut; ++i) {
+          const SharedPlan::Load& x = loads[i];
+          const double keys_us = x.us - FIXED_US, pieces = (double)pieces_of(keys_us, x.per_key, us);
+          put_items(x.tiles * pieces, FIXED_US + keys_us / pieces);
+        }
+        run = std::max(p->levels.back().us, mean + 0.5 * uncut);
+      }
+      const double est = run + joined;
       if (est < best) {
         best = est;
         best_us = us;

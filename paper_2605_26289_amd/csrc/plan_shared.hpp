@@ -40,6 +40,10 @@ struct SharedPlan {
     double us, per_key, tiles, rows, part;
   };
   std::vector<Load> loads;
+  struct Level {  // places that are free from then on
+    double us, places;
+  };
+  std::vector<Level> levels;
   std::vector<Extent> ext;
   std::vector<Pool::Part> parts;   // the entries' chains
   std::vector<int32_t> part0;      // first part of every entry
