@@ -15,10 +15,12 @@
 //                        thousand), T is raised to the n-th of those that came and the lists are gone through again.
 // Scores are made and compared in fp64: rows of one group differ by the logs of sums of 10^5 terms, and two continuations may be close.
 //
-// Measured (kernel times): 64 groups of eight rows of 128 256 bf16 logits, n = 16: chunks 24.8 us (5.3 TB/s; bound by the one read of
-// 131 MB), groups 14.7; with lists of the n best logits themselves, put in order, the chunks' kernel took 36.  One group of four such rows,
-// n = 8: 3.8 and 10.3; 40 groups of up to ten rows of 50 003 fp32 logits, most of them -infinity: 10.9 and 13.9.  The groups' kernel is a chain of
-// round trips and of exchanges over LDS: load 1.1 us, sums 1.2 to 1.8, T 1.3, lists 1.8 to 2.6, logits 2 to 4, places 0.5 to 1.
+// Measured (kernel times): 64 groups of eight rows of 128 256 bf16 logits, n = 16: chunks 24.9 us (131 MB, 5.3 TB/s; 500 vector
+// instructions a wavefront keep the SIMDs busy three fifths of that, six wavefronts to a SIMD instead of five give 2 %), groups 12.7; with
+// lists of the n best logits themselves, put in order, the chunks took 36.  One group of four such rows, n = 8: 3.8 and 9.7; 40 groups
+// of up to ten rows of 50 003 fp32 logits, most of them -infinity: 10.9 and 12.2.  The groups' kernel is a chain of round trips and of
+// exchanges over LDS: load 1.1 us, sums 1.2 to 1.7, T 1.3, lists 1.8 to 2.6, logits 2 to 4, places 0.5 to 1; of 256 lanes instead
+// of 512 it takes 10.3, 14.7 and 14.0, of 1024 10.8, 14.5 and 13.2.
 #include <hip/hip_runtime.h>
 
 #include "logprob_parts.hpp"
@@ -27,7 +29,7 @@ namespace dk {
 
 namespace {
 
-constexpr int BEAM_THREADS = 256, BEAM_WAVES = BEAM_THREADS / 64;
+constexpr int BEAM_THREADS = 512, BEAM_WAVES = BEAM_THREADS / 64;
 constexpr int BEAM_ID_BITS = 20;
 static_assert(BEAM_MAX_VOCAB <= 1 << BEAM_ID_BITS && BEAM_MAX_ROWS <= 1 << (64 - 32 - BEAM_ID_BITS), "row, logit and token in 64 bits");
 constexpr int BEAM_MAX_LISTS = BEAM_MAX_ROWS * (int)((BEAM_MAX_VOCAB + LP_THREADS * LP_UNROLL * 4 - 1) / (LP_THREADS * LP_UNROLL * 4));
@@ -210,7 +212,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
   // the rows' sums, `per` lanes to a row
   int per = 1;
   while (per < 64 && per < n_chunks) per *= 2;
-  const double c = a.scale * 1.4426950408889634;
+  const float c = (float)(a.scale * 1.4426950408889634);  // (chunks' weights in fp32, as their sums: 2^-22 of the row's sum at the most)
   for (int at = 0; at < rows; at += BEAM_THREADS / per) {
     const int r = at + tid / per, s = tid % per;
     const bool there = r < rows;
@@ -221,7 +223,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
     double z = 0.0;
     for (int k = s; there && k < n_chunks; k += per) {
       const float2 q = part(k);  // (of a chunk of nothing but -infinity the sum is 0, of one with a NaN it is one)
-      z += q.x == -INFINITY ? (double)q.y : (double)q.y * exp2(((double)q.x - (double)m) * c);
+      z += q.x == -INFINITY ? (double)q.y : (double)(q.y * __builtin_amdgcn_exp2f((q.x - m) * c));
     }
     for (int off = per / 2; off >= 1; off /= 2) z += __shfl_xor(z, off);
     if (there && s == 0) {
