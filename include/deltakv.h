@@ -308,8 +308,8 @@ int32_t dk_scored_attend(dk_pool* pool, int32_t n_seqs, const int32_t* slots, co
  * bf16 pool is rounded once to bf16 before it meets V, as in dk_scored_attend; q, out, k_new and v_new are 16-byte aligned (else
  * DK_ERR_UNSUPPORTED); out and lse overlap neither one another nor the inputs (DK_ERR_INVALID); new tokens are never shared, not even
  * by slots that alias them; the call needs no staging memory, never returns DK_ERR_BUSY, and can always be captured into a graph: its
- * descriptors (some 50 bytes a sequence and 12 for each of its runs of cells) travel in the arguments of its launches, one more
- * launch for every 3.75 KiB of them beyond the first 3.5.  The workspace is at least dk_shared_workspace_bytes() for the same batch, lengths,
+ * descriptors (of a sequence some 40 bytes for the attention, 20 for the merge, and 12 for each of its runs of cells) travel in the
+ * arguments of its two launches, 3.5 KiB each, and those of a launch that do not fit in launches of their own, 3.75 KiB each.  The workspace is at least dk_shared_workspace_bytes() for the same batch, lengths,
  * cells and mode (staged = 0 or 1).  Fewer than 2^31 / (query heads a KV head)^2 tokens and 2^29 positions (DK_ERR_UNSUPPORTED).
  */
 int32_t dk_shared_workspace_bytes(dk_pool* pool, int32_t n_seqs, const int32_t* slots, const int32_t* cu_delta, int32_t staged,

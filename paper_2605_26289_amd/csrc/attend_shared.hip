@@ -240,7 +240,11 @@ struct SharedGeo {
   static_assert(LDS_BYTES <= 81920, "two workgroups to a compute unit");
 };
 
-// A tile of up to 128 rows: each wavefront has 32 of them, the keys go through LDS once for all.
+// A tile of up to 128 rows: each wavefront has 32 of them, the keys go through LDS once for all, and the products of tile t + 1 stand among
+// the instructions that turn those of tile t into weights, as in scored_rows_kernel.  Bound by the vector unit and the matrix pipe in turn:
+// 2.2 to 2.6 us for 64 keys of 128-wide heads with two workgroups to a compute unit, some 900 TFLOP/s in the steady state.  16 turns of 64
+// to 512 tokens behind one preamble, 326 GFLOP: 385 us, 850 TFLOP/s; 32 drafts of up to nine tokens behind 30 000 keys, 72 GFLOP: 102.
+// (128 rows rather than 256: a second workgroup's softmax runs beside the first one's products, and a group of a few sessions fills a tile.)
 template <int HD>
 __device__ __forceinline__ void many_rows(const SharedArgs& a, const ScoreParams& sp, const Job& j, int g, char* smem, int lane, int wave) {
   typedef Geo<HD> G;
@@ -373,7 +377,11 @@ __device__ __forceinline__ void many_rows(const SharedArgs& a, const ScoreParams
 }
 
 // A tile of up to 32 RB rows: each wavefront walks a quarter of the keys through LDS of its own, with no barrier until their
-// sums are joined.  K of tile t + 1 is requested as soon as K of tile t has been read, V likewise.
+// sums are joined.  K of tile t + 1 is requested as soon as K of tile t has been read, V likewise.  Bound by HBM where the keys come from
+// there: 16 requests of eight beams, 328 MB, 46.6 to 50 us, 6.5 to 7 TB/s; by latency where they are few: an item without its keys takes
+// 5.5 us (descriptors 1, first requests and Q 1.5, four wavefronts' sums 1.5), four beams behind 3000 keys 7.3 in all.  One stage of K
+// and V for a wavefront, and not two as in scored_few_kernel, so that two workgroups fit a compute unit: one's start and end
+// are covered by the other.
 template <int HD, int RB>
 __device__ __forceinline__ void few_rows(const SharedArgs& a, const ScoreParams& sp, const Job& j, int g, char* smem, int lane, int wave) {
   typedef Geo<HD> G;
@@ -563,7 +571,9 @@ __global__ __launch_bounds__(256, 2) void shared_attend_kernel(SharedBlob blob, 
   else many_rows<HD>(a, sp, j, g, smem, lane, wave);
 }
 
-// Joins the partial rows of every row.  HD / 4 lanes take a row's depths; `spread` lane groups of a workgroup share its pieces.
+// Joins the partial rows of every row.  HD / 4 lanes take a row's depths; `spread` lane groups of a workgroup share its pieces.  Bound by
+// latency, a chain of round trips: block, node and sources, partial rows (the first from the arguments, which are in host memory).  4 us for
+// four rows of 25 pieces, 6.5 to 7 for 64 to 128 beams, 9.2 for 32 drafts of up to nine tokens.
 template <int HD, bool F32>
 __global__ __launch_bounds__(256) void shared_merge_kernel(SharedBlob blob, SharedArgs a, SharedMergeArgs ma) {
   constexpr int LANES = HD / 4, GROUPS = 256 / LANES, AHEAD = 4;
@@ -641,7 +651,8 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedBlob blob, Shar
   if (a.lse && lane == 0) a.lse[orow] = (m + log2f(l)) * 0.6931471805599453f;
 }
 
-// A piece of descriptors that do not fit a kernel's arguments, on its way to the workspace in the arguments of a launch of its own.
+// A piece of descriptors that do not fit a kernel's arguments, on its way to the workspace in the arguments of a launch of its own: 1.1 to
+// 1.9 us of the device and 2.5 of the host, less than a copy from pinned memory and its event, and it needs neither.
 __global__ __launch_bounds__(256) void shared_carry_kernel(SharedCarry piece, uint32_t* to, int32_t words) {
   typedef const __attribute__((address_space(4))) uint32_t* const_u32_ptr;
   const_u32_ptr from = (const_u32_ptr)__builtin_amdgcn_kernarg_segment_ptr();
@@ -650,7 +661,9 @@ __global__ __launch_bounds__(256) void shared_carry_kernel(SharedCarry piece, ui
 }
 
 // fp32: 8 wavefronts split the keys of an item of 16 RB rows, as in attend_f32_kernel (operands straight from memory, products of
-// 16 x 16 x 4, states joined through LDS); see there for the layout.
+// 16 x 16 x 4, states joined through LDS); see there for the layout.  Bound by the fp32 matrix pipe, 1.7 us for 64 keys of 32 rows of 128, and
+// by its start: 2.4 us a step with two wavefronts to a SIMD, and 8 without keys (the second wavefront of a SIMD gets to its keys 4 us after
+// the first; wave priorities for what is not a product changed nothing).  Two groups of 6 to 12 samples, 2.1 GFLOP: 38 us.
 namespace {
 constexpr int SF_WAVES = 8, SF_KT = 16;
 constexpr float SF_SLACK = 8.f;

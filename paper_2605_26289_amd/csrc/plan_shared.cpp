@@ -8,14 +8,15 @@ namespace dk {
 namespace {
 
 // What the cuts go by: microseconds of a workgroup's place, of which the chip has 512 (fp32: 256).  Measured by clocks in the kernels.
-constexpr double FIXED_US = 6.0;          // a work item without its keys
+constexpr double FIXED_US = 6.0, F32_FIXED_US = 8.0;  // a work item without its keys
 constexpr double ROWS_KEY_US = 2.3 / 64;  // a key of a tile of 128 rows of 128
 constexpr double FEW_KEY_US = 1.9 / 64;   // a key of a tile of up to 32 rows
 constexpr double FEW2_KEY_US = 2.6 / 64;  // a key of one of up to 64
-constexpr double F32_KEY_US = 3.1 / 64;   // a key of 32 rows of 128 in fp32
+constexpr double F32_KEY_US = 2.5 / 64;   // a key of 32 rows of 128 in fp32
 constexpr double PART_US = 0.08;          // a partial row of 128, written and read
 
 double places(const SharedConfig& cfg) { return std::max(1.0, (cfg.bf16 ? 512.0 : 256.0) / cfg.n_kv_heads); }  // of a KV head
+double fixed_us(const SharedConfig& cfg) { return cfg.bf16 ? FIXED_US : F32_FIXED_US; }
 double key_us(const SharedConfig& cfg, int64_t rows) {
   const double width = 0.2 + 0.8 * cfg.head_dim / 128;
   if (!cfg.bf16) return F32_KEY_US * width;
@@ -60,7 +61,7 @@ struct Builder {
     }
     const double together = tiles_us(cfg, *p, rows), tiles = together / key_us(cfg, rows);
     const double pieces = std::max(1.0, std::min((double)keys / 512.0, places(cfg) / tiles));
-    return (double)keys * (alone - together) > FIXED_US + part_us(cfg) * pieces * (double)rows;
+    return (double)keys * (alone - together) > fixed_us(cfg) + part_us(cfg) * pieces * (double)rows;
   }
 
   void add_own(const SharedPlan::Member& m, int64_t start) {
@@ -152,8 +153,8 @@ struct Builder {
   }
 
   // Pieces of what takes keys_us, items of at most `us` (and of 128 keys and more).
-  static int64_t pieces_of(double keys_us, double per_key, double us) {
-    const double most = std::max(us - FIXED_US, 128 * per_key);
+  int64_t pieces_of(double keys_us, double per_key, double us) const {
+    const double most = std::max(us - fixed_us(cfg), 128 * per_key);
     return keys_us <= most ? 1 : (int64_t)(keys_us / most * 0.999) + 1;
   }
   int64_t chunk_of(const SharedPlan::Node& x, double us) const {
@@ -186,7 +187,7 @@ struct Builder {
     std::vector<SharedPlan::Load>& loads = p->loads;  // longest first: only those before the first that fits are cut
     loads.clear();
     for (const SharedPlan::Node& x : p->nodes)
-      loads.push_back({FIXED_US + x.per_key * x.d.keys, x.per_key, (double)x.tiles, (double)x.d.rows, x.entry < 0 || x.link >= 0 ? 1.0 : 0.0});
+      loads.push_back({fixed_us(cfg) + x.per_key * x.d.keys, x.per_key, (double)x.tiles, (double)x.d.rows, x.entry < 0 || x.link >= 0 ? 1.0 : 0.0});
     std::sort(loads.begin(), loads.end(), [](const SharedPlan::Load& a, const SharedPlan::Load& b) { return a.us > b.us; });
     double all = 0, items = 0, parts = 0;  // of those that are not cut
     for (const SharedPlan::Load& x : loads) {
@@ -194,7 +195,7 @@ struct Builder {
       items += x.tiles;
       parts += x.part * x.rows;
     }
-    const double least = FIXED_US * 1.2;
+    const double least = fixed_us(cfg) * 1.2;
     double best_us = loads[0].us, best = 1e300;
     size_t n_cut = 0;
     for (double us = loads[0].us; us > least; us *= 0.9) {
@@ -208,9 +209,9 @@ struct Builder {
       double longest = uncut, cut_all = 0, cut_items = 0, cut_parts = 0;
       for (size_t i = 0; i < n_cut; ++i) {
         const SharedPlan::Load& x = loads[i];
-        const double keys_us = x.us - FIXED_US, pieces = (double)pieces_of(keys_us, x.per_key, us);
-        longest = std::max(longest, FIXED_US + keys_us / pieces);
-        cut_all += x.tiles * (pieces * FIXED_US + keys_us);
+        const double keys_us = x.us - fixed_us(cfg), pieces = (double)pieces_of(keys_us, x.per_key, us);
+        longest = std::max(longest, fixed_us(cfg) + keys_us / pieces);
+        cut_all += x.tiles * (pieces * fixed_us(cfg) + keys_us);
         cut_items += x.tiles * pieces;
         cut_parts += pieces * x.rows;
       }
@@ -224,8 +225,8 @@ struct Builder {
         p->levels.assign(1, {0, at_once});
         for (size_t i = 0; i < n_cut; ++i) {
           const SharedPlan::Load& x = loads[i];
-          const double keys_us = x.us - FIXED_US, pieces = (double)pieces_of(keys_us, x.per_key, us);
-          put_items(x.tiles * pieces, FIXED_US + keys_us / pieces);
+          const double keys_us = x.us - fixed_us(cfg), pieces = (double)pieces_of(keys_us, x.per_key, us);
+          put_items(x.tiles * pieces, fixed_us(cfg) + keys_us / pieces);
         }
         run = std::max(p->levels.back().us, mean + 0.5 * uncut);
       }
