@@ -30,17 +30,20 @@ __device__ __forceinline__ const T* shared_desc(const SharedArgs& a, const T* p)
 
 __device__ __forceinline__ int shared_token(const SharedArgs& a, int row) { return a.gmagic ? (int)__umulhi((uint32_t)row, a.gmagic) : row; }
 
-// The last of n ascending numbers that is not above x, 64 at a time by a vector load: one round trip.  (Descriptors in the arguments are in
-// host memory, and every cache line of them that a compute unit takes by scalar loads costs about as much again: the search by scalar
-// loads, with the lines asked for beforehand, made the merge of 64 entries 9.4 us instead of 5.5.)
+// The last of n ascending numbers that is not above x (the first is not), 64 of them at a time by a vector load: a round trip up to 64, two up
+// to 4096.  (Descriptors in the arguments are in host memory, and every cache line of them that a compute unit takes by scalar loads
+// costs about as much again: the search by scalar loads, with the lines asked for beforehand, made the merge of 64 entries 9.4 us instead
+// of 5.5.)
 __device__ __forceinline__ int last_not_above(const int32_t* p, int n, int x, int lane) {
-  int count = 0;
-  for (int i = 0; i < n; i += 64) {
-    const int at = i + lane;
+  int first = 0, range = n;
+  while (true) {
+    const int step = (range + 63) >> 6, at = first + lane * step;
     const int v = p[min(at, n - 1)];
-    count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(at < n && v <= x));
+    const int count = __builtin_popcountll(__builtin_amdgcn_ballot_w64(at < first + range && v <= x));
+    first = __builtin_amdgcn_readfirstlane(first + max(count - 1, 0) * step);
+    if (step == 1) return first;
+    range = min(step, n - first);
   }
-  return __builtin_amdgcn_readfirstlane(count - 1);
 }
 
 // A work item: rows row0 .. row0 + nrows - 1 of the node against positions kv_lo .. kv_hi - 1.

@@ -23,6 +23,41 @@ def test_descriptors_travel_all_ways(members, what, dtype):
     assert dk.last_plan(t.pool.handle)["merges"] == members
 
 
+@pytest.mark.parametrize("n", [64, 65, 1100, 4600])
+def test_many_sequences_behind_one_prompt(n):
+    """One token each: every work item and every merged row is found among that many."""
+    hq, hkv, d, prompt = 2, 1, 64, 150
+    pool = DevicePool(n + 1, 16 * (n + 20), hq, hkv, d, "bf16", granule_cells=16)
+    root, *slots = [pool.acquire() for _ in range(n + 1)]
+    rng = np.random.default_rng(26)
+    k, v = (wl.normal(rng, (prompt, hkv, d), "bf16") for _ in range(2))
+    kn, vn = (wl.normal(rng, (n, hkv, d), "bf16") for _ in range(2))
+    q = wl.normal(rng, (n, hq, d), "bf16")
+    to = lambda x: torch.from_numpy(np.ascontiguousarray(x)).to("cuda", torch.bfloat16)
+    pool.append([root], [0, prompt], to(k), to(v))
+    for s in slots:
+        pool.alias(root, s, prompt)
+    cu = np.arange(n + 1, dtype=np.int32)
+    pool.append(slots, cu, to(kn), to(vn))
+    lse = torch.empty((n, hq), dtype=torch.float32, device="cuda")
+    got = pool.shared_attend(slots, cu, to(q), 0.125, lse=lse).float().cpu().numpy()
+    assert dk.last_plan(pool.handle)["merges"] == n
+    lse = lse.cpu().numpy()
+    s0 = np.einsum("nhd,kd->nhk", q.astype(np.float64), k[:, 0].astype(np.float64)) * 0.125
+    s1 = np.einsum("nhd,nd->nh", q.astype(np.float64), kn[:, 0].astype(np.float64)) * 0.125
+    top = np.maximum(s0.max(-1), s1)
+    p0, p1 = np.exp(s0 - top[..., None]), np.exp(s1 - top)
+    z = p0.sum(-1) + p1
+    new = vn[:, 0].astype(np.float64)[:, None]
+    o = (p0 @ v[:, 0].astype(np.float64) + p1[..., None] * new) / z[..., None]
+    mag = (p0 @ np.abs(v[:, 0]).astype(np.float64) + p1[..., None] * np.abs(new)) / z[..., None]
+    size = np.maximum((np.abs(q).astype(np.float64) @ np.abs(k[:, 0]).astype(np.float64).T).max(-1),
+                      np.einsum("nhd,nd->nh", np.abs(q).astype(np.float64), np.abs(kn[:, 0]).astype(np.float64))) * 0.125
+    tol, ltol = bounds((o, top + np.log(z), mag, size), "bf16", prompt + 1, d)
+    assert (np.abs(got - o) <= tol).all()
+    assert (np.abs(lse - (top + np.log(z))) <= ltol).all()
+
+
 def test_probes_see_shared_attention():
     t = Tree(22, 4, 2, 64, "bf16", [(None, 0, 900)] + [(0, 900, 3) for _ in range(6)])
     dk.set_attend_timing(t.pool.handle, 8)
