@@ -15,7 +15,7 @@
 //                        thousand), T is raised to the n-th of those that came and the lists are gone through again.
 // Scores are made and compared in fp64: rows of one group differ by the logs of sums of 10^5 terms, and two continuations may be close.
 //
-// Measured (kernel times): 64 groups of eight rows of 128 256 bf16 logits, n = 16: chunks 24.9 us (131 MB, 5.3 TB/s; 500 vector
+// Measured (kernel times): 64 groups of eight rows of 128 256 bf16 logits, n = 16: chunks 24.6 us (131 MB, 5.3 TB/s; some 450 vector
 // instructions a wavefront keep the SIMDs busy three fifths of that, six wavefronts to a SIMD instead of five give 2 %), groups 12.7; with
 // lists of the n best logits themselves, put in order, the chunks took 36.  One group of four such rows, n = 8: 3.8 and 9.7; 40 groups
 // of up to ten rows of 50 003 fp32 logits, most of them -infinity: 10.9 and 12.2.  The groups' kernel is a chain of round trips and of
@@ -78,6 +78,50 @@ __device__ __forceinline__ float element_of(const uint4& v, int j) {
 
 }  // namespace
 
+namespace {
+
+// Over all lanes: quads, eights and sixteens by data-parallel moves, rows of sixteen and halves by swaps.  (By shuffles through LDS,
+// six round trips of it each, and 16 steps for the thresholds, the chunks of 64 x 8 rows took 25.4 us instead of 24.6.)
+template <int CTRL>
+__device__ __forceinline__ float dpp_move(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+template <typename OP>
+__device__ __forceinline__ float over_lanes(float x, OP op) {
+  x = op(x, dpp_move<0xB1>(x));   // lanes 1, 0, 3, 2 of a quad
+  x = op(x, dpp_move<0x4E>(x));   // lanes 2, 3, 0, 1
+  x = op(x, dpp_move<0x141>(x));  // the other quad of eight lanes
+  x = op(x, dpp_move<0x140>(x));  // the other eight of a row
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// nth_and_kth_largest, in fewer steps where the n largest are within two powers of two of the largest of all, `top` (uniform).
+template <int BITS>
+__device__ __forceinline__ float2 nth_and_kth_from(float x, float top, int n, int k) {
+  const uint32_t key = ordered(x), from = ordered(top) >> 24 << 24;
+  uint32_t tn = 0, tk = 0;
+  const auto search = [&](int high) __attribute__((always_inline)) {
+#pragma unroll
+    for (int bit = high; bit >= 32 - BITS; --bit) {
+      const uint32_t un = tn | (1u << bit), uk = tk | (1u << bit);
+      if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(key >= un)) >= n) tn = un;
+      if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(key >= uk)) >= k) tk = uk;
+    }
+  };
+  if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(key >= from)) >= max(n, k)) {
+    tn = tk = (uint32_t)__builtin_amdgcn_readfirstlane((int)from);
+    search(23);
+  } else {
+    search(31);
+  }
+  return make_float2(from_ordered(max(tn, 0x007fffffu)), from_ordered(max(tk, 0x007fffffu)));
+}
+
+}  // namespace
+
 // A chunk is LP_THREADS * UNROLL * VEC logits; element VEC u + j of a thread is id base + (u LP_THREADS + thread) VEC + j.
 template <typename T, int UNROLL, bool ONCE>
 __global__ __launch_bounds__(LP_THREADS) void beam_chunk_kernel(BeamArgs a, int32_t n_chunks, BeamPart* __restrict__ parts,
@@ -115,7 +159,7 @@ __global__ __launch_bounds__(LP_THREADS) void beam_chunk_kernel(BeamArgs a, int3
   float mine = x[0];
 #pragma unroll
   for (int e = 0; e < N; e += 2) asm("v_max3_f32 %0, %1, %2, %3" : "=v"(mine) : "v"(mine), "v"(x[e]), "v"(x[e + 1]));
-  const float m = wave_max(mine);
+  const float m = over_lanes(mine, [](float p, float q) { return fmaxf(p, q); });
   const float c = (float)a.scale * LOG2E, mr = m == -INFINITY ? 0.f : m, mc = mr * c;
   float s0 = 0.f, s1 = 0.f;
   // (eight at a time: an exponential's result may not be used by the very next instruction)
@@ -135,9 +179,9 @@ __global__ __launch_bounds__(LP_THREADS) void beam_chunk_kernel(BeamArgs a, int3
   };
   if (__builtin_fabsf(mc) <= 1048576.f) sums([&](float v) { return __builtin_fmaf(v, c, -mc); });
   else sums([&](float v) { return (v - mr) * c; });  // the difference first: it may be small against what is multiplied
-  s0 = wave_sum(s0 + s1);
+  s0 = over_lanes(s0 + s1, [](float p, float q) { return p + q; });
   const float r = __builtin_fabsf(mc) <= 1048576.f ? __builtin_fmaf(mr, c, -mc) : 0.f;  // what rounding m c took off
-  const float2 t = nth_and_kth_largest<sizeof(T) == 2 ? 16 : 20>(mine, a.n_out, (a.n_out + LP_WAVES - 1) / LP_WAVES);
+  const float2 t = nth_and_kth_from<sizeof(T) == 2 ? 16 : 18>(mine, m, a.n_out, (a.n_out + LP_WAVES - 1) / LP_WAVES);
   if (lane == 0) wave_part[wave] = make_float4(m, s0 * __builtin_amdgcn_exp2f(-r), t.x, t.y);
   __syncthreads();
   float reach = wave_part[0].z, every = wave_part[0].w, top = wave_part[0].x;
