@@ -18,7 +18,7 @@
 // Measured (kernel times): 64 groups of eight rows of 128 256 bf16 logits, n = 16: chunks 24.6 us (131 MB, 5.3 TB/s; some 450 vector
 // instructions a wavefront keep the SIMDs busy three fifths of that, six wavefronts to a SIMD instead of five give 2 %), groups 12.7; with
 // lists of the n best logits themselves, put in order, the chunks took 36.  One group of four such rows, n = 8: 3.8 and 9.7; 40 groups
-// of up to ten rows of 50 003 fp32 logits, most of them -infinity: 10.9 and 12.2.  The groups' kernel is a chain of round trips and of
+// of up to ten rows of 50 003 fp32 logits, a third of them nearly all -infinity: 10.7 and 12.2.  The groups' kernel is a chain of round trips and of
 // exchanges over LDS: load 1.1 us, sums 1.2 to 1.7, T 1.3, lists 1.8 to 2.6, logits 2 to 4, places 0.5 to 1; of 256 lanes instead
 // of 512 it takes 10.3, 14.7 and 14.0, of 1024 10.8, 14.5 and 13.2.
 #include <hip/hip_runtime.h>
@@ -29,7 +29,7 @@ namespace dk {
 
 namespace {
 
-constexpr int BEAM_THREADS = 512, BEAM_WAVES = BEAM_THREADS / 64;
+constexpr int BEAM_THREADS = 512;
 constexpr int BEAM_ID_BITS = 20;
 static_assert(BEAM_MAX_VOCAB <= 1 << BEAM_ID_BITS && BEAM_MAX_ROWS <= 1 << (64 - 32 - BEAM_ID_BITS), "row, logit and token in 64 bits");
 constexpr int BEAM_MAX_LISTS = BEAM_MAX_ROWS * (int)((BEAM_MAX_VOCAB + LP_THREADS * LP_UNROLL * 4 - 1) / (LP_THREADS * LP_UNROLL * 4));

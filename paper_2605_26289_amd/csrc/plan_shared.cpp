@@ -183,11 +183,11 @@ struct Builder {
   // until the last of those that are cut are done, longest first, or the mean of the places' loads and half of the longest of the others;
   // and the partial rows' way to memory and back.
   void choose_pieces() {
-    const double at_once = places(cfg);
+    const double at_once = places(cfg), fixed = fixed_us(cfg);
     std::vector<SharedPlan::Load>& loads = p->loads;  // longest first: only those before the first that fits are cut
     loads.clear();
     for (const SharedPlan::Node& x : p->nodes)
-      loads.push_back({fixed_us(cfg) + x.per_key * x.d.keys, x.per_key, (double)x.tiles, (double)x.d.rows, x.entry < 0 || x.link >= 0 ? 1.0 : 0.0});
+      loads.push_back({fixed + x.per_key * x.d.keys, x.per_key, (double)x.tiles, (double)x.d.rows, x.entry < 0 || x.link >= 0 ? 1.0 : 0.0, 1, 0});
     std::sort(loads.begin(), loads.end(), [](const SharedPlan::Load& a, const SharedPlan::Load& b) { return a.us > b.us; });
     double all = 0, items = 0, parts = 0;  // of those that are not cut
     for (const SharedPlan::Load& x : loads) {
@@ -195,7 +195,7 @@ struct Builder {
       items += x.tiles;
       parts += x.part * x.rows;
     }
-    const double least = fixed_us(cfg) * 1.2;
+    const double least = fixed * 1.2;
     double best_us = loads[0].us, best = 1e300;
     size_t n_cut = 0;
     for (double us = loads[0].us; us > least; us *= 0.9) {
@@ -208,12 +208,14 @@ struct Builder {
       const double uncut = n_cut < loads.size() ? loads[n_cut].us : 0;
       double longest = uncut, cut_all = 0, cut_items = 0, cut_parts = 0;
       for (size_t i = 0; i < n_cut; ++i) {
-        const SharedPlan::Load& x = loads[i];
-        const double keys_us = x.us - fixed_us(cfg), pieces = (double)pieces_of(keys_us, x.per_key, us);
-        longest = std::max(longest, fixed_us(cfg) + keys_us / pieces);
-        cut_all += x.tiles * (pieces * fixed_us(cfg) + keys_us);
-        cut_items += x.tiles * pieces;
-        cut_parts += pieces * x.rows;
+        SharedPlan::Load& x = loads[i];
+        const double keys_us = x.us - fixed;
+        x.pieces = (double)pieces_of(keys_us, x.per_key, us);
+        x.piece_us = fixed + keys_us / x.pieces;
+        longest = std::max(longest, x.piece_us);
+        cut_all += x.tiles * (x.pieces * fixed + keys_us);
+        cut_items += x.tiles * x.pieces;
+        cut_parts += x.pieces * x.rows;
       }
       const double joined = part_us(cfg) * (parts + cut_parts) / at_once + (parts + cut_parts > 0 ? 3.0 : 0.0);
       const double mean = (all + cut_all) / at_once;
@@ -223,11 +225,7 @@ struct Builder {
         run = mean + 0.5 * longest;
       } else if (items + cut_items > at_once) {
         p->levels.assign(1, {0, at_once});
-        for (size_t i = 0; i < n_cut; ++i) {
-          const SharedPlan::Load& x = loads[i];
-          const double keys_us = x.us - fixed_us(cfg), pieces = (double)pieces_of(keys_us, x.per_key, us);
-          put_items(x.tiles * pieces, fixed_us(cfg) + keys_us / pieces);
-        }
+        for (size_t i = 0; i < n_cut; ++i) put_items(loads[i].tiles * loads[i].pieces, loads[i].piece_us);
         run = std::max(p->levels.back().us, mean + 0.5 * uncut);
       }
       const double est = run + joined;

@@ -38,6 +38,7 @@ struct SharedPlan {
   };
   struct Load {  // of a node that is not cut: time of an item, of a key; row tiles, rows; 1: it leaves partial rows however it is cut
     double us, per_key, tiles, rows, part;
+    double pieces, piece_us;  // of the cut that is looked at
   };
   std::vector<Load> loads;
   struct Level {  // places that are free from then on

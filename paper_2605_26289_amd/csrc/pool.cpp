@@ -44,28 +44,36 @@ int64_t GranuleAllocator::take_fresh() {
 int64_t GranuleAllocator::take_first() {
   if (runs_.empty()) return -1;
   const int64_t g = runs_.begin()->first;
-  remove_from_run(runs_.begin(), g);
+  auto run = runs_.extract(runs_.begin());  // (the run's own entry, one granule shorter)
+  if (--run.mapped() > 0) {
+    ++run.key();
+    runs_.insert(runs_.begin(), std::move(run));
+  }
+  --free_;
   return g;
 }
 
 void GranuleAllocator::give_back(int64_t g) {
-  int64_t s = g, l = 1;
-  auto next = runs_.find(g + 1);
-  if (next != runs_.end()) {
-    l += next->second;
-    runs_.erase(next);
-  }
-  auto it = runs_.lower_bound(g);
-  if (it != runs_.begin()) {
-    --it;
-    if (it->first + it->second == g) {
-      s = it->first;
-      l += it->second;
-      runs_.erase(it);
+  const auto next = runs_.lower_bound(g);
+  const bool joins_next = next != runs_.end() && next->first == g + 1;
+  ++free_;
+  if (next != runs_.begin()) {
+    const auto before = std::prev(next);
+    if (before->first + before->second == g) {
+      before->second += 1 + (joins_next ? next->second : 0);
+      if (joins_next) runs_.erase(next);
+      return;
     }
   }
-  runs_[s] = l;
-  ++free_;
+  if (joins_next) {  // the run's own entry, one granule longer
+    const auto hint = std::next(next);
+    auto run = runs_.extract(next);
+    run.key() = g;
+    ++run.mapped();
+    runs_.insert(hint, std::move(run));
+  } else {
+    runs_.emplace_hint(next, g, 1);
+  }
 }
 
 // ---------------------------------------------------------------- Node
@@ -258,9 +266,11 @@ void Pool::add_extents(const Node& n, int64_t lo, int64_t hi, std::vector<Extent
     add(n.borrow_cell + lo - n.base, lo, std::min(hi, lent) - lo);
     lo = std::min(hi, lent);
   }
-  while (lo < hi) {
-    const int64_t o = lo - lent, take = std::min(hi - lo, n.gr - o % n.gr);
-    add(n.granules[(size_t)(o / n.gr)] * n.gr + o % n.gr, lo, take);
+  if (lo >= hi) return;
+  int64_t g = (lo - lent) / n.gr, off = (lo - lent) - g * n.gr;
+  for (; lo < hi; ++g, off = 0) {
+    const int64_t take = std::min(hi - lo, n.gr - off);
+    add(n.granules[(size_t)g] * n.gr + off, lo, take);
     lo += take;
   }
 }
