@@ -1,4 +1,4 @@
-"""Plans of attention for batches that share cells (host C++, no GPU): compiles the planner together with a checker and runs it."""
+"""Plans of attention for batches that share cells (host C++, no GPU): compiles the planner together with a program that counts what plans hold, and runs it."""
 import os
 import shutil
 import subprocess
