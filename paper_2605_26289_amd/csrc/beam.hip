@@ -403,9 +403,8 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
     const int n_reached = reached;
     __syncthreads();
     if (n_reached <= BEAM_LANES) {
-      // where they are many -- one row leads, and the first T came from other rows' lists -- T rises by what they say themselves (1.7 us;
-      // each round of `expand` takes 2.6)
-      if (n_reached > n && n_reached * unroll > BEAM_THREADS) {
+      // T by what they say themselves
+      const auto raise = [&]() __attribute__((always_inline)) {
         const uint32_t higher = nth_largest(lane_key, n_reached);
         uint32_t which[BEAM_LANES / BEAM_THREADS];
         bool keep[BEAM_LANES / BEAM_THREADS];
@@ -416,7 +415,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
           which[i] = keep[i] ? lanes[k] : 0;
         }
         if ((uint64_t)higher << 32 > least.score) least = {(uint64_t)higher << 32, 0};
-        if (tid == 0) reached = 0;
+        if (tid == 0) came = reached = 0;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < BEAM_LANES / BEAM_THREADS; ++i) {
@@ -424,9 +423,30 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
           if (keep[i]) lanes[to] = which[i];
         }
         __syncthreads();
-      }
+      };
+      // At once where there is no T yet (few lists hold anything: a request's first step), or where they are many -- one row leads, and T came from
+      // other rows' lists; 1.7 us, a round of `expand` takes 2.6.  Else where so much reached the T there is that the places would take
+      // longer (without the second look one row of 6548 logits and 32 continuations took 70 us).
+      const bool early = n_reached > n && (least.score <= 1 || n_reached * unroll > BEAM_THREADS);
+      if (early) raise();
       expand();
-    } else {  // more lanes than there is room for: list by list
+      __syncthreads();
+      const bool late = !early && n_reached > n && came > BEAM_CAP / 2;
+      __syncthreads();
+      if (late) {
+        raise();
+        expand();
+      }
+    } else {
+      // more lanes than there is room for: T from those that came, and the lists again; if that is no higher, list by list
+      const uint32_t higher = nth_largest(lane_key, BEAM_LANES);
+      if ((uint64_t)higher << 32 > least.score) {
+        least = {(uint64_t)higher << 32, 0};
+        __syncthreads();
+        if (tid == 0) reached = 0;
+        __syncthreads();
+        continue;
+      }
       for (int list = 0; list < n_lists; ++list) {
         __syncthreads();
         if (tid == 0) reached = 0;

@@ -159,3 +159,44 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, out))
         assert np.array_equal(got[0].cpu().numpy(), oracle.beam_select(y, scores, [0, 4, 8], 8)[0])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [500, 6548, 20000])
+@pytest.mark.parametrize("lead", [None, 6.0])
+def test_first_steps_and_rows_that_lead(dtype, vocab, lead):
+    """One row of a group takes part, or leads by far: the bound is made of one row's logits alone."""
+    x, scores = draw(31, 60, vocab, "f32")
+    if dtype == "bf16":  # (few values to a bf16 row of this spread: scaled apart by rows, so that scores differ)
+        x = torch.from_numpy(x).to(torch.bfloat16).float().numpy()
+    cu = [0, 28, 60]
+    if lead is None:
+        scores[[i for i in range(60) if i not in (5, 28)]] = -INF
+    else:
+        scores[[5, 28]] += np.float32(lead * 3)
+    want = oracle.beam_select(x, scores, cu, 65, 0.69)
+    for n in (1, 8, 32, 64):
+        got = select(x, scores, cu, n, dtype, 0.69)
+        tol = SUM_TOL + 2.0 ** -24 * (np.abs(want[2][:, :n]) + 1)
+        assert (np.abs(got[2] - want[2][:, :n]) <= tol).all()
+        apart = np.abs(want[2][:, :n] - want[2][:, 1:n + 1])
+        if ((apart == 0) | (apart > 2 * SUM_TOL)).all():
+            assert np.array_equal(got[0], want[0][:, :n]) and np.array_equal(got[1], want[1][:, :n])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_lanes_reach_the_first_bound_than_there_is_room_for(dtype):
+    """Two rows of 40 lead by five and more: the bound is of other rows' logits, and thousands of the leading ones' reach it."""
+    x, scores = draw(32, 40, 60000, "f32")
+    if dtype == "bf16":
+        x = torch.from_numpy(x).to(torch.bfloat16).float().numpy()
+    scores[:] = -20.0 - np.linspace(0, 1, 40, dtype=np.float32)
+    scores[[7, 21]] = -14.5, -13.8
+    want = oracle.beam_select(x, scores, [0, 40], 64)
+    for n in (5, 63):
+        got = select(x, scores, [0, 40], n, dtype)
+        s = want[2][0, :n + 1]
+        assert (np.abs(got[2][0] - s[:n]) <= SUM_TOL + 2.0 ** -24 * (np.abs(s[:n]) + 1)).all()
+        apart = s[:-1] - s[1:]
+        if ((apart == 0) | (apart > 2 * SUM_TOL)).all():
+            assert np.array_equal(got[0][0], want[0][0, :n]) and np.array_equal(got[1][0], want[1][0, :n])
