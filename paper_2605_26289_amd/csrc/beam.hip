@@ -17,7 +17,7 @@
 //
 // Measured (kernel times): 64 groups of eight rows of 128 256 bf16 logits, n = 16: chunks 24.6 us (131 MB, 5.3 TB/s; some 450 vector
 // instructions a wavefront keep the SIMDs busy three fifths of that, six wavefronts to a SIMD instead of five give 2 %), groups 12.7; with
-// lists of the n best logits themselves, put in order, the chunks took 36.  One group of four such rows, n = 8: 3.8 and 9.7; 40 groups
+// lists of the n best logits themselves, put in order, the chunks took 36.  One group of four such rows, n = 8: 3.6 and 10.2; 40 groups
 // of up to ten rows of 50 003 fp32 logits, a third of them nearly all -infinity: 10.7 and 12.2.  The groups' kernel is a chain of round trips and of
 // exchanges over LDS: load 1.1 us, sums 1.2 to 1.7, T 1.3, lists 1.8 to 2.6, logits 2 to 4, places 0.5 to 1; of 256 lanes instead
 // of 512 it takes 10.3, 14.7 and 14.0, of 1024 10.8, 14.5 and 13.2.
@@ -299,16 +299,28 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
   // The n-th largest of some numbers in LDS but for the last bits (2^-8 of a score and less), 0 if there are fewer; every wavefront
   // finds it by itself.
   const auto nth_largest = [&](const uint32_t* of, int count_of) __attribute__((always_inline)) {
-    constexpr int KEEP = 4;
+    constexpr int KEEP = 16;  // of a lane (where they were read again for every bit, 672 took 7 to 11 us)
     uint32_t mine[KEEP], t = 0;
 #pragma unroll
-    for (int i = 0; i < KEEP; ++i) mine[i] = lane + 64 * i < count_of ? of[lane + 64 * i] : 0u;
+    for (int i = 0; i < KEEP; ++i) mine[i] = 0;
+#pragma unroll
+    for (int i0 = 0; i0 < KEEP; i0 += 4) {
+      if (64 * i0 >= count_of) break;
+#pragma unroll
+      for (int i = i0; i < i0 + 4; ++i) mine[i] = lane + 64 * i < count_of ? of[lane + 64 * i] : 0u;
+    }
     for (int bit = 31; bit >= 15; --bit) {
       const uint32_t u = t | 1u << bit;
       int count = __builtin_popcountll(__builtin_amdgcn_ballot_w64(mine[0] >= u));
       if (count_of > 64) {
 #pragma unroll
-        for (int i = 1; i < KEEP; ++i) count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(mine[i] >= u));
+        for (int i = 1; i < 4; ++i) count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(mine[i] >= u));
+#pragma unroll
+        for (int i0 = 4; i0 < KEEP; i0 += 4) {
+          if (64 * i0 >= count_of) break;
+#pragma unroll
+          for (int i = i0; i < i0 + 4; ++i) count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(mine[i] >= u));
+        }
         for (int i = 64 * KEEP; i < count_of; i += 64) count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i + lane < count_of && of[i + lane] >= u));
       }
       if (count >= n) t = u;
