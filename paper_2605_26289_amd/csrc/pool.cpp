@@ -12,9 +12,18 @@ GranuleAllocator::GranuleAllocator(int64_t n) : tails_((size_t)std::max<int64_t>
 
 void GranuleAllocator::remove_from_run(std::map<int64_t, int64_t>::iterator it, int64_t g) {
   const int64_t s = it->first, l = it->second;
-  runs_.erase(it);
-  if (g > s) runs_[s] = g - s;
-  if (g + 1 < s + l) runs_[g + 1] = s + l - (g + 1);
+  if (l == 1) {
+    runs_.erase(it);
+  } else if (g == s) {  // the run's own entry, one granule shorter
+    const auto hint = std::next(it);
+    auto run = runs_.extract(it);
+    run.key() = g + 1;
+    run.mapped() = l - 1;
+    runs_.insert(hint, std::move(run));
+  } else {
+    if (g + 1 < s + l) runs_.emplace_hint(std::next(it), g + 1, s + l - (g + 1));  // (may throw: before anything changes)
+    it->second = g - s;
+  }
   --free_;
 }
 
@@ -90,16 +99,18 @@ int64_t Node::granules_needed(int64_t extra) const {
 
 void Node::grow(int64_t extra, bool anywhere) {
   const int64_t add = granules_needed(extra);
+  const size_t want = granules.size() + (size_t)add;
+  if (want > granules.capacity()) granules.reserve(std::max(want, 2 * granules.capacity()));  // a granule that is taken has its place
   for (int64_t i = 0; i < add; ++i) {
     int64_t g = -1;
     if (!granules.empty()) {
-      alloc->unmark_tail(granules.back());
       if (alloc->take(granules.back() + 1)) g = granules.back() + 1;
     } else if (borrow_cap > 0) {  // continue right behind the granule the first cells were borrowed from
       const int64_t after = (borrow_cell + borrow_cap) / gr;
       if (alloc->take(after)) g = after;
     }
     if (g < 0) g = anywhere ? alloc->take_first() : alloc->take_fresh();
+    if (!granules.empty()) alloc->unmark_tail(granules.back());
     granules.push_back(g);
     alloc->mark_tail(g);
   }
