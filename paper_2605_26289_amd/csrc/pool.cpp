@@ -459,6 +459,14 @@ int32_t Pool::reorder(int32_t n, const int32_t* slots, const int32_t* parents, R
     if (r->keeper[(size_t)parents[i]] != i && s.head && s.head->len > whole(*s.head)) ++need;
   }
   if (need > alloc_.free_count()) return ERR_NO_CELLS;
+  struct Unless {  // a call that throws keeps no reference to the states: they would count as shared from then on
+    Reorder* r;
+    ~Unless() {
+      if (!r) return;
+      r->before.clear();
+      r->moves.clear();
+    }
+  } failed{r};
   r->before.reserve((size_t)n);
   r->moves.reserve((size_t)need);
   std::vector<std::shared_ptr<Node>> heads((size_t)n);
@@ -474,7 +482,6 @@ int32_t Pool::reorder(int32_t n, const int32_t* slots, const int32_t* parents, R
     if (base > 0) {
       a = h;
       while (a->base >= base) a = a->parent;
-      a->frozen = std::max(a->frozen, base);
     }
     heads[(size_t)i] = std::make_shared<Node>(&alloc_, gr_, a, base);
     if (rest > 0) {
@@ -482,9 +489,12 @@ int32_t Pool::reorder(int32_t n, const int32_t* slots, const int32_t* parents, R
       r->moves.push_back({h->cell_of(keep), heads[(size_t)i]->cell_of(0), rest});
     }
   }
+  failed.r = nullptr;
   for (int32_t i = 0; i < n; ++i) {
     Slot& s = slots_[slots[i]];
-    set_head(s, std::move(heads[(size_t)i]));
+    std::shared_ptr<Node>& h = heads[(size_t)i];
+    if (h && r->keeper[(size_t)parents[i]] != i && h->parent) h->parent->frozen = std::max(h->parent->frozen, h->base);
+    set_head(s, std::move(h));
     s.len = r->before[(size_t)parents[i]].len;
   }
   return OK;

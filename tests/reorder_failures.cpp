@@ -28,6 +28,19 @@ void operator delete(void* p, std::size_t) noexcept { std::free(p); }
   } while (0)
 static long g_at = 0;
 
+static int64_t held(Pool& pool) {
+  int64_t h = -1;
+  pool.stats(&h, nullptr);
+  return h;
+}
+static int32_t slot_of(Pool& pool, int32_t tokens) {
+  int32_t s = -1;
+  CHECK(pool.acquire(0, 0, &s) == OK);
+  const int32_t cu[2] = {0, tokens};
+  CHECK(pool.append(1, &s, cu, nullptr, nullptr) == OK);
+  return s;
+}
+
 // A node that cannot grow takes no granule from the allocator, and no run of free ones is forgotten.
 static void granules() {
   long failures = 0;
@@ -77,9 +90,54 @@ static void granules() {
   CHECK(failures > 4);
 }
 
+// Whichever allocation of the call fails: every slot is what it was, and nothing refers to its cells but itself.
+static void out_of_memory() {
+  long failures = 0;
+  for (g_at = 0;; ++g_at) {
+    Pool pool(8, 0, 64 * 16, 16);
+    std::vector<int32_t> slots;
+    for (int i = 0; i < 6; ++i) slots.push_back(slot_of(pool, 40 + 3 * i));
+    std::vector<std::vector<int64_t>> before;
+    for (int32_t s : slots) {
+      before.emplace_back(64, -1);
+      CHECK(pool.cells(s, before.back().data(), 64) == OK);
+    }
+    const std::vector<int32_t> parents = {0, 0, 0, 3, 3, 1};
+    const int64_t full = held(pool);
+    Pool::Reorder re;
+    bool thrown = false;
+    g_fails = g_at;
+    try {
+      (void)pool.reorder(6, slots.data(), parents.data(), &re);
+    } catch (const std::bad_alloc&) {
+      thrown = true;
+    }
+    g_fails = -1;
+    if (!thrown) {
+      pool.settle_reorder(&re);
+      break;
+    }
+    ++failures;
+    CHECK(held(pool) == full);
+    for (size_t i = 0; i < slots.size(); ++i) {
+      int64_t len = 0;
+      CHECK(pool.length(slots[i], &len) == OK && len == 40 + 3 * (int64_t)i);
+      std::vector<int64_t> now(64, -1);
+      CHECK(pool.cells(slots[i], now.data(), 64) == OK && now == before[i]);
+    }
+    // nothing shares them: cells come back as soon as they are trimmed, all of them when the slots go
+    CHECK(pool.trim(slots[0], 8) == OK);
+    CHECK(held(pool) == full - 2 * 16);
+    for (int32_t s : slots) CHECK(pool.release(s) == OK);
+    CHECK(held(pool) == 0);
+  }
+  CHECK(failures > 10);
+}
+
 int main(int argc, char** argv) {
   const char* what = argc > 1 ? argv[1] : "";
   if (!std::strcmp(what, "granules")) granules();
+  else if (!std::strcmp(what, "out_of_memory")) out_of_memory();
   else return 2;
   std::printf("ok\n");
   return 0;

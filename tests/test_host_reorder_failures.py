@@ -29,3 +29,8 @@ def run_check(tmp_path, what, sanitizer):
 @pytest.mark.parametrize("sanitizer", [None, "address,undefined"])
 def test_a_failed_allocation_loses_no_granule(tmp_path, sanitizer):
     run_check(tmp_path, "granules", sanitizer)
+
+
+@pytest.mark.parametrize("sanitizer", [None, "address,undefined"])
+def test_a_failed_allocation_leaves_every_slot_as_it_was(tmp_path, sanitizer):
+    run_check(tmp_path, "out_of_memory", sanitizer)
