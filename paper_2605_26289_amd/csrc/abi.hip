@@ -494,6 +494,7 @@ int32_t dk_seq_reorder(dk_pool* pool, int32_t n, const int32_t* slots, const int
     dk::Pool::Reorder& r = pool->reordered;
     const int32_t rc = pool->meta.reorder(n, slots, parents, &r);
     if (rc != DK_OK) return rc;
+    // the pool is locked until it is settled or undone; nothing in between throws
     hipError_t e = hipSuccess;
     dk::KvMoves moves;
     int32_t count = 0;

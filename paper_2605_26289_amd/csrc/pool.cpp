@@ -430,7 +430,7 @@ int32_t Pool::append(int32_t n_seqs, const int32_t* slots, const int32_t* cu_del
 
 int32_t Pool::reorder(int32_t n, const int32_t* slots, const int32_t* parents, Reorder* r) {
   if (n < 0 || (n > 0 && (!slots || !parents))) return ERR_INVALID;
-  std::lock_guard<std::mutex> lk(mu_);
+  std::unique_lock<std::mutex> lk(mu_);
   r->before.clear();
   r->moves.clear();
   std::vector<char> seen(slots_.size(), 0);
@@ -497,11 +497,12 @@ int32_t Pool::reorder(int32_t n, const int32_t* slots, const int32_t* parents, R
     set_head(s, std::move(h));
     s.len = r->before[(size_t)parents[i]].len;
   }
+  r->lock = std::move(lk);
   return OK;
 }
 
 void Pool::undo_reorder(int32_t n, const int32_t* slots, Reorder* r) {
-  std::lock_guard<std::mutex> lk(mu_);
+  const std::unique_lock<std::mutex> lk = std::move(r->lock);
   for (int32_t i = 0; i < n && i < (int32_t)r->before.size(); ++i) {
     Slot& s = slots_[slots[i]];
     set_head(s, r->before[(size_t)i].head);
@@ -511,7 +512,7 @@ void Pool::undo_reorder(int32_t n, const int32_t* slots, Reorder* r) {
 }
 
 void Pool::settle_reorder(Reorder* r) {
-  std::lock_guard<std::mutex> lk(mu_);
+  const std::unique_lock<std::mutex> lk = std::move(r->lock);
   r->before.clear();
 }
 

@@ -127,7 +127,8 @@ class Pool {
   // parent takes its chain over as it is, itself if it is among them, else the first; every other one aliases what fills whole
   // quarters of granules (granules below 256 cells: whole ones) and gets cells of its own for the rest, which `moves` says where to copy from.  `before` keeps what the
   // slots were, so that undo_reorder() can put it back; settle_reorder() lets go of it (states that no slot has any more give their cells
-  // back there, so it is not left to the next call).
+  // back there, so it is not left to the next call).  After OK one of the two has to follow on the same thread, and until it does the pool
+  // is locked: a slot that another thread releases or trims in between could not be put back.
   struct Move {
     int64_t from, to, len;  // cells
   };
@@ -135,6 +136,7 @@ class Pool {
     std::vector<Slot> before;
     std::vector<Move> moves;
     std::vector<int32_t> keeper;
+    std::unique_lock<std::mutex> lock;
   };
   int32_t reorder(int32_t n, const int32_t* slots, const int32_t* parents, Reorder* r);
   void undo_reorder(int32_t n, const int32_t* slots, Reorder* r);

@@ -1,15 +1,19 @@
 // The bookkeeping of reordered states where something goes wrong on the way, on the host.  One check a run, by its name.
+#include <atomic>
+#include <chrono>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
 #include <new>
+#include <random>
+#include <thread>
 #include <vector>
 
 #include "../paper_2605_26289_amd/csrc/pool.hpp"
 
 using namespace dk;
 
-static long g_fails = -1;  // the allocation that fails, counted from 0 on; < 0: none does
+static thread_local long g_fails = -1;  // the allocation that fails, counted from 0 on; < 0: none does
 static bool take_allocation() { return g_fails < 0 || g_fails-- != 0; }
 void* operator new(std::size_t n) {
   void* p = take_allocation() ? std::malloc(n ? n : 1) : nullptr;
@@ -134,10 +138,113 @@ static void out_of_memory() {
   CHECK(failures > 10);
 }
 
+// Between a reorder and its end (kept or taken back) no other thread's call comes in: what is taken back is what was there.
+static void one_step() {
+  for (g_at = 0; g_at < 2; ++g_at) {
+    Pool pool(8, 0, 64 * 16, 16);
+    std::vector<int32_t> slots;
+    for (int i = 0; i < 4; ++i) slots.push_back(slot_of(pool, 40 + 3 * i));
+    const std::vector<int32_t> parents = {0, 0, 0, 0};
+    Pool::Reorder re;
+    CHECK(pool.reorder(4, slots.data(), parents.data(), &re) == OK);
+    std::atomic<bool> started{false};
+    int32_t released = -1, acquired = -1, fresh = -1;
+    std::thread other([&] {
+      started = true;
+      released = pool.release(slots[2]);
+      acquired = pool.acquire(0, 0, &fresh);
+    });
+    while (!started) std::this_thread::yield();
+    std::this_thread::sleep_for(std::chrono::milliseconds(100));  // (a call that could come in has, by now)
+    if (g_at == 0) pool.undo_reorder(4, slots.data(), &re);
+    else pool.settle_reorder(&re);
+    other.join();
+    CHECK(released == OK && acquired == OK);
+    for (int i = 0; i < 4; ++i) {
+      int64_t len = -1;
+      const int32_t rc = pool.length(slots[(size_t)i], &len);
+      if (i == 2 && fresh != slots[2]) CHECK(rc == ERR_NO_SLOT);
+      else CHECK(rc == OK && len == (i == 2 ? 0 : g_at == 0 ? 40 + 3 * i : 40));
+    }
+    int64_t len = -1;
+    CHECK(pool.length(fresh, &len) == OK && len == 0);
+    for (int i = 0; i < 4; ++i)
+      if (i != 2) CHECK(pool.release(slots[(size_t)i]) == OK);
+    CHECK(held(pool) == 0);
+  }
+}
+
+// Searches on threads of their own, some of their calls taken back, while others acquire, alias, trim and release.
+static void threads() {
+  constexpr int kThreads = 5, kSteps = 1500;
+  Pool pool(4 * kThreads + 1, 0, 1 << 14, 16);
+  const int32_t prompt = slot_of(pool, 100);
+  std::atomic<int> failures{0};
+  const auto search = [&](int id) {
+    std::mt19937 rng(500 + (unsigned)id);
+    Pool::Reorder re;
+    std::vector<int32_t> slots;
+    std::vector<int64_t> lens;
+    for (int step = 0; step < kSteps; ++step) {
+      if (slots.empty()) {
+        for (int i = 0; i < 4; ++i) {
+          int32_t s = -1;
+          if (pool.acquire(0, -1, &s) != OK || pool.alias(prompt, s, 0, 90 + i) != OK) ++failures;
+          slots.push_back(s);
+          lens.push_back(90 + i);
+        }
+      }
+      std::vector<int32_t> parents, cu = {0};
+      for (int i = 0; i < 4; ++i) {
+        parents.push_back((int32_t)(rng() % 4));
+        cu.push_back(i + 1);
+      }
+      const int32_t rc = pool.reorder(4, slots.data(), parents.data(), &re);
+      if (rc == OK && rng() % 3 == 0) {
+        pool.undo_reorder(4, slots.data(), &re);
+      } else if (rc == OK) {
+        pool.settle_reorder(&re);
+        std::vector<int64_t> after;
+        for (int i = 0; i < 4; ++i) after.push_back(lens[(size_t)parents[(size_t)i]]);
+        lens = after;
+      } else if (rc != ERR_NO_CELLS) {
+        ++failures;
+      }
+      if (pool.append(4, slots.data(), cu.data(), nullptr, nullptr) == OK)
+        for (int64_t& l : lens) ++l;
+      if (rng() % 8 == 0) {
+        const size_t i = rng() % 4;
+        lens[i] -= (int64_t)(rng() % 5);
+        if (pool.trim(slots[i], lens[i]) != OK) ++failures;
+      }
+      for (int i = 0; i < 4; ++i) {
+        int64_t len = -1;
+        if (pool.length(slots[(size_t)i], &len) != OK || len != lens[(size_t)i]) ++failures;
+      }
+      if (step % 60 == 59) {
+        for (int32_t s : slots)
+          if (pool.release(s) != OK) ++failures;
+        slots.clear();
+        lens.clear();
+      }
+    }
+    for (int32_t s : slots)
+      if (pool.release(s) != OK) ++failures;
+  };
+  std::vector<std::thread> all;
+  for (int i = 0; i < kThreads; ++i) all.emplace_back(search, i);
+  for (std::thread& t : all) t.join();
+  CHECK(failures == 0);
+  CHECK(pool.release(prompt) == OK);
+  CHECK(held(pool) == 0);
+}
+
 int main(int argc, char** argv) {
   const char* what = argc > 1 ? argv[1] : "";
   if (!std::strcmp(what, "granules")) granules();
   else if (!std::strcmp(what, "out_of_memory")) out_of_memory();
+  else if (!std::strcmp(what, "one_step")) one_step();
+  else if (!std::strcmp(what, "threads")) threads();
   else return 2;
   std::printf("ok\n");
   return 0;

@@ -34,3 +34,13 @@ def test_a_failed_allocation_loses_no_granule(tmp_path, sanitizer):
 @pytest.mark.parametrize("sanitizer", [None, "address,undefined"])
 def test_a_failed_allocation_leaves_every_slot_as_it_was(tmp_path, sanitizer):
     run_check(tmp_path, "out_of_memory", sanitizer)
+
+
+@pytest.mark.parametrize("sanitizer", [None, "address,undefined", "thread"])
+def test_no_other_call_comes_between_a_reorder_and_its_end(tmp_path, sanitizer):
+    run_check(tmp_path, "one_step", sanitizer)
+
+
+@pytest.mark.parametrize("sanitizer", ["thread", "address,undefined"])
+def test_searches_on_several_threads(tmp_path, sanitizer):
+    run_check(tmp_path, "threads", sanitizer)
