@@ -10,10 +10,24 @@ GranuleAllocator::GranuleAllocator(int64_t n) : tails_((size_t)std::max<int64_t>
   if (n > 0) runs_[0] = n;
 }
 
-void GranuleAllocator::remove_from_run(std::map<int64_t, int64_t>::iterator it, int64_t g) {
+// Before a granule is taken: an entry for every run that may come of giving it and those taken before it back, and one for what its run
+// may leave on either side.
+void GranuleAllocator::make_entries() {
+  const int64_t most = std::min((int64_t)runs_.size() + (total_ - free_) + 2, (total_ + 1) / 2);
+  while ((int64_t)(runs_.size() + spare_.size()) < most) spare_.emplace_hint(spare_.end(), next_spare_++, 0);
+}
+
+void GranuleAllocator::drop_entry(Runs::iterator it) noexcept {
+  auto entry = runs_.extract(it);
+  entry.key() = next_spare_++;
+  spare_.insert(spare_.end(), std::move(entry));
+}
+
+void GranuleAllocator::remove_from_run(Runs::iterator it, int64_t g) {
+  make_entries();  // (may throw: before anything changes)
   const int64_t s = it->first, l = it->second;
   if (l == 1) {
-    runs_.erase(it);
+    drop_entry(it);
   } else if (g == s) {  // the run's own entry, one granule shorter
     const auto hint = std::next(it);
     auto run = runs_.extract(it);
@@ -21,8 +35,13 @@ void GranuleAllocator::remove_from_run(std::map<int64_t, int64_t>::iterator it, 
     run.mapped() = l - 1;
     runs_.insert(hint, std::move(run));
   } else {
-    if (g + 1 < s + l) runs_.emplace_hint(std::next(it), g + 1, s + l - (g + 1));  // (may throw: before anything changes)
     it->second = g - s;
+    if (g + 1 < s + l) {
+      auto run = spare_.extract(std::prev(spare_.end()));
+      run.key() = g + 1;
+      run.mapped() = s + l - (g + 1);
+      runs_.insert(std::next(it), std::move(run));
+    }
   }
   --free_;
 }
@@ -53,16 +72,11 @@ int64_t GranuleAllocator::take_fresh() {
 int64_t GranuleAllocator::take_first() {
   if (runs_.empty()) return -1;
   const int64_t g = runs_.begin()->first;
-  auto run = runs_.extract(runs_.begin());  // (the run's own entry, one granule shorter)
-  if (--run.mapped() > 0) {
-    ++run.key();
-    runs_.insert(runs_.begin(), std::move(run));
-  }
-  --free_;
+  remove_from_run(runs_.begin(), g);
   return g;
 }
 
-void GranuleAllocator::give_back(int64_t g) {
+void GranuleAllocator::give_back(int64_t g) noexcept {
   const auto next = runs_.lower_bound(g);
   const bool joins_next = next != runs_.end() && next->first == g + 1;
   ++free_;
@@ -70,7 +84,7 @@ void GranuleAllocator::give_back(int64_t g) {
     const auto before = std::prev(next);
     if (before->first + before->second == g) {
       before->second += 1 + (joins_next ? next->second : 0);
-      if (joins_next) runs_.erase(next);
+      if (joins_next) drop_entry(next);
       return;
     }
   }
@@ -81,7 +95,10 @@ void GranuleAllocator::give_back(int64_t g) {
     ++run.mapped();
     runs_.insert(hint, std::move(run));
   } else {
-    runs_.emplace_hint(next, g, 1);
+    auto run = spare_.extract(std::prev(spare_.end()));
+    run.key() = g;
+    run.mapped() = 1;
+    runs_.insert(next, std::move(run));
   }
 }
 

@@ -39,13 +39,18 @@ class GranuleAllocator {
   // Takes the free granule with the lowest number; -1 if none is free.  For states of less than a granule, which fill gaps: looking
   // through the runs for the longest costs a microsecond and more where there are many.
   int64_t take_first();
-  void give_back(int64_t g);
+  void give_back(int64_t g) noexcept;  // allocates nothing
   void mark_tail(int64_t g) { tails_[(size_t)g] = 1; }
   void unmark_tail(int64_t g) { tails_[(size_t)g] = 0; }
 
  private:
-  void remove_from_run(std::map<int64_t, int64_t>::iterator it, int64_t g);
-  std::map<int64_t, int64_t> runs_;  // start -> length, maximal and disjoint
+  typedef std::map<int64_t, int64_t> Runs;
+  void remove_from_run(Runs::iterator it, int64_t g);
+  void make_entries();
+  void drop_entry(Runs::iterator it) noexcept;
+  Runs runs_;   // start -> length, maximal and disjoint
+  Runs spare_;  // entries for runs to come, under numbers of their own: as many as giving back all that is taken can need
+  int64_t next_spare_ = 0;
   std::vector<char> tails_;          // 1: last granule of a live node (a place where a sequence may grow)
   int64_t free_;
   int64_t total_;

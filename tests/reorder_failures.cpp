@@ -14,7 +14,8 @@
 using namespace dk;
 
 static thread_local long g_fails = -1;  // the allocation that fails, counted from 0 on; < 0: none does
-static bool take_allocation() { return g_fails < 0 || g_fails-- != 0; }
+static thread_local bool g_all_fail = false;
+static bool take_allocation() { return !g_all_fail && (g_fails < 0 || g_fails-- != 0); }
 void* operator new(std::size_t n) {
   void* p = take_allocation() ? std::malloc(n ? n : 1) : nullptr;
   if (!p) throw std::bad_alloc();
@@ -92,6 +93,45 @@ static void granules() {
     CHECK(found == (taken ? 15 : 16));
   }
   CHECK(failures > 4);
+}
+
+// Giving cells back needs no memory: it is done where sequences end, in destructors too.
+static void giving_back() {
+  for (g_at = 0; g_at < 40; ++g_at) {
+    std::mt19937 rng((unsigned)g_at);
+    const int n = 1 + (int)(rng() % 70);
+    GranuleAllocator alloc(n);
+    std::vector<int64_t> taken;
+    taken.reserve((size_t)n);
+    std::vector<char> free_now((size_t)n, 1);
+    for (int turn = 0; turn < 300; ++turn) {
+      const int what = (int)(rng() % 4);
+      const int64_t some = (int64_t)(rng() % (unsigned)n);
+      const int64_t g = what == 0 ? alloc.take_first() : what == 1 ? alloc.take_fresh() : alloc.take(some) ? some : -1;
+      if (what < 2) CHECK((g >= 0) == ((int64_t)taken.size() < n));
+      if (g >= 0) {
+        CHECK(free_now[(size_t)g]);
+        free_now[(size_t)g] = 0;
+        taken.push_back(g);
+      }
+      g_all_fail = true;
+      if (turn % 60 > 40) {
+        const size_t back = (size_t)(rng() % (unsigned)(taken.size() + 1));
+        for (size_t i = 0; i < back; ++i) {
+          const size_t k = (size_t)(rng() % (unsigned)taken.size());
+          alloc.give_back(taken[k]);
+          free_now[(size_t)taken[k]] = 1;
+          taken[k] = taken.back();
+          taken.pop_back();
+        }
+      }
+      g_all_fail = false;
+      CHECK(alloc.free_count() == n - (int64_t)taken.size());
+    }
+    for (int64_t g = 0; g < n; ++g)
+      if (free_now[(size_t)g]) CHECK(alloc.take_first() == g);
+    CHECK(alloc.take_first() == -1 && alloc.free_count() == 0);
+  }
 }
 
 // Whichever allocation of the call fails: every slot is what it was, and nothing refers to its cells but itself.
@@ -242,6 +282,7 @@ static void threads() {
 int main(int argc, char** argv) {
   const char* what = argc > 1 ? argv[1] : "";
   if (!std::strcmp(what, "granules")) granules();
+  else if (!std::strcmp(what, "giving_back")) giving_back();
   else if (!std::strcmp(what, "out_of_memory")) out_of_memory();
   else if (!std::strcmp(what, "one_step")) one_step();
   else if (!std::strcmp(what, "threads")) threads();

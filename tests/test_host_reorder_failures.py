@@ -32,6 +32,11 @@ def test_a_failed_allocation_loses_no_granule(tmp_path, sanitizer):
 
 
 @pytest.mark.parametrize("sanitizer", [None, "address,undefined"])
+def test_giving_cells_back_needs_no_memory(tmp_path, sanitizer):
+    run_check(tmp_path, "giving_back", sanitizer)
+
+
+@pytest.mark.parametrize("sanitizer", [None, "address,undefined"])
 def test_a_failed_allocation_leaves_every_slot_as_it_was(tmp_path, sanitizer):
     run_check(tmp_path, "out_of_memory", sanitizer)
 
