@@ -152,7 +152,7 @@ int32_t dk_seq_trim_batch(dk_pool* pool, int32_t n_seqs, const int32_t* slots, c
  * granule of its own for the rest, into which those tokens' K and V are copied on `stream`.  So a search's sequences stay in few
  * runs of cells however long it goes on, what is copied does not depend on their length, and dk_shared_attend finds what they share.  Afterwards all of them grow independently.
  * DK_ERR_INVALID (a parent out of range), DK_ERR_NO_SLOT, DK_ERR_DUP_SLOT, and DK_ERR_NO_CELLS unless the arena has a free granule for
- * every copy -- cells of states that no slot has any more are free after the call, not during it -- leave every slot as it was.
+ * every copy -- cells that no slot sees any more are free (to whole granules) after the call, not during it -- leave every slot as it was.
  * Cells are chosen at call time: a captured call replays its copies, not the bookkeeping.
  */
 int32_t dk_seq_reorder(dk_pool* pool, int32_t n, const int32_t* slots, const int32_t* parents, void* stream);

@@ -107,6 +107,35 @@ Node::~Node() {
   if (borrow_cap > 0 && parent) parent->tail_lent = false;  // nothing refers to the borrowed cells any more
   if (!granules.empty()) alloc->unmark_tail(granules.back());
   for (int64_t g : granules) alloc->give_back(g);
+  if (parent) parent->drop_child(base);
+}
+
+void Node::add_child(int64_t at) {
+  if (last.count == 0 || last.base == at) {
+    last = {at, last.count + 1};
+  } else if (last.base < at) {
+    others.push_back(last);
+    last = {at, 1};
+  } else {
+    const auto it = std::lower_bound(others.begin(), others.end(), at, [](const Children& c, int64_t x) { return c.base < x; });
+    if (it != others.end() && it->base == at) ++it->count;
+    else others.insert(it, {at, 1});
+  }
+}
+
+void Node::drop_child(int64_t at) noexcept {
+  if (at != last.base) {
+    const auto it = std::lower_bound(others.begin(), others.end(), at, [](const Children& c, int64_t x) { return c.base < x; });
+    if (--it->count == 0) others.erase(it);
+  } else if (--last.count == 0 && !others.empty()) {
+    last = others.back();
+    others.pop_back();
+    cut_back();
+  }
+}
+
+void Node::cut_back() noexcept {
+  if (owners == 0 && last.count > 0 && last.base < end()) shrink_to(last.base - base);
 }
 
 int64_t Node::granules_needed(int64_t extra) const {
@@ -134,7 +163,7 @@ void Node::grow(int64_t extra, bool anywhere) {
   len += extra;
 }
 
-void Node::shrink_to(int64_t new_len) {
+void Node::shrink_to(int64_t new_len) noexcept {
   const int64_t keep = (std::max<int64_t>(0, new_len - borrow_cap) + gr - 1) / gr;
   if ((int64_t)granules.size() > keep) {
     alloc->unmark_tail(granules.back());
@@ -154,10 +183,14 @@ Pool::Pool(int32_t n_slots, int32_t n_session, int64_t arena_cells, int32_t gran
   for (int32_t s = n_transient_; s < n_slots; ++s) free_[1].push_back(s);
 }
 
-void Pool::set_head(Slot& s, std::shared_ptr<Node> n) {
-  if (s.head) --s.head->owners;
-  s.head = std::move(n);
+void Pool::swap_head(Slot& s, std::shared_ptr<Node>& n) noexcept {
+  s.head.swap(n);
   if (s.head) ++s.head->owners;
+  if (n) --n->owners;
+}
+void Pool::set_head(Slot& s, std::shared_ptr<Node> n) noexcept {
+  swap_head(s, n);
+  if (n) n->cut_back();
 }
 
 int32_t Pool::acquire(int32_t region, int64_t timeout_ms, int32_t* slot_out) {
@@ -511,7 +544,7 @@ int32_t Pool::reorder(int32_t n, const int32_t* slots, const int32_t* parents, R
     Slot& s = slots_[slots[i]];
     std::shared_ptr<Node>& h = heads[(size_t)i];
     if (h && r->keeper[(size_t)parents[i]] != i && h->parent) h->parent->frozen = std::max(h->parent->frozen, h->base);
-    set_head(s, std::move(h));
+    swap_head(s, h);
     s.len = r->before[(size_t)parents[i]].len;
   }
   r->lock = std::move(lk);
@@ -520,16 +553,18 @@ int32_t Pool::reorder(int32_t n, const int32_t* slots, const int32_t* parents, R
 
 void Pool::undo_reorder(int32_t n, const int32_t* slots, Reorder* r) {
   const std::unique_lock<std::mutex> lk = std::move(r->lock);
-  for (int32_t i = 0; i < n && i < (int32_t)r->before.size(); ++i) {
+  for (int32_t i = 0; i < n; ++i) {
     Slot& s = slots_[slots[i]];
-    set_head(s, r->before[(size_t)i].head);
+    swap_head(s, r->before[(size_t)i].head);
     s.len = r->before[(size_t)i].len;
   }
-  r->before.clear();
+  r->before.clear();  // (what the slots would have become; every node has its owner again)
 }
 
 void Pool::settle_reorder(Reorder* r) {
   const std::unique_lock<std::mutex> lk = std::move(r->lock);
+  for (const Slot& s : r->before)
+    if (s.head) s.head->cut_back();
   r->before.clear();
 }
 

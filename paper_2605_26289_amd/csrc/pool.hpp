@@ -60,9 +60,12 @@ class GranuleAllocator {
 // range is [base, base + len); everything below `base` is read through `parent`,
 // truncated at `base`.  A sequence that aliases another one gets a fresh, empty node
 // whose parent is the donor's node: nothing is copied and nothing per cell is touched.
+// Once no sequence can append to a node any more it holds only what its children see, to whole granules.
 struct Node {
   Node(GranuleAllocator* a, int64_t granule_cells, std::shared_ptr<Node> p, int64_t b)
-      : alloc(a), gr(granule_cells), parent(std::move(p)), base(b) {}
+      : alloc(a), gr(granule_cells), parent(std::move(p)), base(b) {
+    if (parent) parent->add_child(base);
+  }
   ~Node();
   Node(const Node&) = delete;
   Node& operator=(const Node&) = delete;
@@ -70,7 +73,10 @@ struct Node {
   int64_t end() const { return base + len; }
   int64_t granules_needed(int64_t extra) const;  // granules an append of `extra` tokens must add
   void grow(int64_t extra, bool anywhere = false);  // caller has checked the allocator holds enough; anywhere: a first granule fills a gap
-  void shrink_to(int64_t new_len);               // own length, frees whole unused granules
+  void shrink_to(int64_t new_len) noexcept;      // own length, frees whole unused granules
+  void add_child(int64_t at);
+  void drop_child(int64_t at) noexcept;
+  void cut_back() noexcept;  // no owner: what lies behind the last child's base is nobody's
   int64_t cell_of(int64_t own_offset) const {
     if (own_offset < borrow_cap) return borrow_cell + own_offset;
     const int64_t o = own_offset - borrow_cap;
@@ -92,6 +98,12 @@ struct Node {
   int64_t borrow_cap = 0;
   bool tail_lent = false;  // the unused rest of this node's last granule is some child's borrow room
   int32_t owners = 0;      // sequences whose newest node this is: they may still append to it
+  struct Children {
+    int64_t base;
+    int32_t count;
+  };
+  Children last{0, 0};            // the children that begin furthest back (most nodes' all)
+  std::vector<Children> others;   // those in front of them, ascending
 };
 
 struct Slot {
@@ -171,7 +183,8 @@ class Pool {
  private:
   bool valid(int32_t slot) const { return slot >= 0 && slot < (int32_t)slots_.size() && slots_[slot].in_use; }
   int32_t trim_locked(int32_t slot, int64_t new_len);
-  void set_head(Slot& s, std::shared_ptr<Node> n);
+  static void swap_head(Slot& s, std::shared_ptr<Node>& n) noexcept;  // leaves the one that was there whole
+  static void set_head(Slot& s, std::shared_ptr<Node> n) noexcept;
   static void resolve(const std::shared_ptr<Node>& head, int64_t len, std::vector<Extent>* out);
 
   std::mutex mu_;

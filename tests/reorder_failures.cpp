@@ -279,12 +279,113 @@ static void threads() {
   CHECK(held(pool) == 0);
 }
 
+// Cells that no slot sees any more are free after the call, but for what is left of a granule.
+static int32_t alias_of(Pool& pool, int32_t donor, int64_t n) {
+  int32_t s = -1;
+  CHECK(pool.acquire(0, 0, &s) == OK && pool.alias(donor, s, 0, n) == OK);
+  return s;
+}
+static int32_t append_to(Pool& pool, int32_t s, int32_t n) {
+  const int32_t cu[2] = {0, n};
+  return pool.append(1, &s, cu, nullptr, nullptr);
+}
+static int32_t reorder(Pool& pool, const std::vector<int32_t>& slots, const std::vector<int32_t>& parents) {
+  Pool::Reorder re;
+  const int32_t rc = pool.reorder((int32_t)slots.size(), slots.data(), parents.data(), &re);
+  if (rc == OK) pool.settle_reorder(&re);
+  return rc;
+}
+static void cells_come_back() {
+  {  // a long state goes, its beginning is another's prefix
+    Pool pool(4, 0, 2048, 256);
+    const int32_t a = slot_of(pool, 64), b = alias_of(pool, a, 64);
+    CHECK(append_to(pool, a, 1500) == OK && held(pool) == 7 * 256);
+    CHECK(reorder(pool, {a, b}, {1, 1}) == OK && held(pool) == 256);
+    CHECK(append_to(pool, b, 600) == OK);
+    int64_t len = 0;
+    CHECK(pool.length(a, &len) == OK && len == 64);
+  }
+  {  // cells of a sequence that is gone, seen by a state that goes now, through a node of its own without a token
+    Pool pool(8, 0, 4096, 256);
+    const int32_t p = slot_of(pool, 1500), a = alias_of(pool, p, 1400), b = alias_of(pool, p, 64);
+    CHECK(pool.release(p) == OK && held(pool) >= 6 * 256);
+    CHECK(reorder(pool, {a, b}, {1, 1}) == OK && held(pool) == 256);
+  }
+  {  // the child that saw most goes later, in another call; one that sees as much stays
+    Pool pool(8, 0, 8192, 256);
+    const int32_t a = slot_of(pool, 64);
+    CHECK(append_to(pool, a, 1936) == OK);  // eight granules
+    const int32_t b = alias_of(pool, a, 1900), c = alias_of(pool, a, 1900), d = alias_of(pool, a, 300), e = slot_of(pool, 3);
+    CHECK(reorder(pool, {a, e}, {1, 1}) == OK && held(pool) == 8 * 256 + 2 * 256);
+    CHECK(reorder(pool, {b, e}, {1, 1}) == OK && held(pool) == 8 * 256 + 3 * 256);
+    CHECK(reorder(pool, {c, d}, {1, 1}) == OK && held(pool) == 2 * 256 + 3 * 256);
+    CHECK(append_to(pool, c, 5) == OK && append_to(pool, d, 5) == OK);
+    int64_t len = 0;
+    CHECK(pool.length(c, &len) == OK && len == 305);
+    std::vector<int64_t> x(305), y(305);
+    CHECK(pool.cells(c, x.data(), 305) == OK && pool.cells(d, y.data(), 305) == OK);
+    for (int i = 0; i < 305; ++i) CHECK((x[(size_t)i] == y[(size_t)i]) == (i < 300));
+  }
+  {  // a state that goes in the same call in which another slot takes it over stays whole, and so does one that is taken back
+    Pool pool(8, 0, 8192, 256);
+    const int32_t a = slot_of(pool, 1000), b = alias_of(pool, a, 100), c = slot_of(pool, 7);
+    CHECK(reorder(pool, {a, b, c}, {2, 1, 0}) == OK);
+    int64_t len = 0;
+    CHECK(pool.length(c, &len) == OK && len == 1000 && held(pool) == 4 * 256 + 256);
+    std::vector<int32_t> slots = {a, b, c}, parents = {1, 1, 1};
+    Pool::Reorder re;
+    CHECK(pool.reorder(3, slots.data(), parents.data(), &re) == OK);
+    pool.undo_reorder(3, slots.data(), &re);
+    CHECK(pool.length(c, &len) == OK && len == 1000 && held(pool) == 5 * 256);
+    std::vector<int64_t> x(1000);
+    CHECK(pool.cells(c, x.data(), 1000) == OK);
+    std::vector<char> seen(8192, 0);
+    for (int64_t cell : x) CHECK(cell >= 0 && !seen[(size_t)cell]++);
+    CHECK(append_to(pool, c, 24) == OK && held(pool) == 5 * 256);
+  }
+  // a search that goes on: what is held stays within some granules of what the slots see
+  for (int beams : {2, 5, 16}) {
+    g_at = beams;
+    Pool pool(40, 0, 256 * 4096, 256);
+    std::mt19937 rng((unsigned)beams);
+    const int32_t prompt = slot_of(pool, 1000);
+    std::vector<int32_t> slots, cu = {0};
+    for (int i = 0; i < beams; ++i) {
+      slots.push_back(alias_of(pool, prompt, 1000));
+      cu.push_back(i + 1);
+    }
+    CHECK(pool.release(prompt) == OK);
+    for (int step = 0; step < 3000; ++step) {
+      std::vector<int32_t> parents;
+      for (int i = 0; i < beams; ++i) parents.push_back((int32_t)(rng() % (unsigned)beams));
+      CHECK(reorder(pool, slots, parents) == OK && pool.append(beams, slots.data(), cu.data(), nullptr, nullptr) == OK);
+      if (step % 100 != 99) continue;
+      std::vector<char> granule(4096, 0);
+      int64_t granules = 0;
+      for (int32_t s : slots) {
+        int64_t len = 0;
+        CHECK(pool.length(s, &len) == OK && len == 1001 + step);
+        std::vector<int64_t> x((size_t)len);
+        CHECK(pool.cells(s, x.data(), len) == OK);
+        for (int64_t cell : x) {
+          granules += granule[(size_t)(cell / 256)] == 0;
+          granule[(size_t)(cell / 256)] = 1;
+        }
+      }
+      CHECK(held(pool) == 256 * granules);  // no granule without a cell that some slot sees
+    }
+    for (int32_t s : slots) CHECK(pool.release(s) == OK);
+    CHECK(held(pool) == 0);
+  }
+}
+
 int main(int argc, char** argv) {
   const char* what = argc > 1 ? argv[1] : "";
   if (!std::strcmp(what, "granules")) granules();
   else if (!std::strcmp(what, "giving_back")) giving_back();
   else if (!std::strcmp(what, "out_of_memory")) out_of_memory();
   else if (!std::strcmp(what, "one_step")) one_step();
+  else if (!std::strcmp(what, "cells_come_back")) cells_come_back();
   else if (!std::strcmp(what, "threads")) threads();
   else return 2;
   std::printf("ok\n");

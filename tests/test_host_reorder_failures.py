@@ -49,3 +49,8 @@ def test_no_other_call_comes_between_a_reorder_and_its_end(tmp_path, sanitizer):
 @pytest.mark.parametrize("sanitizer", ["thread", "address,undefined"])
 def test_searches_on_several_threads(tmp_path, sanitizer):
     run_check(tmp_path, "threads", sanitizer)
+
+
+@pytest.mark.parametrize("sanitizer", [None, "address,undefined"])
+def test_cells_that_no_slot_sees_come_back(tmp_path, sanitizer):
+    run_check(tmp_path, "cells_come_back", sanitizer)
