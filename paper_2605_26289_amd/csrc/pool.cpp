@@ -13,14 +13,20 @@ GranuleAllocator::GranuleAllocator(int64_t n) : tails_((size_t)std::max<int64_t>
 // Before a granule is taken: an entry for every run that may come of giving it and those taken before it back, and one for what its run
 // may leave on either side.
 void GranuleAllocator::make_entries() {
-  const int64_t most = std::min((int64_t)runs_.size() + (total_ - free_) + 2, (total_ + 1) / 2);
-  while ((int64_t)(runs_.size() + spare_.size()) < most) spare_.emplace_hint(spare_.end(), next_spare_++, 0);
+  const size_t most = (size_t)std::min((int64_t)runs_.size() + (total_ - free_) + 2, (total_ + 1) / 2);
+  // (room for those in use too: giving back puts them here)
+  if (most > spare_.capacity()) spare_.reserve(std::max(most, 2 * spare_.capacity()));
+  for (Runs made; runs_.size() + spare_.size() < most;) spare_.push_back(made.extract(made.emplace(0, 0).first));
 }
 
-void GranuleAllocator::drop_entry(Runs::iterator it) noexcept {
-  auto entry = runs_.extract(it);
-  entry.key() = next_spare_++;
-  spare_.insert(spare_.end(), std::move(entry));
+void GranuleAllocator::drop_entry(Runs::iterator it) noexcept { spare_.push_back(runs_.extract(it)); }
+
+void GranuleAllocator::add_run(Runs::iterator hint, int64_t start, int64_t length) noexcept {
+  Runs::node_type run = std::move(spare_.back());
+  spare_.pop_back();
+  run.key() = start;
+  run.mapped() = length;
+  runs_.insert(hint, std::move(run));
 }
 
 void GranuleAllocator::remove_from_run(Runs::iterator it, int64_t g) {
@@ -36,12 +42,7 @@ void GranuleAllocator::remove_from_run(Runs::iterator it, int64_t g) {
     runs_.insert(hint, std::move(run));
   } else {
     it->second = g - s;
-    if (g + 1 < s + l) {
-      auto run = spare_.extract(std::prev(spare_.end()));
-      run.key() = g + 1;
-      run.mapped() = s + l - (g + 1);
-      runs_.insert(std::next(it), std::move(run));
-    }
+    if (g + 1 < s + l) add_run(std::next(it), g + 1, s + l - (g + 1));
   }
   --free_;
 }
@@ -95,10 +96,7 @@ void GranuleAllocator::give_back(int64_t g) noexcept {
     ++run.mapped();
     runs_.insert(hint, std::move(run));
   } else {
-    auto run = spare_.extract(std::prev(spare_.end()));
-    run.key() = g;
-    run.mapped() = 1;
-    runs_.insert(next, std::move(run));
+    add_run(next, g, 1);
   }
 }
 

@@ -48,9 +48,9 @@ class GranuleAllocator {
   void remove_from_run(Runs::iterator it, int64_t g);
   void make_entries();
   void drop_entry(Runs::iterator it) noexcept;
-  Runs runs_;   // start -> length, maximal and disjoint
-  Runs spare_;  // entries for runs to come, under numbers of their own: as many as giving back all that is taken can need
-  int64_t next_spare_ = 0;
+  void add_run(Runs::iterator hint, int64_t start, int64_t length) noexcept;
+  Runs runs_;                           // start -> length, maximal and disjoint
+  std::vector<Runs::node_type> spare_;  // entries for runs to come: as many as giving back all that is taken can need
   std::vector<char> tails_;          // 1: last granule of a live node (a place where a sequence may grow)
   int64_t free_;
   int64_t total_;
