@@ -9,7 +9,7 @@
 //                        one of the chunk's n best, each with the largest of its logits: those that reach T, which n lanes of a
 //                        wavefront reach, or n / 4 of every one (found bit by bit with ballots, as in token_logprobs_chunk_kernel).
 //   beam_select_kernel   one workgroup per group: folds the sums of its rows, finds T -- the n-th largest score of the wavefronts' (or
-//                        chunks', or lanes') largest logits, by its upper bits: as many continuations are T or more, so the n best are --
+//                        chunks', or lanes') largest logits, by how far it is from the best one of all: as many continuations are T or more, so the n best are --
 //                        and reads the logits of the lanes that reach it once more, some n of them.  What reaches T there goes to LDS, and
 //                        each one's place is the number of those before it.  Where more do than there is room for (equal logits by the
 //                        thousand), T is raised to the n-th of those that came and the lists are gone through again.
@@ -223,11 +223,12 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
   __shared__ uint32_t heads[BEAM_MAX_LISTS];
   __shared__ Found found[BEAM_CAP];
   __shared__ uint32_t lanes[BEAM_LANES];  // list * 256 + thread
-  __shared__ uint32_t lane_key[BEAM_LANES];  // upper bits of the score of the largest logit there
+  __shared__ uint32_t lane_key[BEAM_LANES];  // the largest logit's there, see key_of
   __shared__ double base[BEAM_MAX_ROWS];  // of a row that takes part: its score less the log of its sum
   __shared__ float most[BEAM_MAX_ROWS];   // its largest logit; NaN: it takes no part
   __shared__ int32_t lists_on[BEAM_LISTS];
   __shared__ int32_t came, reached, active;
+  __shared__ uint32_t top_bits;  // upper bits of the best row's best score
   __shared__ Found bound;
   const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int n = a.n_out;
@@ -250,7 +251,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
     for (int i = tid; i < n_lists * kind; i += BEAM_THREADS) heads[i] = __float_as_uint(kind == 1 ? gp[i].m : gp[i / LP_WAVES].top[i % LP_WAVES]);
   }
   if (tid < rows) most[tid] = own_score;
-  if (tid == 0) came = reached = 0;
+  if (tid == 0) came = reached = 0, top_bits = 0;
   __syncthreads();
 
   // the rows' sums, `per` lanes to a row
@@ -275,6 +276,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
       const bool live = __builtin_fabsf(score) < INFINITY && __builtin_fabsf(m) < INFINITY && z > 0.0 && z < (double)INFINITY;
       base[r] = live ? (double)score - log(z) : 0.0;
       most[r] = live ? m : __uint_as_float(0x7fc00000u);
+      if (live) atomicMax(&top_bits, (uint32_t)(ordered64(base[r]) >> 32));
     }
   }
   __syncthreads();
@@ -288,16 +290,26 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
     return e == 0 ? 0 : score_of(list / n_chunks, from_ordered((uint32_t)(e >> 32)));
   };
 
+  // Bounds are found among keys: how far a score is below `top`, which none is above, as a float in order.  (A score by itself grows with
+  // the length of what has been said: of its 17 upper bits the last is 8 near -300 and 128 near -5000: bounds made of those
+  // let so much through that a call took 1382 us there instead of 22.)  0: none, also of a bound that everything reaches.
+  const double top = from_ordered64((uint64_t)top_bits << 32 | 0xffffffffu);
+  const auto key_of = [&](uint64_t score) -> uint32_t { return score == 0 ? 0u : ordered(fminf((float)(from_ordered64(score) - top), -0x1p-126f)); };
+  // a score that none with such a key or a larger one is below (the difference was rounded to fp64 and to fp32)
+  const auto score_at = [&](uint32_t key) -> uint64_t {
+    if (key <= 0x007fffffu) return 1;  // (-infinity is the first)
+    return ordered64(top + (double)from_ordered(key) * (1.0 + 0x1p-20) - __builtin_fabs(top) * 0x1p-50);
+  };
   int n_heads = n_lists * kind;
   if (kind != 0) {
-    for (int i = tid; i < n_heads; i += BEAM_THREADS) heads[i] = (uint32_t)(score_of(i / (kind * n_chunks), __uint_as_float(heads[i])) >> 32);
+    for (int i = tid; i < n_heads; i += BEAM_THREADS) heads[i] = key_of(score_of(i / (kind * n_chunks), __uint_as_float(heads[i])));
   } else {  // (fewer than BEAM_MAX_OUT / LP_WAVES lists)
     n_heads = n_lists * BEAM_STEP;
-    for (int i = tid; i < n_heads; i += BEAM_THREADS) heads[i] = (uint32_t)(entry_score(i / BEAM_STEP, gl[i / BEAM_STEP * BEAM_LIST + i % BEAM_STEP]) >> 32);
+    for (int i = tid; i < n_heads; i += BEAM_THREADS) heads[i] = key_of(entry_score(i / BEAM_STEP, gl[i / BEAM_STEP * BEAM_LIST + i % BEAM_STEP]));
   }
   __syncthreads();
-  // The n-th largest of some numbers in LDS but for the last bits (2^-8 of a score and less), 0 if there are fewer; every wavefront
-  // finds it by itself.
+  // The n-th largest of some keys in LDS but for the last bits (2^-8 of the distance from `top`), 0 if there are fewer; every wavefront finds
+  // it by itself.
   const auto nth_largest = [&](const uint32_t* of, int count_of) __attribute__((always_inline)) {
     constexpr int KEEP = 16;  // of a lane (where they were read again for every bit, 672 took 7 to 11 us)
     uint32_t mine[KEEP], t = 0;
@@ -309,7 +321,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
 #pragma unroll
       for (int i = i0; i < i0 + 4; ++i) mine[i] = lane + 64 * i < count_of ? of[lane + 64 * i] : 0u;
     }
-    for (int bit = 31; bit >= 15; --bit) {
+    for (int bit = 30; bit >= 15; --bit) {  // (the keys of negative floats)
       const uint32_t u = t | 1u << bit;
       int count = __builtin_popcountll(__builtin_amdgcn_ballot_w64(mine[0] >= u));
       if (count_of > 64) {
@@ -327,9 +339,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
     }
     return t;
   };
-  const uint32_t t = nth_largest(heads, n_heads);
-  Found least = {(uint64_t)t << 32, 0};
-  if (least.score == 0) least.score = 1;  // (0 is none)
+  Found least = {score_at(nth_largest(heads, n_heads)), 0};
 
   // places in LDS for those lanes of a wavefront that say so
   const auto places = [&](bool take, int32_t* counter) __attribute__((always_inline)) {
@@ -376,7 +386,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
         else
           for (int w = 0; w < kind; ++w) head = max(head, heads[list * kind + w]);
       }
-      const bool take = list < n_lists && head >= (uint32_t)(least.score >> 32);
+      const bool take = list < n_lists && head >= (least.score <= 1 ? 1u : key_of(least.score));
       const int at = places(take, &active);
       if (take) lists_on[at] = list;
       __syncthreads();
@@ -400,7 +410,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
             const int to = places(reaches, &reached);
             if (reaches && to < BEAM_LANES) {
               lanes[to] = (uint32_t)(from[j] * BEAM_LIST) | (uint32_t)(q[j] & 0xffu);
-              lane_key[to] = (uint32_t)(key >> 32);
+              lane_key[to] = key_of(key);
             }
             // a list goes on where this step of it was full
             const bool more = __shfl((unsigned long long)q[j], lane | (BEAM_STEP - 1)) != 0 && e + BEAM_STEP < BEAM_LIST;
@@ -426,7 +436,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
           keep[i] = k < n_reached && lane_key[k] >= higher;
           which[i] = keep[i] ? lanes[k] : 0;
         }
-        if ((uint64_t)higher << 32 > least.score) least = {(uint64_t)higher << 32, 0};
+        if (score_at(higher) > least.score) least = {score_at(higher), 0};
         if (tid == 0) came = reached = 0;
         __syncthreads();
 #pragma unroll
@@ -451,9 +461,9 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
       }
     } else {
       // more lanes than there is room for: T from those that came, and the lists again; if that is no higher, list by list
-      const uint32_t higher = nth_largest(lane_key, BEAM_LANES);
-      if ((uint64_t)higher << 32 > least.score) {
-        least = {(uint64_t)higher << 32, 0};
+      const uint64_t higher = score_at(nth_largest(lane_key, BEAM_LANES));
+      if (higher > least.score) {
+        least = {higher, 0};
         __syncthreads();
         if (tid == 0) reached = 0;
         __syncthreads();

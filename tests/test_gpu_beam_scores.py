@@ -1,0 +1,116 @@
+"""dk_beam_select where the beams' cumulative scores are far from zero, as those of long continuations are: results, and that a call takes
+no longer for it.  Rows and tokens are compared always: the inputs' best continuations are checked to be apart."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_beam import SUM_TOL
+from paper_2605_26289_amd import binding as dk
+from paper_2605_26289_amd import workloads as wl
+
+pytestmark = pytest.mark.gpu
+
+ROWS, VOCAB = 8, 128256
+
+
+def logits_of(seed, dtype, rows=ROWS, vocab=VOCAB, spread=2.5):
+    x = (np.random.default_rng(seed).standard_normal((rows, vocab), dtype=np.float32) * np.float32(spread))
+    return torch.from_numpy(x).to(torch.bfloat16).float().numpy() if dtype == "bf16" else x
+
+
+def best(x, scores, cu, n, scale=1.0):
+    """The n best of every group, from all scores in 64 bits: by score, row, logit, token."""
+    groups = len(cu) - 1
+    rows, tokens, out = np.zeros((groups, n), np.int64), np.zeros((groups, n), np.int64), np.zeros((groups, n))
+    for g in range(groups):
+        y = scale * x[cu[g]:cu[g + 1]].astype(np.float64)
+        top = y.max(1, keepdims=True)
+        s = scores[cu[g]:cu[g + 1], None].astype(np.float64) + (y - top) - np.log(np.exp(y - top).sum(1, keepdims=True))
+        some = np.argpartition(-s, 4 * n, axis=None)[:4 * n] if s.size > 4 * n else np.arange(s.size)
+        r, t = np.unravel_index(some, s.shape)
+        order = np.lexsort((t, -y[r, t], r, -s[r, t]))[:n]
+        rows[g], tokens[g], out[g] = r[order] + cu[g], t[order], s[r, t][order]
+    return rows, tokens, out
+
+
+class Call:
+    def __init__(self, x, cu, n, dtype, scale=1.0):
+        rows, vocab = x.shape
+        assert vocab % 8 == 0
+        kind = torch.bfloat16 if dtype == "bf16" else torch.float32
+        code = dk.BF16 if dtype == "bf16" else dk.F32
+        self.logits = torch.from_numpy(x).to("cuda", kind)
+        self.scores = torch.empty(rows, dtype=torch.float32, device="cuda")
+        self.out = [torch.empty((len(cu) - 1, n), dtype=t, device="cuda") for t in (torch.int32, torch.int32, torch.float32)]
+        ws = torch.empty(dk.beam_workspace_bytes(rows, vocab, code, n), dtype=torch.uint8, device="cuda")
+        cu_dev = torch.tensor(cu, dtype=torch.int32, device="cuda")
+        self.run = lambda: dk.beam_select(len(cu) - 1, rows, cu_dev, self.logits, code, vocab, vocab, self.scores, n, *self.out, ws, scale=scale)
+
+    def __call__(self, scores):
+        self.scores.copy_(torch.from_numpy(scores))
+        for o in self.out:
+            o.fill_(-7)
+        self.run()
+        torch.cuda.synchronize()
+        return [o.cpu().numpy() for o in self.out]
+
+    def shortest_us(self, scores, times=15):
+        self.scores.copy_(torch.from_numpy(scores))
+        took = []
+        for _ in range(times):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            self.run()
+            b.record()
+            b.synchronize()
+            took.append(a.elapsed_time(b) * 1e3)
+        return min(took)
+
+
+def check(got, want, n):
+    s = want[2]
+    gaps = s[:, :-1] - s[:, 1:]
+    assert ((gaps == 0) | (gaps > 2 * SUM_TOL)).all(), "inputs with continuations that are too close to tell apart"
+    assert np.array_equal(got[0], want[0][:, :n]) and np.array_equal(got[1], want[1][:, :n])
+    assert (np.abs(got[2] - s[:, :n]) <= SUM_TOL + 2.0 ** -24 * (np.abs(s[:, :n]) + 1)).all()
+
+
+def spread_scores(seed, rows, offset):
+    return (np.random.default_rng(seed).standard_normal(rows) * 2 + offset).astype(np.float32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [16, 64])
+@pytest.mark.parametrize("offset", [-20.0, -300.0, -700.0, -40000.0, 5000.0])
+def test_far_scores(dtype, n, offset):
+    x, scores = logits_of(1, dtype), spread_scores(2, ROWS, offset)
+    check(Call(x, [0, ROWS], n, dtype)(scores), best(x, scores, [0, ROWS], n + 1), n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_far_scores_that_differ_by_much(dtype):
+    """Rows hundreds apart, one group near zero and one far from it, a row that takes no part."""
+    x = logits_of(3, dtype, 12, 40000)
+    scores = spread_scores(4, 12, -3.0)
+    scores[:4] += np.float32([-300, -700, 0, -4])
+    scores[6:] += np.float32([-900, -901, -1500, -900.5, -903, -2000])
+    scores[8] = -np.inf
+    want = best(np.delete(x, 8, 0), np.delete(scores, 8), [0, 6, 11], 41)
+    want[0][want[0] >= 8] += 1
+    check(Call(x, [0, 6, 12], 40, dtype)(scores), want, 40)
+
+
+@pytest.mark.parametrize("n", [16, 64])
+def test_far_scores_take_no_longer(n):
+    """The same logits behind scores near -20 and far below: the bound that continuations have to reach is as tight.
+
+    (With a bound of as many bits of the score itself, a call on these took many times as long.)"""
+    x = logits_of(1, "bf16")
+    call = Call(x, [0, ROWS], n, "bf16")
+    near, far = spread_scores(2, ROWS, -20.0), [spread_scores(2, ROWS, o) for o in (-300.0, -700.0, -5000.0)]
+    call.shortest_us(near)
+    us = call.shortest_us(near)
+    for scores in far:
+        took = call.shortest_us(scores)
+        print(f"n {n}: {us:.1f} us near zero, {took:.1f} us at {scores.mean():.0f}", flush=True)
+        assert took <= 2 * us
