@@ -438,7 +438,9 @@ int32_t dk_token_logprobs(int32_t total_rows, const void* logits, int32_t dtype,
  *                 continuations the rest are -1, -1 and -infinity
  *   scale         the inverse of the temperature, 2^-20 .. 2^20;  n_out  1 .. 64;  vocab <= 2^20 (DK_ERR_UNSUPPORTED otherwise)
  *   workspace     DEVICE, 256-byte aligned, >= dk_beam_workspace_bytes() for the same arguments
- * Scores are made and compared in fp64 from sums in fp32, 1e-7 of a log probability.  total_rows < 2^24, less than 2^35 logits in all.
+ * Scores are made and compared in fp64 from row sums in fp32.  A sum's roundings are 2^-24 x 148 (9e-6 of a log probability) at the very most
+ * and come to less than 4e-7 for normally distributed logits of up to 128 256 tokens; rows round their sums differently, so continuations of
+ * different rows that are closer than that may come in either order.  total_rows < 2^24, less than 2^35 logits in all.
  * Asynchronous on `stream`; stateless, needs no pool; allocates nothing.
  */
 int32_t dk_beam_workspace_bytes(int32_t total_rows, int64_t vocab, int32_t dtype, int32_t n_out, int64_t* bytes_out);

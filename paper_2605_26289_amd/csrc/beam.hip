@@ -51,6 +51,10 @@ struct BeamPart {
 // A lane and the largest of its logits.  0: none.
 typedef uint64_t Entry;
 
+// Of a logit, in log2 units.  Rounded once: its error moves every term of a row's sum the same way, ln sum by up to as many times 2^-24 as
+// the mean term is nats below the largest.
+__device__ __forceinline__ float beam_factor(const BeamArgs& a) { return (float)(a.scale * 1.4426950408889634); }
+
 // Whole numbers in the order of the doubles (no NaN).  0: none.
 __device__ __forceinline__ uint64_t ordered64(double x) {
   const uint64_t b = (uint64_t)__double_as_longlong(x + 0.0);
@@ -160,7 +164,7 @@ __global__ __launch_bounds__(LP_THREADS) void beam_chunk_kernel(BeamArgs a, int3
 #pragma unroll
   for (int e = 0; e < N; e += 2) asm("v_max3_f32 %0, %1, %2, %3" : "=v"(mine) : "v"(mine), "v"(x[e]), "v"(x[e + 1]));
   const float m = over_lanes(mine, [](float p, float q) { return fmaxf(p, q); });
-  const float c = (float)a.scale * LOG2E, mr = m == -INFINITY ? 0.f : m, mc = mr * c;
+  const float c = beam_factor(a), mr = m == -INFINITY ? 0.f : m, mc = mr * c;
   float s0 = 0.f, s1 = 0.f;
   // (eight at a time: an exponential's result may not be used by the very next instruction)
   const auto sums = [&](auto y) __attribute__((always_inline)) {
@@ -257,7 +261,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
   // the rows' sums, `per` lanes to a row
   int per = 1;
   while (per < 64 && per < n_chunks) per *= 2;
-  const float c = (float)(a.scale * 1.4426950408889634);  // (chunks' weights in fp32, as their sums: 2^-22 of the row's sum at the most)
+  const float c = beam_factor(a);  // (chunks' weights in fp32, as their sums: 2^-22 of the row's sum at the most)
   for (int at = 0; at < rows; at += BEAM_THREADS / per) {
     const int r = at + tid / per, s = tid % per;
     const bool there = r < rows;

@@ -114,3 +114,27 @@ def test_far_scores_take_no_longer(n):
         took = call.shortest_us(scores)
         print(f"n {n}: {us:.1f} us near zero, {took:.1f} us at {scores.mean():.0f}", flush=True)
         assert took <= 2 * us
+
+
+@pytest.mark.parametrize("scale", [0.700066, 0.695115, 0.70306, 0.709371])
+def test_the_scale_is_rounded_once(scale):
+    """A row whose sum shows little but how scale log2(e) was rounded.
+
+    Every chunk of 4096 (256 lanes of 2 x 8) holds one 0 among the first wavefront's logits and 3072 of -8 among those of the other three: sums
+    within a wavefront are whole numbers, S = 1 + 3072 w with w = 2^(-8 c), and c is all that is rounded in -8 c.  In steps of 2^-24: of w
+    two (the exponential's last place) and 8 scale times the error of c, each by the share W = 3072 w / S; of the three sums of
+    wavefronts one each, by the partial sum's size.  The chunks' sums are added in fp64.  (With scale and log2(e) rounded before their
+    product ln S was 9.6 steps off and more, by arithmetic.)"""
+    vocab = 32 * 4096
+    x = np.full((32, 2, 256, 8), -8.0, np.float32)
+    x[:, :, :64] = -np.inf
+    x[:, 0, 0, 0] = 0.0
+    x = x.reshape(1, vocab)
+    exact = scale * 1.4426950408889634
+    w = 3072 * np.exp(-8 * scale)
+    steps = w / (1 + w) * (2 + 2.0 ** 24 * abs(float(np.float32(exact)) / exact - 1) * 8 * scale) + (3 + 2 * w) / (1 + w)
+    ln_s = np.log(32 * (1 + w))
+    score = np.float32(ln_s + 1 / 64)
+    got = Call(x, [0, 1], 1, "bf16", scale)(np.float32([score]))
+    assert got[0][0, 0] == 0 and got[1][0, 0] == 0
+    assert abs(float(got[2][0, 0]) - (float(score) - ln_s)) <= 2.0 ** -24 * (steps + 0.1)  # (the result is 1/64: its own rounding is 2^-31)
