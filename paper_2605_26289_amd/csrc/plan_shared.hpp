@@ -49,12 +49,12 @@ struct SharedPlan {
   std::vector<Pool::Part> parts;   // the entries' chains
   std::vector<int32_t> part0;      // first part of every entry
   std::vector<int64_t> n;          // cached tokens of every entry before the call
-  std::vector<Member> members, spare;
+  std::vector<Member> members;
   std::vector<Task> tasks;
   std::vector<Link> links;
   std::vector<Node> nodes;
   std::vector<DkShSeg> node_segs;
-  std::vector<int32_t> order, place;
+  std::vector<int32_t> order;
 
   std::vector<int32_t> starts;     // first work item of every node, and behind the last
   std::vector<DkShNode> out_nodes;
