@@ -245,8 +245,9 @@ struct SharedGeo {
 
 // A tile of up to 128 rows: each wavefront has 32 of them, the keys go through LDS once for all, and the products of tile t + 1 stand among
 // the instructions that turn those of tile t into weights, as in scored_rows_kernel.  Bound by the vector unit and the matrix pipe in turn:
-// 2.2 to 2.6 us for 64 keys of 128-wide heads with two workgroups to a compute unit, some 900 TFLOP/s in the steady state.  16 turns of 64
-// to 512 tokens behind one preamble, 326 GFLOP: 385 us, 850 TFLOP/s; 32 drafts of up to nine tokens behind 30 000 keys, 72 GFLOP: 102.
+// 2.2 to 2.6 us for 64 keys of 128-wide heads with two workgroups to a compute unit.  16 turns of 64 to 512 tokens behind one preamble, 326
+// GFLOP: calls of 383 to 390 us, 840 to 850 TFLOP/s; one after the other for 25 ms, in a trace, 392 to 456, 411 on average.  32 drafts of up to nine tokens
+// behind 30 000 keys, 72 GFLOP: 102 to 135 in such a trace, 119 on average.
 // (128 rows rather than 256: a second workgroup's softmax runs beside the first one's products, and a group of a few sessions fills a tile.)
 template <int HD>
 __device__ __forceinline__ void many_rows(const SharedArgs& a, const ScoreParams& sp, const Job& j, int g, char* smem, int lane, int wave) {
@@ -381,7 +382,7 @@ __device__ __forceinline__ void many_rows(const SharedArgs& a, const ScoreParams
 
 // A tile of up to 32 RB rows: each wavefront walks a quarter of the keys through LDS of its own, with no barrier until their
 // sums are joined.  K of tile t + 1 is requested as soon as K of tile t has been read, V likewise.  Bound by HBM where the keys come from
-// there: 16 requests of eight beams, 328 MB, 46.6 to 50 us, 6.5 to 7 TB/s; by latency where they are few: an item without its keys takes
+// there: 16 requests of eight beams, 328 MB, 47 to 49 us on average (least 44), 6.7 to 7 TB/s; by latency where they are few: an item without its keys takes
 // 5.5 us (descriptors 1, first requests and Q 1.5, four wavefronts' sums 1.5), four beams behind 3000 keys 7.3 in all.  One stage of K
 // and V for a wavefront, and not two as in scored_few_kernel, so that two workgroups fit a compute unit: one's start and end
 // are covered by the other.
@@ -575,8 +576,8 @@ __global__ __launch_bounds__(256, 2) void shared_attend_kernel(SharedBlob blob, 
 }
 
 // Joins the partial rows of every row.  HD / 4 lanes take a row's depths; `spread` lane groups of a workgroup share its pieces.  Bound by
-// latency, a chain of round trips: block, node and sources, partial rows (the first from the arguments, which are in host memory).  4 us for
-// four rows of 25 pieces, 6.5 to 7 for 64 to 128 beams, 9.2 for 32 drafts of up to nine tokens.
+// latency, a chain of round trips: block, node and sources, partial rows (the first from the arguments, which are in host memory).  On average
+// 4.9 us for four rows of 25 pieces (least 4.0), 6.7 to 7.2 for 64 to 128 beams, 10.6 for 32 drafts of up to nine tokens (least 9.1).
 template <int HD, bool F32>
 __global__ __launch_bounds__(256) void shared_merge_kernel(SharedBlob blob, SharedArgs a, SharedMergeArgs ma) {
   constexpr int LANES = HD / 4, GROUPS = 256 / LANES, AHEAD = 4;

@@ -16,9 +16,9 @@
 // Scores are made and compared in fp64: rows of one group differ by the logs of sums of 10^5 terms, and two continuations may be close.
 //
 // Measured (kernel times): 64 groups of eight rows of 128 256 bf16 logits, n = 16: chunks 24.6 us (131 MB, 5.3 TB/s; some 450 vector
-// instructions a wavefront keep the SIMDs busy three fifths of that, six wavefronts to a SIMD instead of five give 2 %), groups 12.7; with
-// lists of the n best logits themselves, put in order, the chunks took 36.  One group of four such rows, n = 8: 3.6 and 10.2; 40 groups
-// of up to ten rows of 50 003 fp32 logits, a third of them nearly all -infinity: 10.7 and 12.2.  The groups' kernel is a chain of round trips and of
+// instructions a wavefront keep the SIMDs busy three fifths of that, six wavefronts to a SIMD instead of five give 2 %), groups 12.3; with
+// lists of the n best logits themselves, put in order, the chunks took 36.  One group of four such rows, n = 8: 3.5 and 10.2; 40 groups
+// of up to ten rows of 50 003 fp32 logits, a third of them nearly all -infinity: 10.6 and 12.2.  The groups' kernel is a chain of round trips and of
 // exchanges over LDS: load 1.1 us, sums 1.2 to 1.7, T 1.3, lists 1.8 to 2.6, logits 2 to 4, places 0.5 to 1; of 256 lanes instead
 // of 512 it takes 10.3, 14.7 and 14.0, of 1024 10.8, 14.5 and 13.2.
 #include <hip/hip_runtime.h>
@@ -464,7 +464,8 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_select_kernel(BeamArgs a, i
         expand();
       }
     } else {
-      // more lanes than there is room for: T from those that came, and the lists again; if that is no higher, list by list
+      // more lanes than there is room for: T from those that came, and the lists again; if that is no higher, list by list (equal logits by the
+      // thousand where the n-th best is one of them: four rows of 30 000 take 0.29 ms, eight of 128 256 1.74)
       const uint64_t higher = score_at(nth_largest(lane_key, BEAM_LANES));
       if (higher > least.score) {
         least = {higher, 0};

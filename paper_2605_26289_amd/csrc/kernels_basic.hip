@@ -135,8 +135,8 @@ hipError_t launch_kv_scatter_runs(const ArenaView& a, void* k_arena, void* v_are
 // Reordered states: what a child's state has of its own, copied into its cells.  Workgroup (2 m + v, y): 32 KiB of K (v 0) or V of move m,
 // its heads one behind the other, eight 16-byte loads of a lane on their way before the first store.  Bound by latency: arguments and
 // the move come from host memory in one round trip, which a division by an argument in front of the move made two.  One to three copies of
-// up to 63 cells of 8 heads of 128 (0.26 MB read and written each): 4.8 us; 50 of them, half as long
-// on average, 7.6 for 13 MB.
+// up to 63 cells of 8 heads of 128 (0.26 MB read and written each): 5.2 us on average, 4.8 at least; 50 of them, half as long, 10.3 on
+// average and 7.6 at least for 13 MB.
 constexpr int KV_MOVE_LOADS = 8, KV_MOVE_VECS = 256 * KV_MOVE_LOADS;
 static_assert(sizeof(KvMoves) + 96 <= 4096, "kernel arguments are limited to 4 KiB");
 __global__ __launch_bounds__(256) void kv_move_kernel(KvMoves moves, uint4* __restrict__ k_arena, uint4* __restrict__ v_arena,
