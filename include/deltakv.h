@@ -156,7 +156,8 @@ int32_t dk_seq_trim_batch(dk_pool* pool, int32_t n_seqs, const int32_t* slots, c
  * do every slot's newest tokens: up to four times the cells that the slots see, and a granule a slot.
  * DK_ERR_INVALID (a parent out of range), DK_ERR_NO_SLOT, DK_ERR_DUP_SLOT, and DK_ERR_NO_CELLS unless the arena has a free granule for
  * every copy -- cells that no slot sees any more are free (to whole granules) after the call, not during it -- leave every slot as it was.
- * Cells are chosen at call time: a captured call replays its copies, not the bookkeeping.
+ * Cells are chosen at call time: a captured call replays its copies, not the bookkeeping.  Other threads' calls on the pool's slots wait
+ * until the copies are enqueued.
  */
 int32_t dk_seq_reorder(dk_pool* pool, int32_t n, const int32_t* slots, const int32_t* parents, void* stream);
 

@@ -138,3 +138,67 @@ def test_the_scale_is_rounded_once(scale):
     got = Call(x, [0, 1], 1, "bf16", scale)(np.float32([score]))
     assert got[0][0, 0] == 0 and got[1][0, 0] == 0
     assert abs(float(got[2][0, 0]) - (float(score) - ln_s)) <= 2.0 ** -24 * (steps + 0.1)  # (the result is 1/64: its own rounding is 2^-31)
+
+
+def check_every_way(x, scores, cu, n, dtype, scale):
+    """What holds however close scores are: every continuation is one, none twice, its score is right, those of a row are in the row's exact
+    order (their differences have no part in the row's sum), rows are in order within the roundings, and nothing better is left out."""
+    got = Call(x, cu, n, dtype, scale)(scores)
+    for g in range(len(cu) - 1):
+        rows = slice(cu[g], cu[g + 1])
+        y = scale * x[rows].astype(np.float64)
+        top = y.max(1, keepdims=True)
+        with np.errstate(invalid="ignore"):
+            s = scores[rows, None].astype(np.float64) + (y - top) - np.log(np.exp(y - top).sum(1, keepdims=True))
+        s[~np.isfinite(scores[rows])] = -np.inf
+        r, t, out = got[0][g] - cu[g], got[1][g], got[2][g]
+        count = min(n, int(np.isfinite(s).sum()))
+        assert (got[0][g][count:] == -1).all() and (t[count:] == -1).all() and np.isneginf(out[count:]).all()
+        r, t, out = r[:count], t[:count], out[:count]
+        assert (r >= 0).all() and (r < s.shape[0]).all() and (t >= 0).all() and (t < s.shape[1]).all()
+        assert len(set(zip(r.tolist(), t.tolist()))) == count
+        mine = s[r, t]
+        assert (np.abs(out - mine) <= SUM_TOL + 2.0 ** -24 * (np.abs(mine) + 1)).all()
+        assert (mine[:-1] - mine[1:] >= -2 * SUM_TOL).all()
+        taken = np.zeros(s.shape, bool)
+        taken[r, t] = True
+        assert not (~taken & (s > mine[-1] + 2 * SUM_TOL)).any()
+        for row in set(r.tolist()):
+            of = t[r == row]
+            order = np.lexsort((np.arange(s.shape[1]), -x[cu[g] + row].astype(np.float64)))[:len(of)]
+            assert np.array_equal(of, order)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [504, 6552, 20000])
+@pytest.mark.parametrize("lead,offset", [(None, -20.0), (18.0, -20.0), (None, -800.0), (18.0, -800.0), (0.0, -800.0)])
+def test_first_steps_and_rows_that_lead(dtype, vocab, lead, offset):
+    x, scores = logits_of(31, dtype, 60, vocab), spread_scores(32, 60, offset)
+    if lead is None:
+        scores[[i for i in range(60) if i not in (5, 28)]] = -np.inf
+    else:
+        scores[[5, 28]] += np.float32(lead)
+    for n in (1, 8, 32, 64):
+        check_every_way(x, scores, [0, 28, 60], n, dtype, 0.69)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("offset", [0.0, -700.0])
+def test_more_lanes_reach_the_first_bound_than_there_is_room_for(dtype, offset):
+    x = logits_of(33, dtype, 40, 60000)
+    scores = (-20.0 - np.linspace(0, 1, 40)).astype(np.float32)
+    scores[[7, 21]] = -14.5, -13.8
+    for n in (5, 63, 64):
+        check_every_way(x, scores + np.float32(offset), [0, 40], n, dtype, 1.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("offset", [-20.0, -700.0])
+def test_masks_of_the_lowest_value_that_leave_fewer_than_n(dtype, offset):
+    """Three tokens a row are allowed, the others hold the type's lowest value: continuations all the same, equal ones by the thousand."""
+    lowest = float(torch.finfo(torch.bfloat16).min) if dtype == "bf16" else -3e38
+    x = np.full((6, 9000), lowest, np.float32)
+    x[:, [5, 700, 8999]] = logits_of(34, dtype, 6, 8)[:, :3]
+    scores = spread_scores(35, 6, offset)
+    for n in (12, 40):
+        check_every_way(x, scores, [0, 4, 6], n, dtype, 1.0)
