@@ -102,10 +102,18 @@ void GranuleAllocator::give_back(int64_t g) noexcept {
 
 // ---------------------------------------------------------------- Node
 Node::~Node() {
-  if (borrow_cap > 0 && parent) parent->tail_lent = false;  // nothing refers to the borrowed cells any more
   if (!granules.empty()) alloc->unmark_tail(granules.back());
   for (int64_t g : granules) alloc->give_back(g);
-  if (parent) parent->drop_child(base);
+  // Those in front that only this one held go one by one: a chain may be longer than the stack is deep.
+  for (std::shared_ptr<Node> up = leave_parent(); up && up.use_count() == 1;) up = up->leave_parent();
+}
+
+std::shared_ptr<Node> Node::leave_parent() noexcept {
+  if (parent) {
+    if (borrow_cap > 0) parent->tail_lent = false;  // nothing refers to the borrowed cells any more
+    parent->drop_child(base);
+  }
+  return std::move(parent);
 }
 
 void Node::add_child(int64_t at) {

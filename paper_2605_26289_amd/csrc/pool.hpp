@@ -74,6 +74,7 @@ struct Node {
   int64_t granules_needed(int64_t extra) const;  // granules an append of `extra` tokens must add
   void grow(int64_t extra, bool anywhere = false);  // caller has checked the allocator holds enough; anywhere: a first granule fills a gap
   void shrink_to(int64_t new_len) noexcept;      // own length, frees whole unused granules
+  std::shared_ptr<Node> leave_parent() noexcept;
   void add_child(int64_t at);
   void drop_child(int64_t at) noexcept;
   void cut_back() noexcept;  // no owner: what lies behind the last child's base is nobody's

@@ -1,4 +1,6 @@
 // The bookkeeping of reordered states where something goes wrong on the way, on the host.  One check a run, by its name.
+#include <pthread.h>
+
 #include <atomic>
 #include <chrono>
 #include <cstdio>
@@ -379,6 +381,36 @@ static void cells_come_back() {
   }
 }
 
+// A search's chain of nodes is as long as the search: letting go of it does not need a stack as deep.
+static void long_chains() {
+  const int steps = 20000;
+  Pool pool(2, 0, 2 * steps + 64, 1);
+  const std::vector<int32_t> slots = {slot_of(pool, 1), slot_of(pool, 1)}, cu = {0, 1, 2};
+  for (int step = 0; step < steps; ++step) {
+    const int32_t parent = step & 1;
+    CHECK(reorder(pool, slots, {parent, parent}) == OK);
+    CHECK(pool.append(2, slots.data(), cu.data(), nullptr, nullptr) == OK);
+  }
+  int64_t runs = 0, depth = 0, len = 0;
+  CHECK(pool.seq_stats(slots[0], &runs, &depth) == OK && depth > steps / 2);
+  CHECK(pool.length(slots[0], &len) == OK && len == steps + 1);
+  pthread_attr_t small;
+  pthread_attr_init(&small);
+  pthread_attr_setstacksize(&small, 512 << 10);
+  struct Both {
+    Pool* pool;
+    const std::vector<int32_t>* slots;
+  } both{&pool, &slots};
+  pthread_t t;
+  CHECK(pthread_create(&t, &small, [](void* p) -> void* {
+    const Both& b = *(const Both*)p;
+    for (int32_t s : *b.slots) CHECK(b.pool->release(s) == OK);
+    return nullptr;
+  }, &both) == 0);
+  pthread_join(t, nullptr);
+  CHECK(held(pool) == 0);
+}
+
 int main(int argc, char** argv) {
   const char* what = argc > 1 ? argv[1] : "";
   if (!std::strcmp(what, "granules")) granules();
@@ -386,6 +418,7 @@ int main(int argc, char** argv) {
   else if (!std::strcmp(what, "out_of_memory")) out_of_memory();
   else if (!std::strcmp(what, "one_step")) one_step();
   else if (!std::strcmp(what, "cells_come_back")) cells_come_back();
+  else if (!std::strcmp(what, "long_chains")) long_chains();
   else if (!std::strcmp(what, "threads")) threads();
   else return 2;
   std::printf("ok\n");

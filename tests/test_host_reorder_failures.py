@@ -54,3 +54,8 @@ def test_searches_on_several_threads(tmp_path, sanitizer):
 @pytest.mark.parametrize("sanitizer", [None, "address,undefined"])
 def test_cells_that_no_slot_sees_come_back(tmp_path, sanitizer):
     run_check(tmp_path, "cells_come_back", sanitizer)
+
+
+@pytest.mark.parametrize("sanitizer", [None, "address,undefined"])
+def test_long_chains_are_let_go_of(tmp_path, sanitizer):
+    run_check(tmp_path, "long_chains", sanitizer)
